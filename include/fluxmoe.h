@@ -33,7 +33,8 @@
  *           failure on the calling thread.  No C++ exception crosses the ABI.
  * Outputs.  Fully overwritten, except `counts` of moe_profile_hist and
  *           moe_profile_route (adds) and
- *           the weight gradients of moe_grouped_swiglu_bwd when accumulate_dw.
+ *           the weight gradients of moe_grouped_swiglu_bwd, moe_router_bwd and
+ *           moe_sublayer_norm_bwd when accumulate_dw.
  */
 #ifndef FLUXMOE_H
 #define FLUXMOE_H
@@ -93,6 +94,66 @@ int moe_route_topk(const void* X, const void* Wr, int dtype, const float* bias,
  */
 int moe_route_bwd(const float* gate, const int32_t* idx, const float* dgate, const void* Wr, int dtype,
                   int T, int d, int E, int k, void* dX, int accumulate, void* stream);
+
+/* moe_balance_loss: the auxiliary loss that keeps a router from sending every
+ * token to a few experts while it is trained (the skew of Section 2.2,
+ * Observation 2, left to itself, grows), one loss per sequence, averaged over
+ * the tokens, and the per-expert counts it is made of.  With p[t,:] the softmax
+ * of logits[t,:] over all E experts, sequence b the tokens [seg[b], seg[b+1])
+ * whose keep flag is set, n_b their number and n = sum_b n_b:
+ *   counts[b,e] = choices idx[t,j] == e of the tokens of b
+ *   dprob[b,e]  = coef * E * counts[b,e] / (k * n * n_b)     (0 when n_b = 0)
+ *   loss[0]     = sum_b sum_e dprob[b,e] * sum_{t in b} p[t,e]
+ * (coef * sum_b (n_b / n) * E * sum_e f_e P_e with f the sequence's shares of
+ * choices and P its mean probabilities: coef when both are even).  dprob is the
+ * loss's derivative by each p[t,e] of the sequence with the counts held fixed;
+ * moe_balance_loss_bwd takes it.
+ * logits [T,E] fp32, as moe_route_topk writes them; -inf is an expert of
+ * probability 0, and a row of nothing but -inf has no probabilities (its
+ * choices count, its p are 0).  idx [T,k]; entries outside [0, E) count nowhere.
+ * seg [B+1] int32 (device, non-decreasing, values clamped to [0, T]; tokens
+ * outside [seg[0], seg[B]) belong to no sequence) or NULL: one sequence of all
+ * T tokens, B = 1.  keep [T] uint8 or NULL (all): tokens with 0 (padding) are
+ * left out, and their logits are not looked at.  counts [B,E] int32, dprob
+ * [B,E] fp32 and loss [1] fp32 are overwritten, also when T == 0.
+ * coef finite; 1 <= B <= 4096; E and k as for moe_route_topk.  Sums over tokens run
+ * in a fixed order (fp32 within at most 64 tokens, fp64 above).
+ */
+int moe_balance_loss(const float* logits, const int32_t* idx, const int32_t* seg, const uint8_t* keep,
+                     int T, int E, int k, int B, float coef,
+                     int32_t* counts, float* dprob, float* loss, void* ws, size_t ws_bytes, void* stream);
+size_t moe_balance_loss_workspace_size(int T, int E, int B);
+
+/* moe_balance_loss_bwd: the gradient of the router's logits, dense over the
+ * experts: the balance loss's share through the softmax over all E, and, when
+ * gate, idx and dgate are given (all three or none), the gates' share of
+ * moe_route_bwd with the selection held fixed:
+ *   dlogits[t,e] = dloss[0] * p[t,e] * (dprob[b,e] - sum_i p[t,i] dprob[b,i])
+ *                  + sum_{j: idx[t,j] = e} gate[t,j] * (dgate[t,j] - sum_i gate[t,i] dgate[t,i])
+ * b the token's sequence; the first term is 0 for tokens that keep or seg
+ * leave out, and for rows without probabilities.  dloss [1] fp32 (device), the
+ * gradient of the loss, or NULL (1).  logits, seg, keep, T, E, B as given to
+ * moe_balance_loss and dprob as it left it; dlogits [T,E] fp32, may alias logits.
+ * k is read only when gate, idx and dgate are given.
+ */
+int moe_balance_loss_bwd(const float* logits, const float* dprob, const float* dloss, const int32_t* seg,
+                         const uint8_t* keep, const float* gate, const int32_t* idx, const float* dgate,
+                         int T, int E, int k, int B, float* dlogits, void* stream);
+
+/* moe_router_bwd: the products of the router's backward for a dense gradient
+ * of its logits (moe_route_bwd forms dX alone, of the selected experts alone):
+ *   dX    = (accumulate_dx ? dX : 0) + dlogits Wr        [T,d] dtype, one rounding
+ *   dWr   = (accumulate_dw ? dWr : 0) + dlogits^T X      [E,d] fp32
+ *   dbias = (accumulate_dw ? dbias : 0) + sum_t dlogits  [E] fp32
+ * Each output may be NULL (not formed); X is read for dWr only, Wr for dX only
+ * (NULL where unused).  Sums in fp32, in a fixed order; dlogits keep 24 bits
+ * in dWr and 16 in a bf16 dX.  With T == 0, dWr and dbias become 0 unless accumulating.
+ * X [T,d] and Wr [E,d] in dtype; dlogits [T,E] fp32.  dX may not alias X.
+ */
+int moe_router_bwd(const float* dlogits, const void* X, const void* Wr, int dtype, int T, int d, int E,
+                   void* dX, int accumulate_dx, float* dWr, float* dbias, int accumulate_dw,
+                   void* ws, size_t ws_bytes, void* stream);
+size_t moe_router_bwd_workspace_size(int T, int d, int E);
 
 /* ------------------------------------------------- quantisation profiling --
  * moe_quantize_int8: the low-bit profiling copy of a weight matrix
@@ -162,6 +223,74 @@ int moe_residual_add(const void* X, const void* Y, int T, int d, int dtype,
  */
 int moe_rms_norm(const void* X, const void* Y, int T, int d, int dtype, float eps,
                  void* out_sum, void* out_norm, void* stream);
+
+/* moe_sublayer_norm: what stands around a block of the models that are tuned
+ * (pre-norm transformers; the paper's blocks carry learned gains, some a norm
+ * after the block too), in one pass over the rows: the block's output Y goes
+ * through its post-norm, gate and the residual scale into the stream, and the
+ * stream through the next block's pre-norm:
+ *   u = post_norm ? Y * rstd_y : Y      rstd_y[t] = 1 / sqrt(mean_i Y[t,i]^2 + eps)
+ *   S = alpha * X + gate[t] * (u * w_post)              (fp32, one rounding)
+ *   N = S * rstd_s * w_pre              rstd_s[t] = 1 / sqrt(mean_i S[t,i]^2 + eps)
+ * (N from the rounded S, one rounding; a zero row with eps = 0 has rstd 0).
+ * With post_norm = 0, w_post is a layer scale.  Y NULL: the pre-norm alone, S =
+ * alpha * X; gate, w_post and rstd_y must then be NULL and post_norm 0.
+ * X, Y, S, N [T,d] in dtype; gate [T], w_post, w_pre [d] fp32 or NULL (1);
+ * S NULL: not stored; N NULL: not formed (the last block), rstd_s then NULL.
+ * rstd_y, rstd_s [T] fp32 or NULL: kept for the backward.  S and N may alias X
+ * or Y, not each other.  alpha finite, eps finite and >= 0; d % 8 == 0, d <= 8192.
+ */
+int moe_sublayer_norm(const void* X, const void* Y, const float* gate, const float* w_post, const float* w_pre,
+                      int T, int d, int dtype, float alpha, int post_norm, float eps,
+                      void* S, void* N, float* rstd_y, float* rstd_s, void* stream);
+
+/* moe_sublayer_norm_bwd: its backward, from the gradients dS of the stream and
+ * dN of the normalised stream (either may be NULL, 0):
+ *   xh = S * rstd_s,   q = dN * w_pre
+ *   D  = dS + rstd_s * (q - xh * mean_i(q xh))            (fp32)
+ *   dX = alpha * D
+ *   dgate[t] = sum_i D u w_post,   dv = gate[t] * D * w_post
+ *   dY = post_norm ? rstd_y * (dv - u * mean_i(dv u)) : dv
+ *   dw_post = sum_t gate[t] * D * u,   dw_pre = sum_t dN * xh
+ * S, Y, rstd_s, rstd_y as the forward left them (S and rstd_s are read only
+ * with dN, rstd_y only with post_norm); gate, w_post, w_pre, alpha, post_norm
+ * as the forward had them.  Each of dX, dY [T,d] dtype, dgate [T], dw_post,
+ * dw_pre [d] fp32 may be NULL (not formed); Y NULL: only dX and dw_pre.  dw_pre
+ * without dN is 0.  accumulate_dw = 1 adds to dw_post and dw_pre.  dX and dY may
+ * alias any of S, Y, dS, dN, not each other.  Row sums and the sums over the rows run
+ * in fp32 in a fixed order.  Limits as for moe_sublayer_norm; with T == 0, dw_* become
+ * 0 unless accumulating.
+ */
+int moe_sublayer_norm_bwd(const void* dS, const void* dN, const void* S, const void* Y, const float* gate,
+                          const float* w_post, const float* w_pre, const float* rstd_y, const float* rstd_s,
+                          int T, int d, int dtype, float alpha, int post_norm,
+                          void* dX, void* dY, float* dgate, float* dw_post, float* dw_pre, int accumulate_dw,
+                          void* ws, size_t ws_bytes, void* stream);
+size_t moe_sublayer_norm_bwd_workspace_size(int T, int d);
+
+/* moe_quantize_mxfp4: the 4-bit profiling copy of a weight matrix (Section 4.1
+ * profiles with 4-bit copies), microscaled: a row's elements in blocks of 32
+ * share a power of two, an element is a 4-bit float (sign, 2 exponent bits, 1
+ * mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives).
+ *   byte  = max(floor(log2(max_i |W_i|)) - 2, -127) + 127      (block scale)
+ *   code  = nearest of the 8 magnitudes to |W_i| / 2^(byte - 127), ties to the
+ *           even code, above 6 to 6; bit 3 the sign
+ * A zero block has byte 0 and codes 0 or 8 (-0); a block with an infinity or a
+ * NaN has byte 255 (not a number) and codes 0.
+ * W [rows, cols] in dtype.  codes [rows, ceil(cols / 32) * 16] bytes, column
+ * 2i in the low and 2i + 1 in the high half of byte i; scale [rows,
+ * ceil(cols / 128) * 4] bytes; both are 0 past the row's columns and blocks.
+ * rows >= 1, cols % 8 == 0.
+ */
+int moe_quantize_mxfp4(const void* W, int dtype, long rows, int cols, uint8_t* codes, uint8_t* scale,
+                       void* stream);
+
+/* moe_dequant_mxfp4: the values the codes stand for, exact in both types down
+ * to 2^-126: out[r,c] = value(code) * 2^(byte - 127); byte 255 gives NaN.  Layouts
+ * as moe_quantize_mxfp4's; out [rows, cols] in out_dtype.
+ */
+int moe_dequant_mxfp4(const uint8_t* codes, const uint8_t* scale, long rows, int cols, int out_dtype,
+                      void* out, void* stream);
 
 /* ---------------------------------------------------------------- merging --
  * moe_merge_plan: which experts of one layer are merged, from its histogram
@@ -417,6 +546,37 @@ int moe_grouped_swiglu_fwd_q8(const moe_layer_q8* L, const void* X, const void* 
                               const int32_t* offsets, int T, int k, void* H, void* O,
                               void* ws, size_t ws_bytes, void* stream);
 size_t moe_grouped_swiglu_fwd_q8_workspace_size(const moe_layer_q8* L, int T, int k);
+
+/* moe_grouped_swiglu_fwd_mx4: the forward of the 4-bit profiling model, both
+ * operands of its products microscaled 4-bit rows (MX, moe_quantize_mxfp4's rule):
+ *   H = silu(MX(X_s) Q_gate^T) * (MX(X_s) Q_up^T)     (fp32 sums)
+ *   O = MX(H) Q_down^T                                (fp32 sums, one rounding)
+ * H is quantised from its fp32 values and not written out.  X [T,d] bf16 is
+ * quantised once per token; routed row p reads token perm_token[p]
+ * (moe_permute's; values clamped to [0, T)), so X_perm is not needed.  offsets,
+ * the row space and O [R_tot, d] bf16 as in moe_grouped_swiglu_fwd; O's rows
+ * behind the last routed one are left as they were.  The struct's tables are
+ * DEVICE arrays of S_routed + S_shared device pointers to moe_quantize_mxfp4's
+ * codes and scales of W_gate, W_up [I,d] and W_down [d,I] (codes 16-byte, scales
+ * 4-byte aligned; read on the device only, not checked).  d and I multiples of
+ * 8; d * I and T * d, both rounded up to 128 columns, at most 2^32.
+ */
+typedef struct moe_layer_mx4 {
+  int d;
+  int I;
+  int S_routed;
+  int S_shared;
+  const uint8_t* const* q_gate;
+  const uint8_t* const* q_up;
+  const uint8_t* const* q_down;
+  const uint8_t* const* s_gate;
+  const uint8_t* const* s_up;
+  const uint8_t* const* s_down;
+} moe_layer_mx4;
+int moe_grouped_swiglu_fwd_mx4(const moe_layer_mx4* L, const void* X, const int32_t* perm_token,
+                               const int32_t* offsets, int T, int k, void* O,
+                               void* ws, size_t ws_bytes, void* stream);
+size_t moe_grouped_swiglu_fwd_mx4_workspace_size(const moe_layer_mx4* L, int T, int k);
 
 /* moe_unpermute: the gate-weighted combine of the expert outputs, the output
  * of the MoE layer of Section 2.1 (each token's output is the sum of its

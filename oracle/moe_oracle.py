@@ -27,6 +27,12 @@ What each function follows:
 * Quantised profiling of a layer stack (Section 4.1): int8 router and experts,
   each layer reading the RMS-normalised stream (the pre-norm of the paper's
   models), layers coupled by a residual stream.
+* The same pass with 4-bit experts (Section 4.1 profiles with 4-bit copies),
+  microscaled: blocks of 32 along a row share a power of two.
+* What a router's training adds: a balance loss per sequence, its gradient and
+  the dense backward of the router's products.
+* The norms around a block with learned gains, gate and residual scale, and
+  their gradients.
 * Layer-aware merging (Section 5): the per-layer budget of Eq. 1 (Section 5.1),
   then PCA features of the experts' parameters and K-Means with cosine
   distance over all layers at once, cross-layer pairs masked (Section 5.2).
@@ -694,7 +700,7 @@ def rms_norm_rows(X, eps: float = 1e-6) -> np.ndarray:
     return X / np.where(den > 0, den, 1.0)
 
 
-def quantized_stack_profile(X0, layers: Sequence[Dict], k: int, eps: float = 1e-6):
+def quantized_stack_profile(X0, layers: Sequence[Dict], k: int, eps: float = 1e-6, experts: str = "int8"):
     """Profiling pass of Section 4.1 with a low-bit copy of a stack of MoE
     layers: each layer's router and expert matrices are quantised per row to
     int8 (quantize_int8_rows), and the layer runs on them — the int8 router's
@@ -707,6 +713,9 @@ def quantized_stack_profile(X0, layers: Sequence[Dict], k: int, eps: float = 1e-
     their input, make the stream grow without bound over a deep stack).
     layers[l]: dict with Wr [E,d], bias [E] or None, wg [E,I,d], wu [E,I,d],
     wd [E,d,I] and optionally sg, su, sd (shared experts).
+    experts = "mxfp4": the expert matrices are microscaled 4-bit rows, and so
+    are the activations in front of their products (swiglu_mx4_fwd); "mxfp4-weights":
+    only the matrices are (the fp32 stack runs on their values).
     Returns (counts [L][E] int64, idx [L][T,k], gate [L][T,k], X [L+1][T,d]).
     """
     X = _f64(X0)
@@ -724,6 +733,8 @@ def quantized_stack_profile(X0, layers: Sequence[Dict], k: int, eps: float = 1e-
         def deq(W):
             W = np.asarray(W)
             n = W.shape[0]
+            if experts != "int8":
+                return mxfp4_round(W.reshape(-1, W.shape[-1])).reshape(W.shape)
             qq, ss = quantize_int8_rows(W.reshape(-1, W.shape[-1]))
             return dequantize_rows(qq, ss).reshape(W.shape) if n else W
 
@@ -736,9 +747,167 @@ def quantized_stack_profile(X0, layers: Sequence[Dict], k: int, eps: float = 1e-
             wu = list(wu) + list(suq)
             wd = list(wd) + list(sdq)
         slots = SlotWeights(wg, wu, wd, [False] * (E + n_sh), n_shared=n_sh)
-        Y = moe_forward(Xn, idx, gate, np.arange(E), slots)
+        if experts == "mxfp4":
+            Y = sum((swiglu_mx4_fwd(Xn, wg[E + i], wu[E + i], wd[E + i])[1] for i in range(n_sh)), np.zeros_like(X))
+            for e in range(E):
+                t, j = np.nonzero(idx == e)
+                if len(t):
+                    Y[t] += gate[t, j][:, None] * swiglu_mx4_fwd(Xn[t], wg[e], wu[e], wd[e])[1]
+        else:
+            Y = moe_forward(Xn, idx, gate, np.arange(E), slots)
         X = X + Y
         idxs.append(idx)
         gates.append(gate)
         Xs.append(X)
     return counts, idxs, gates, Xs
+
+
+# --------------------------------------------- microscaled 4-bit profiling ----
+
+MXFP4_VALUES = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)   # by code
+
+
+def mxfp4_rows(W):
+    """(codes [rows, cols] in 0..15, byte [rows, ceil(cols / 32)]): blocks of 32
+    along the row share the scale 2^(byte - 127), byte = max(floor(log2 of the
+    block's largest magnitude) - 2, -127) + 127; an element takes the code of the
+    nearest of the 8 magnitudes times the scale, on a tie the even code, above the
+    largest the largest; code + 8 with the sign bit.  A zero block has byte 0."""
+    W = _f64(W)
+    rows, cols = W.shape
+    nb = -(-cols // 32)
+    codes = np.zeros((rows, cols), dtype=np.uint8)
+    byte = np.zeros((rows, nb), dtype=np.uint8)
+    for b in range(nb):
+        x = W[:, 32 * b:32 * b + 32]
+        top = np.abs(x).max(axis=1)
+        _, e = np.frexp(top)                       # top = m 2^e, m in [0.5, 1)
+        e = np.where(top > 0, np.maximum(e - 1 - 2, -127), -127)
+        byte[:, b] = e + 127
+        a = np.abs(x) / np.exp2(e.astype(F64))[:, None]
+        dist = np.abs(a[:, :, None] - np.array(MXFP4_VALUES))
+        # an odd code is moved back by less than any real difference of distances
+        codes[:, 32 * b:32 * b + 32] = np.argmin(dist * (1 + 1e-15) + 1e-14 * (np.arange(8) % 2), axis=2)
+    return codes + (np.signbit(W) * 8).astype(np.uint8), byte
+
+
+def mxfp4_values(codes, byte) -> np.ndarray:
+    """What codes and bytes stand for."""
+    codes = np.asarray(codes)
+    v = np.array(MXFP4_VALUES)[codes & 7] * np.where(codes & 8, -1.0, 1.0)
+    return v * np.repeat(np.exp2(np.asarray(byte, dtype=F64) - 127), 32, axis=1)[:, :codes.shape[1]]
+
+
+def mxfp4_round(W) -> np.ndarray:
+    return mxfp4_values(*mxfp4_rows(W))
+
+
+def swiglu_mx4_fwd(x, Wg, Wu, Wd):
+    """(H, O) of one expert of the 4-bit model: activations are quantised in front
+    of each product, Wg, Wu, Wd are values of quantised weights."""
+    xq = mxfp4_round(x)
+    a = xq @ _f64(Wg).T
+    H = a * sigmoid(a) * (xq @ _f64(Wu).T)
+    return H, mxfp4_round(H) @ _f64(Wd).T
+
+
+# -------------------------------------------------------- router's training ----
+
+def full_softmax(logits) -> np.ndarray:
+    """softmax over all experts; -inf is probability 0, a row of -inf is all 0."""
+    z = np.asarray(logits, dtype=F64)
+    m = z.max(axis=1, keepdims=True)
+    e = np.exp(z - np.where(np.isinf(m), 0.0, m))
+    return e / np.maximum(e.sum(axis=1, keepdims=True), np.finfo(F64).tiny)
+
+
+def balance_loss(logits, idx, k: int, coef: float, seg=None, keep=None):
+    """(counts [B,E], dprob [B,E], loss): one balance loss per sequence, averaged
+    over the kept tokens.  With f_e the share of the sequence's n_b k choices that
+    went to e, P_e its mean probability,
+        loss = coef sum_b (n_b / n) E sum_e f_e P_e,
+    and dprob its derivative by a token's p with the choices held fixed."""
+    p = full_softmax(logits)
+    T, E = p.shape
+    seg = [0, T] if seg is None else list(seg)
+    B = len(seg) - 1
+    keep = np.ones(T, dtype=bool) if keep is None else np.asarray(keep).astype(bool)
+    member = [np.array([t for t in range(seg[b], seg[b + 1]) if keep[t]], dtype=np.int64) for b in range(B)]
+    n = sum(len(m) for m in member)
+    counts, dprob, loss = np.zeros((B, E), dtype=np.int64), np.zeros((B, E)), 0.0
+    for b, m in enumerate(member):
+        if len(m) == 0:
+            continue
+        ch = np.asarray(idx)[m].ravel()
+        counts[b] = np.bincount(ch[(ch >= 0) & (ch < E)], minlength=E)
+        f, P = counts[b] / (len(m) * k), p[m].mean(axis=0)
+        loss += coef * len(m) / n * E * float(f @ P)
+        dprob[b] = coef * E * f / n
+    return counts, dprob, loss
+
+
+def balance_loss_backward(logits, dprob, dloss, seg=None, keep=None, gate=None, idx=None, dgate=None) -> np.ndarray:
+    """dlogits [T,E]: the loss's share through the softmax over all experts, and the
+    gates' share of route_topk_backward when gate, idx, dgate are given."""
+    p = full_softmax(logits)
+    T, E = p.shape
+    seg = [0, T] if seg is None else list(seg)
+    out = np.zeros((T, E))
+    for b in range(len(seg) - 1):
+        for t in range(seg[b], seg[b + 1]):
+            if keep is None or keep[t]:
+                out[t] = dloss * p[t] * (dprob[b] - p[t] @ dprob[b])
+    if gate is not None:
+        for t in range(T):
+            inner = float(np.dot(gate[t].astype(F64), dgate[t].astype(F64)))
+            for j, e in enumerate(np.asarray(idx)[t]):
+                if 0 <= e < E:
+                    out[t, e] += float(gate[t, j]) * (float(dgate[t, j]) - inner)
+    return out
+
+
+# -------------------------------------------------------- norms of a block ----
+
+def _rstd(v, eps):
+    ms = np.mean(v * v, axis=1, keepdims=True) + eps
+    return np.where(ms > 0, 1.0 / np.sqrt(np.where(ms > 0, ms, 1.0)), 0.0)
+
+
+def sublayer_norm(X, Y, gate=None, w_post=None, w_pre=None, alpha=1.0, post_norm=True, eps=1e-6):
+    """(S, N): the block's output Y through its post-norm, gain and gate onto alpha
+    times the stream X, and the stream through the next block's pre-norm."""
+    X = _f64(X)
+    S = alpha * X
+    if Y is not None:
+        Y = _f64(Y)
+        u = Y * _rstd(Y, eps) if post_norm else Y
+        v = u if w_post is None else u * _f64(w_post)
+        S = S + (v if gate is None else _f64(gate)[:, None] * v)
+    N = S * _rstd(S, eps)
+    return S, N if w_pre is None else N * _f64(w_pre)
+
+
+def sublayer_norm_backward(dS, dN, S, Y, rstd_s, rstd_y=None, gate=None, w_post=None, w_pre=None, alpha=1.0):
+    """Gradients of sublayer_norm from the stream S and the rows' scales that its
+    forward left; rstd_y None: no post-norm.  dict of dX, dw_pre and, with Y, dY,
+    dw_post, dgate.  With x = S r, dN/dS of a row is r (I - x x^T / d)."""
+    S = _f64(S)
+    d = S.shape[1]
+    r = _f64(rstd_s)[:, None]
+    x = S * r
+    dN = np.zeros_like(S) if dN is None else _f64(dN)
+    q = dN if w_pre is None else dN * _f64(w_pre)
+    D = r * q - x * r * (x * q).sum(axis=1, keepdims=True) / d
+    if dS is not None:
+        D = D + _f64(dS)
+    out = {"dX": alpha * D, "dw_pre": (dN * x).sum(axis=0)}
+    if Y is not None:
+        ry = 1.0 if rstd_y is None else _f64(rstd_y)[:, None]
+        u = _f64(Y) * ry
+        g = 1.0 if gate is None else _f64(gate)[:, None]
+        w = np.ones(d) if w_post is None else _f64(w_post)
+        dv = g * D * w
+        out["dY"] = dv if rstd_y is None else ry * dv - u * ry * (u * dv).sum(axis=1, keepdims=True) / d
+        out["dgate"] = (D * u * w).sum(axis=1)
+        out["dw_post"] = (g * D * u).sum(axis=0)
+    return out

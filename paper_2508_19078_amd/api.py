@@ -40,6 +40,12 @@ class moe_layer_q8(ctypes.Structure):
                 ("s_down", _vp)]
 
 
+class moe_layer_mx4(ctypes.Structure):
+    _fields_ = [("d", _c_int), ("I", _c_int), ("S_routed", _c_int), ("S_shared", _c_int),
+                ("q_gate", _vp), ("q_up", _vp), ("q_down", _vp), ("s_gate", _vp), ("s_up", _vp),
+                ("s_down", _vp)]
+
+
 # name -> (restype, argtypes)
 _SIGS = {
     "moe_last_error": (ctypes.c_char_p, []),
@@ -78,6 +84,22 @@ _SIGS = {
     "moe_dequant_int8": (_c_int, [_vp, _vp, ctypes.c_long, _c_int, _c_int, _vp, _vp]),
     "moe_residual_add": (_c_int, [_vp, _vp, _c_int, _c_int, _c_int, _vp, _vp]),
     "moe_rms_norm": (_c_int, [_vp, _vp, _c_int, _c_int, _c_int, _f, _vp, _vp, _vp]),
+    "moe_balance_loss": (_c_int, [_vp, _vp, _vp, _vp, _c_int, _c_int, _c_int, _c_int, _f, _vp, _vp, _vp, _vp, _c_size,
+                                  _vp]),
+    "moe_balance_loss_workspace_size": (_c_size, [_c_int, _c_int, _c_int]),
+    "moe_balance_loss_bwd": (_c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _c_int, _c_int, _c_int, _c_int, _vp, _vp]),
+    "moe_router_bwd": (_c_int, [_vp, _vp, _vp, _c_int, _c_int, _c_int, _c_int, _vp, _c_int, _vp, _vp, _c_int, _vp,
+                                _c_size, _vp]),
+    "moe_router_bwd_workspace_size": (_c_size, [_c_int, _c_int, _c_int]),
+    "moe_sublayer_norm": (_c_int, [_vp, _vp, _vp, _vp, _vp, _c_int, _c_int, _c_int, _f, _c_int, _f, _vp, _vp, _vp, _vp,
+                                   _vp]),
+    "moe_sublayer_norm_bwd": (_c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _c_int, _c_int, _c_int, _f, _c_int,
+                                       _vp, _vp, _vp, _vp, _vp, _c_int, _vp, _c_size, _vp]),
+    "moe_sublayer_norm_bwd_workspace_size": (_c_size, [_c_int, _c_int]),
+    "moe_quantize_mxfp4": (_c_int, [_vp, _c_int, ctypes.c_long, _c_int, _vp, _vp, _vp]),
+    "moe_dequant_mxfp4": (_c_int, [_vp, _vp, ctypes.c_long, _c_int, _c_int, _vp, _vp]),
+    "moe_grouped_swiglu_fwd_mx4": (_c_int, [_vp, _vp, _vp, _vp, _c_int, _c_int, _vp, _vp, _c_size, _vp]),
+    "moe_grouped_swiglu_fwd_mx4_workspace_size": (_c_size, [_vp, _c_int, _c_int]),
     "moe_merge_budget": (_c_int, [_vp, _vp, _c_int, _c_int, _f, _c_int, ctypes.c_double, _vp, _vp]),
     "moe_cluster_workspace_size": (_c_size, [_c_int, _c_int, _c_int, _c_int]),
     "moe_cluster_experts": (_c_int, [_vp, _c_int, _c_int, _c_int, _c_int, _c_int, _vp, _vp, _c_int, _c_int,
@@ -190,6 +212,78 @@ def moe_route_bwd(gate, idx, dgate, Wr, dX, accumulate=False, stream=None):
                  dtype_code(Wr.dtype), T, d, E, k, ptr(dX, Wr.dtype), int(bool(accumulate)), stream_ptr(stream))
 
 
+def _shaped(name, x, shape):
+    """x, or ValueError unless it is None or has this shape: the library takes
+    the sizes of one argument and reads the others by them."""
+    if x is not None and tuple(x.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(x.shape)}, expected {tuple(shape)}")
+    return x
+
+
+def _here(*tensors):
+    """ValueError for a tensor on another GPU than the current one, whose stream
+    the call is enqueued on."""
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != torch.cuda.current_device():
+            raise ValueError(f"tensor argument is on {t.device}, the current device is "
+                             f"cuda:{torch.cuda.current_device()}")
+
+
+def _ws(ws):
+    return (ptr(ws), ws.numel() * ws.element_size()) if ws is not None else (None, 0)
+
+
+def moe_balance_loss_workspace_size(T, E, B) -> int:
+    return lib().moe_balance_loss_workspace_size(T, E, B)
+
+
+def moe_balance_loss(logits, idx, coef, counts, dprob, loss, ws, seg=None, keep=None, stream=None):
+    """seg [B+1] int32: the sequences' first tokens and their end; keep [T] uint8, 0 = padding."""
+    T, E = logits.shape
+    k, B = idx.shape[1], 1 if seg is None else seg.shape[0] - 1
+    for n, x, shape in (("idx", idx, (T, k)), ("counts", counts, (B, E)), ("dprob", dprob, (B, E)),
+                        ("loss", loss, (1,)), ("keep", keep, (T,))):
+        _shaped(n, x, shape)
+    _here(logits, idx, counts, dprob, loss, ws, seg, keep)
+    return _call("moe_balance_loss", ptr(logits, F32), ptr(idx, I32), ptr(seg, I32), ptr(keep, U8), T, E, k, B,
+                 float(coef), ptr(counts, I32), ptr(dprob, F32), ptr(loss, F32), *_ws(ws), stream_ptr(stream))
+
+
+def moe_balance_loss_bwd(logits, dprob, dloss, dlogits, seg=None, keep=None, gate=None, idx=None, dgate=None,
+                         stream=None):
+    """gate, idx, dgate [T,k], if given, add the gates' share (all three or none)."""
+    T, E = logits.shape
+    B = 1 if seg is None else seg.shape[0] - 1
+    k = 0 if idx is None else idx.shape[1]
+    for n, x, shape in (("dprob", dprob, (B, E)), ("dloss", dloss, (1,)), ("dlogits", dlogits, (T, E)),
+                        ("keep", keep, (T,)), ("gate", gate, (T, k)), ("idx", idx, (T, k)), ("dgate", dgate, (T, k))):
+        _shaped(n, x, shape)
+    _here(logits, dprob, dloss, dlogits, seg, keep, gate, idx, dgate)
+    return _call("moe_balance_loss_bwd", ptr(logits, F32), ptr(dprob, F32), ptr(dloss, F32), ptr(seg, I32),
+                 ptr(keep, U8), ptr(gate, F32), ptr(idx, I32), ptr(dgate, F32), T, E, k, B, ptr(dlogits, F32),
+                 stream_ptr(stream))
+
+
+def moe_router_bwd_workspace_size(T, d, E) -> int:
+    return lib().moe_router_bwd_workspace_size(T, d, E)
+
+
+def moe_router_bwd(dlogits, X, Wr, ws, dX=None, dWr=None, dbias=None, accumulate_dx=False, accumulate_dw=False,
+                   stream=None):
+    """X is read for dWr, Wr for dX; either may be None where its output is."""
+    T, E = dlogits.shape
+    like = next((t for t in (X, Wr, dX, dWr) if t is not None), None)
+    d = 8 if like is None else like.shape[1]            # dbias alone has no width
+    dt = next((t.dtype for t in (X, Wr, dX) if t is not None), torch.float32)
+    for n, x, shape in (("X", X, (T, d)), ("Wr", Wr, (E, d)), ("dX", dX, (T, d)), ("dWr", dWr, (E, d)),
+                        ("dbias", dbias, (E,))):
+        _shaped(n, x, shape)
+    _here(dlogits, X, Wr, ws, dX, dWr, dbias)
+    return _call("moe_router_bwd", ptr(dlogits, F32), ptr(X, dt), ptr(Wr, dt), dtype_code(dt), T, d, E, ptr(dX, dt),
+                 int(bool(accumulate_dx)), ptr(dWr, F32), ptr(dbias, F32), int(bool(accumulate_dw)), *_ws(ws),
+                 stream_ptr(stream))
+
+
 def moe_quantize_int8(W, Wq, scale, stream=None):
     E, d = W.shape
     return _call("moe_quantize_int8", ptr(W, FLOAT), dtype_code(W.dtype), E, d, ptr(Wq, I8), ptr(scale, F32),
@@ -231,6 +325,67 @@ def moe_rms_norm(X, Y, out_norm, out_sum=None, eps=1e-6, stream=None):
     T, d = X.shape
     return _call("moe_rms_norm", ptr(X, FLOAT), ptr(Y, X.dtype), T, d, dtype_code(X.dtype), float(eps),
                  ptr(out_sum, X.dtype), ptr(out_norm, X.dtype), stream_ptr(stream))
+
+
+def moe_sublayer_norm(X, Y, S, N, alpha=1.0, gate=None, w_post=None, w_pre=None, post_norm=True, eps=1e-6,
+                      rstd_y=None, rstd_s=None, stream=None):
+    """S = alpha X + gate (norm(Y) w_post), N = norm(S) w_pre; Y None: the pre-norm
+    alone.  rstd_y, rstd_s [T] fp32, if given, are kept for the backward."""
+    T, d = X.shape
+    for n, x, shape in (("Y", Y, (T, d)), ("S", S, (T, d)), ("N", N, (T, d)), ("gate", gate, (T,)),
+                        ("w_post", w_post, (d,)), ("w_pre", w_pre, (d,)), ("rstd_y", rstd_y, (T,)),
+                        ("rstd_s", rstd_s, (T,))):
+        _shaped(n, x, shape)
+    _here(X, Y, S, N, gate, w_post, w_pre, rstd_y, rstd_s)
+    return _call("moe_sublayer_norm", ptr(X, FLOAT), ptr(Y, X.dtype), ptr(gate, F32), ptr(w_post, F32),
+                 ptr(w_pre, F32), T, d, dtype_code(X.dtype), float(alpha), int(bool(post_norm) and Y is not None),
+                 float(eps), ptr(S, X.dtype), ptr(N, X.dtype), ptr(rstd_y, F32), ptr(rstd_s, F32), stream_ptr(stream))
+
+
+def moe_sublayer_norm_bwd_workspace_size(T, d) -> int:
+    return lib().moe_sublayer_norm_bwd_workspace_size(T, d)
+
+
+def moe_sublayer_norm_bwd(dS, dN, S, Y, rstd_s, dX, dY, ws, alpha=1.0, rstd_y=None, gate=None, w_post=None,
+                          w_pre=None, post_norm=True, dgate=None, dw_post=None, dw_pre=None, accumulate_dw=False,
+                          stream=None):
+    """Backward of moe_sublayer_norm; outputs that are None are not formed."""
+    like = next(t for t in (dS, dN, S, Y) if t is not None)
+    T, d = like.shape
+    dt = like.dtype
+    for n, x, shape in (("dS", dS, (T, d)), ("dN", dN, (T, d)), ("S", S, (T, d)), ("Y", Y, (T, d)), ("dX", dX, (T, d)),
+                        ("dY", dY, (T, d)), ("gate", gate, (T,)), ("dgate", dgate, (T,)), ("rstd_y", rstd_y, (T,)),
+                        ("rstd_s", rstd_s, (T,)), ("w_post", w_post, (d,)), ("w_pre", w_pre, (d,)),
+                        ("dw_post", dw_post, (d,)), ("dw_pre", dw_pre, (d,))):
+        _shaped(n, x, shape)
+    _here(dS, dN, S, Y, rstd_s, dX, dY, ws, rstd_y, gate, w_post, w_pre, dgate, dw_post, dw_pre)
+    return _call("moe_sublayer_norm_bwd", ptr(dS, dt), ptr(dN, dt), ptr(S, dt), ptr(Y, dt), ptr(gate, F32),
+                 ptr(w_post, F32), ptr(w_pre, F32), ptr(rstd_y, F32), ptr(rstd_s, F32), T, d, dtype_code(dt),
+                 float(alpha), int(bool(post_norm) and Y is not None), ptr(dX, dt), ptr(dY, dt), ptr(dgate, F32),
+                 ptr(dw_post, F32), ptr(dw_pre, F32), int(bool(accumulate_dw)), *_ws(ws), stream_ptr(stream))
+
+
+def mxfp4_shapes(rows, cols):
+    """Shapes of the codes and of the scale bytes of a [rows, cols] matrix."""
+    return (rows, -(-cols // 32) * 16), (rows, -(-cols // 128) * 4)
+
+
+def moe_quantize_mxfp4(W, codes, scale, stream=None):
+    rows, cols = W.shape
+    for n, x, shape in zip(("codes", "scale"), (codes, scale), mxfp4_shapes(rows, cols)):
+        _shaped(n, x, shape)
+    _here(W, codes, scale)
+    return _call("moe_quantize_mxfp4", ptr(W, FLOAT), dtype_code(W.dtype), rows, cols, ptr(codes, U8), ptr(scale, U8),
+                 stream_ptr(stream))
+
+
+def moe_dequant_mxfp4(codes, scale, out, stream=None):
+    rows, cols = out.shape
+    for n, x, shape in zip(("codes", "scale"), (codes, scale), mxfp4_shapes(rows, cols)):
+        _shaped(n, x, shape)
+    _here(codes, scale, out)
+    return _call("moe_dequant_mxfp4", ptr(codes, U8), ptr(scale, U8), rows, cols, dtype_code(out.dtype),
+                 ptr(out, FLOAT), stream_ptr(stream))
 
 
 def moe_merge_plan(counts, n_merge, group, total_tokens, expert_map, slot_src, grp_ptr, grp_member,
@@ -377,6 +532,21 @@ def moe_grouped_swiglu_fwd_q8(layer, X, X_perm, offsets, T, k, H, O, ws, stream=
                  T, k, ptr(H, FLOAT), ptr(O, FLOAT), ptr(ws), ws.numel() * ws.element_size(), stream_ptr(stream))
 
 
+def moe_grouped_swiglu_fwd_mx4_workspace_size(layer, T, k) -> int:
+    return lib().moe_grouped_swiglu_fwd_mx4_workspace_size(ptr(layer), T, k)
+
+
+def moe_grouped_swiglu_fwd_mx4(layer, X, perm_token, offsets, T, k, O, ws, stream=None):
+    st = layer.struct if hasattr(layer, "struct") else layer
+    _shaped("X", X, (T, st.d))
+    _shaped("offsets", offsets, (st.S_routed + 1,))
+    _shaped("perm_token", perm_token, (T * k,))
+    _shaped("O", O, (T * (k + st.S_shared), st.d))
+    _here(X, perm_token, offsets, O, ws)
+    return _call("moe_grouped_swiglu_fwd_mx4", ptr(layer), ptr(X, torch.bfloat16), ptr(perm_token, I32),
+                 ptr(offsets, I32), T, k, ptr(O, torch.bfloat16), *_ws(ws), stream_ptr(stream))
+
+
 def moe_unpermute(layer, O, inv, perm_gate, T, k, Y, stream=None):
     return _call("moe_unpermute", ptr(layer), ptr(O, FLOAT), ptr(inv, I32), ptr(perm_gate, F32), T, k,
                  ptr(Y, FLOAT), stream_ptr(stream))
@@ -459,3 +629,25 @@ class LayerTablesQ8:
         self.keep = [q_gate, q_up, q_down, s_gate, s_up, s_down]
         self.tabs = [table(x) for x in self.keep]
         self.struct = moe_layer_q8(d, I, S_routed, S_shared, *[ptr(t) for t in self.tabs])
+
+
+class LayerTablesMX4:
+    """Device pointer tables of a layer's 4-bit experts and the moe_layer_mx4
+    struct.  q_*: per-slot code tensors (routed slots, then shared) and s_*
+    their scale bytes, as moe_quantize_mxfp4 writes them for W_gate, W_up [I,d]
+    and W_down [d,I]."""
+
+    def __init__(self, d: int, I: int, S_routed: int, S_shared: int, q_gate, q_up, q_down, s_gate, s_up, s_down,
+                 device="cuda"):
+        S = S_routed + S_shared
+
+        def table(name, x, shape):
+            if len(x) != S:
+                raise ValueError(f"{name} has {len(x)} matrices for {S} slots")
+            return torch.tensor([ptr(_shaped(name, t, shape), U8) for t in x], dtype=torch.int64, device=device)
+
+        (cg, sg), (cd, sd) = mxfp4_shapes(I, d), mxfp4_shapes(d, I)
+        self.keep = [q_gate, q_up, q_down, s_gate, s_up, s_down]
+        self.tabs = [table(*a) for a in (("q_gate", q_gate, cg), ("q_up", q_up, cg), ("q_down", q_down, cd),
+                                         ("s_gate", s_gate, sg), ("s_up", s_up, sg), ("s_down", s_down, sd))]
+        self.struct = moe_layer_mx4(d, I, S_routed, S_shared, *[ptr(t) for t in self.tabs])

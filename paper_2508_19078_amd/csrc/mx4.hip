@@ -1,0 +1,576 @@
+// Microscaled 4-bit rows (MXFP4) and the grouped SwiGLU forward on them (the
+// formulas stand in the header at moe_quantize_mxfp4 and
+// moe_grouped_swiglu_fwd_mx4).
+//
+// The products run on v_mfma_scale_f32_32x32x64_f8f6f4 with both operands e2m1:
+// a lane holds 32 consecutive k of one row (16 bytes) and the scale byte of
+// exactly that block, lane l row l % 32 and k block l / 32, so packed rows are
+// MFMA fragments as they lie in memory.
+//
+// * 16 x 64 slabs (128 k of a row) go global -> LDS with global_load_lds_dwordx4
+//   into a ring of NS slabs, the scales beside them (one dword per row and slab);
+//   one block barrier per slab, several blocks per compute unit.
+// * Weights are the first operand, so a lane's 16 sums of a 32 x 32 tile belong to
+//   one activation row; weight rows are dealt to the operand's rows so that they
+//   are 16 consecutive columns (tile_column).  Two lanes then hold a whole
+//   32-block of H: its maximum is 15 comparisons and one exchange, and H is
+//   quantised in registers.
+// * X and H in the workspace have rows of whole 128-blocks, zero behind the row's
+//   end: a slab past K meets zero codes and needs no case of its own.
+#include "debug.hpp"
+#include "gemm_bf16.hpp"
+#include "tile_sched.hpp"
+
+namespace fm {
+namespace {
+
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+
+__host__ __device__ constexpr int up32(int n) { return (n + 31) / 32 * 32; }
+__host__ __device__ constexpr int up128(int n) { return (n + 127) / 128 * 128; }
+
+// Block scale of a largest magnitude, given as the bits of its absolute value:
+// floor(log2) - 2, biased by 127; 255 for infinities and NaN.
+__device__ __forceinline__ uint32_t mx_byte(uint32_t top) {
+  const uint32_t e = top >> 23;
+  return e == 255 ? 255u : e < 2 ? 0u : e - 2;
+}
+// 2^(127 - byte), by which an element is multiplied (exactly, but for results far
+// below the smallest code).
+__device__ __forceinline__ float mx_inv(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+
+// Eight values times s as codes, the first in the lowest bits.
+__device__ __forceinline__ uint32_t mx_codes8(const float* v, float s) {
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0] * s, v[1] * s, 1.0f, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2] * s, v[3] * s, 1.0f, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4] * s, v[5] * s, 1.0f, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6] * s, v[7] * s, 1.0f, 3);
+  return c;
+}
+
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// Columns [128 blk, 128 blk + 128) of a row by 16 lanes (q: lane within them), 8
+// columns each; codes are written up to column code_cols (0 past cols).
+template <typename T>
+__device__ __forceinline__ void quantize128(const T* row, int cols, int blk, int q, int code_cols, uint8_t* codes,
+                                            uint8_t* scale) {
+  const int c = blk * 128 + q * 8;
+  float v[8];
+  if (c < cols) {
+    unpack16(ld16(row + c), v, (T*)nullptr);
+    if constexpr (sizeof(T) == 4) unpack16(ld16(row + c + 4), v + 4, (T*)nullptr);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+  }
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, abs_bits(v[i]));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+  const uint32_t byte = mx_byte(top);
+  const uint32_t code = byte == 255 ? 0u : mx_codes8(v, mx_inv(byte));
+  if (c < code_cols) *(FM_GLOBAL uint32_t*)(codes + c / 2) = code;
+  uint32_t s = byte << (8 * (q >> 2));
+  s |= (uint32_t)__shfl_xor((int)s, 4);
+  s |= (uint32_t)__shfl_xor((int)s, 8);
+  if (q == 0) *(FM_GLOBAL uint32_t*)(scale + blk * 4) = s;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_quantize_mx(const T* __restrict__ W, uint32_t items, int cols, int nb,
+                                                     uint8_t* __restrict__ codes, uint8_t* __restrict__ scale) {
+  const uint32_t item = blockIdx.x * 16 + threadIdx.x / 16;
+  if (item >= items) return;
+  const uint32_t r = item / nb;
+  quantize128(W + (size_t)r * cols, cols, (int)(item - r * nb), threadIdx.x % 16, up32(cols),
+              codes + (size_t)r * (up32(cols) / 2), scale + (size_t)r * nb * 4);
+}
+
+// The value of the low 4 bits, an e2m1 code: 0, 0.5 and then exponent and mantissa
+// shifted into an fp32.
+__device__ __forceinline__ float mx_value(uint32_t c) {
+  const uint32_t m = c & 7u;
+  const uint32_t bits = m < 2 ? m * 0x3F000000u : ((m >> 1) + 126u) << 23 | (m & 1u) << 22;
+  return __uint_as_float(bits | (c & 8u) << 28);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_dequant_mx(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scale,
+                                                    uint32_t items, int cols, int n8, T* __restrict__ out) {
+  const uint32_t item = blockIdx.x * 256 + threadIdx.x;
+  if (item >= items) return;
+  const uint32_t r = item / n8, c = (item - r * n8) * 8;
+  const uint32_t code = *(const FM_GLOBAL uint32_t*)(codes + (size_t)r * (up32(cols) / 2) + c / 2);
+  const uint32_t byte = scale[(size_t)r * (up128(cols) / 32) + c / 32];
+  // 2^(byte - 127): below 2^-126 a subnormal; 255 is NaN
+  const float s = byte == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float(byte ? byte << 23 : 0x00400000u);
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = mx_value(code >> (4 * i)) * s;
+  T* o = out + (size_t)r * cols + c;
+  st16(o, pack16(v, (T*)nullptr));
+  if constexpr (sizeof(T) == 4) st16(o + 4, pack16(v + 4, (T*)nullptr));
+}
+
+// ------------------------------------------------------- grouped products ----
+
+struct MxPtrs {
+  const uint8_t* const* qg;
+  const uint8_t* const* qu;
+  const uint8_t* const* qd;
+  const uint8_t* const* sg;
+  const uint8_t* const* su;
+  const uint8_t* const* sd;
+};
+
+// Workspace: row-tile prefix, X and H as packed rows of whole 128-blocks.
+struct MxWs {
+  int32_t* mbase;
+  uint8_t *xq, *xs, *hq, *hs;
+};
+inline size_t round256(size_t b) { return (b + 255) / 256 * 256; }
+inline MxWs mx_ws_at(void* ws, const moe_layer_mx4* L, int T, int k, size_t* bytes) {
+  const size_t S = L->S_routed + L->S_shared, R = (size_t)T * (k + L->S_shared);
+  const size_t nd = up128(L->d) / 128, nI = up128(L->I) / 128;
+  MxWs w;
+  char* p = (char*)ws;
+  auto take = [&](size_t b) {
+    char* at = p;
+    p += round256(b);
+    return at;
+  };
+  w.mbase = (int32_t*)take((S + 1) * 4);
+  w.xq = (uint8_t*)take((size_t)T * nd * 64);
+  w.xs = (uint8_t*)take((size_t)T * nd * 4);
+  w.hq = (uint8_t*)take(R * nI * 64);
+  w.hs = (uint8_t*)take(R * nI * 4);
+  *bytes = (size_t)(p - (char*)ws);
+  return w;
+}
+
+// X's tokens as packed rows; the last block builds the row-tile prefix instead.
+__global__ __launch_bounds__(256) void k_mx_prep(const bf16* __restrict__ X, RowArgs ra, int tile_rows, int nb,
+                                                 uint8_t* __restrict__ xq, uint8_t* __restrict__ xs,
+                                                 int32_t* __restrict__ mbase) {
+  if (blockIdx.x == gridDim.x - 1) {
+    __shared__ int wsum[4];
+    tile_sched(mbase, wsum, ra, tile_rows);
+    return;
+  }
+  const uint32_t item = blockIdx.x * 16 + threadIdx.x / 16;   // below 2^25: T up128(d) <= 2^32
+  if (item >= (uint32_t)ra.Tn * nb) return;
+  const uint32_t r = item / nb;
+  quantize128(X + (size_t)r * ra.d, ra.d, (int)(item - r * nb), threadIdx.x % 16, nb * 128, xq + (size_t)r * nb * 64,
+              xs + (size_t)r * nb * 4);
+}
+
+// 4 bytes per lane from base + off to LDS l + 4 * lane (see dma16s).
+__device__ __forceinline__ void dma4s(const void* base, uint32_t off, FM_LDS void* l) {
+  base = uniform_ptr(base);
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %3\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dword %1, %2\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(off), "s"(base), "s"((uint32_t)(uintptr_t)l)
+      : "memory");
+}
+
+// RA activation rows x RB weight rows by WM x WN waves, NS slabs in the ring, BPC
+// blocks per compute unit.
+template <int RA_, int RB_, int WM_, int WN_, int NS_, int BPC_> struct MxCfg {
+  static constexpr int RA = RA_, RB = RB_, WM = WM_, WN = WN_, NS = NS_, BPC = BPC_;
+  static constexpr int TM = RA / WM, TN = RB / WN, MI = TM / 32, NJ = TN / 32;
+  static constexpr int A_BYTES = RA * 64, B_BYTES = RB * 64;
+  static constexpr int SLAB = A_BYTES + B_BYTES + (RA + RB) * 4;
+  static constexpr int A_INS = RA / 64, B_INS = RB / 64;   // 16 rows each, per wave
+  static constexpr int S_ALL = (RA + RB) / 64;             // scale instructions of a slab
+  static constexpr int S_INS = (S_ALL + 3) / 4;            // per wave (some twice)
+  static constexpr int INS = A_INS + B_INS + S_INS;
+  static constexpr int LDS = NS * SLAB;
+  static_assert(WM * WN == 4 && RA % 64 == 0 && RB % 64 == 0 && TM % 32 == 0 && TN % 32 == 0, "4 waves of 32-multiples");
+  static_assert(NS >= 2 && (NS - 2) * INS < 64 && BPC * LDS <= 160 * 1024, "ring");
+};
+
+__device__ __forceinline__ int mx_column(int m) { return 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
+// Chunk swizzles of a 64-byte slab row: 16 consecutive lanes' rows at one logical
+// chunk on 16 distinct 4-bank groups; lanes read activation rows in order, weight
+// rows in the order of mx_column.
+__device__ __forceinline__ int mx_swz_a(int r) { return (r >> 2) & 3; }
+__device__ __forceinline__ int mx_swz_b(int r) { return ((r >> 2) & 1) * 2 | ((r >> 4) & 1); }
+
+// One operand pair of a tile, rows relative to it.  w2: the second of two matrices
+// whose 32-row blocks alternate (gate, up).
+struct MxTile {
+  const uint8_t *x, *xs;        // activations' codes and scales
+  const int32_t* tok;           // row -> activation row (gathered), or NULL
+  int rows, Tn;                 // activation rows of the tile's slot from the tile on
+  const uint8_t *w, *w2, *s, *s2;
+  int wrows;                    // weight rows (per matrix) from the tile on
+  int kx, kw;                   // 128-blocks of an activation row; 32-blocks of a weight row
+};
+
+template <class C, bool PAIR>
+__device__ __forceinline__ void mx_gemm(const MxTile& t, FM_LDS char* lds, f32x16_t (&acc)[C::MI][C::NJ]) {
+  const int lane = lane_id(), wave = wave_id();
+  const int nk = t.kx;
+  const uint32_t ldx = t.kx * 64, ldxs = t.kx * 4, ldw = t.kw * 16, ldws = (t.kw + 3) / 4 * 4;
+  uint32_t oa[C::A_INS], ob[C::B_INS], kb[C::B_INS], os[C::S_INS];
+  auto xrow = [&](int r) {
+    r = min(r, t.rows - 1);
+    return (uint32_t)(t.tok ? min(max(gptr(t.tok)[r], 0), t.Tn - 1) : r);
+  };
+  auto wrow = [&](int r) { return (uint32_t)min(PAIR ? 32 * (r >> 6) + (r & 31) : r, t.wrows - 1); };
+#pragma unroll
+  for (int u = 0; u < C::A_INS; ++u) {
+    const int r = 16 * (wave * C::A_INS + u) + (lane >> 2);
+    oa[u] = xrow(r) * ldx + 16 * ((lane & 3) ^ mx_swz_a(r));
+  }
+#pragma unroll
+  for (int u = 0; u < C::B_INS; ++u) {
+    const int r = 16 * (wave * C::B_INS + u) + (lane >> 2);
+    kb[u] = (lane & 3) ^ mx_swz_b(r);
+    ob[u] = wrow(r) * ldw;
+  }
+#pragma unroll
+  for (int u = 0; u < C::S_INS; ++u) {
+    const int ins = (wave + 4 * u) % C::S_ALL, r = 64 * ins + lane;
+    os[u] = r < C::RA ? xrow(r) * ldxs : wrow(r - C::RA) * ldws;
+  }
+  auto issue = [&](int slab, int buf) {
+    FM_LDS char* const l = lds + buf * C::SLAB;
+#pragma unroll
+    for (int u = 0; u < C::A_INS; ++u) dma16s(t.x + (size_t)slab * 64, oa[u], l + (wave * C::A_INS + u) * 1024);
+#pragma unroll
+    for (int u = 0; u < C::B_INS; ++u) {
+      const int ins = wave * C::B_INS + u;
+      const uint8_t* const m = PAIR && ((ins >> 1) & 1) ? t.w2 : t.w;
+      // a chunk behind the row's end meets zero activations: any valid one
+      dma16s(m, ob[u] + 16 * min(4 * slab + (int)kb[u], t.kw - 1), l + C::A_BYTES + ins * 1024);
+    }
+#pragma unroll
+    for (int u = 0; u < C::S_INS; ++u) {
+      const int ins = (wave + 4 * u) % C::S_ALL;
+      FM_LDS char* const at = l + C::A_BYTES + C::B_BYTES + ins * 256;
+      if (ins * 64 < C::RA) {
+        dma4s(t.xs + (size_t)slab * 4, os[u], at);
+      } else if (PAIR) {
+        // 64 scales: 32 rows of each matrix
+        const uintptr_t second = (uintptr_t)t.s2 - (uintptr_t)t.s;
+        const uint8_t* const p = t.s + (size_t)slab * 4 + os[u] + ((lane >> 5) ? second : 0);
+        uint32_t saved;
+        asm volatile(
+            "s_mov_b32 %0, m0\n\t"
+            "s_mov_b32 m0, %2\n\t"
+            "s_nop 0\n\t"
+            "global_load_lds_dword %1, off\n\t"
+            "s_mov_b32 m0, %0"
+            : "=&s"(saved)
+            : "v"(p), "s"((uint32_t)(uintptr_t)at)
+            : "memory");
+      } else {
+        dma4s(t.s + (size_t)slab * 4, os[u], at);
+      }
+    }
+  };
+  const int row0 = (wave % C::WM) * C::TM, col0 = (wave / C::WM) * C::TN;
+  const int m = lane & 31, h = lane >> 5;
+  uint32_t fa[C::MI], fb[C::NJ], ga[C::MI], gb[C::NJ];
+#pragma unroll
+  for (int i = 0; i < C::MI; ++i) {
+    const int r = row0 + 32 * i + m;
+    fa[i] = r * 64 + ((h ^ mx_swz_a(r)) << 4);
+    ga[i] = C::A_BYTES + C::B_BYTES + r * 4;
+  }
+#pragma unroll
+  for (int j = 0; j < C::NJ; ++j) {
+    const int r = col0 + 32 * j + mx_column(m);
+    fb[j] = C::A_BYTES + r * 64 + ((h ^ mx_swz_b(r)) << 4);
+    gb[j] = C::A_BYTES + C::B_BYTES + (C::RA + r) * 4;
+  }
+#pragma unroll
+  for (int i = 0; i < C::MI; ++i)
+#pragma unroll
+    for (int j = 0; j < C::NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+#pragma nounroll
+  for (int s = 0; s < C::NS - 1 && s < nk; ++s) issue(s, s);
+  int cur = 0, nxt = C::NS - 1;
+#pragma nounroll
+  for (int kt = 0; kt < nk; ++kt) {
+    // slab kt has landed once at most the slabs after it are in flight
+    if (nk - 1 - kt >= C::NS - 2) wait_vmcnt<(C::NS - 2) * C::INS>();
+    else wait_vmcnt<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    FM_LDS char* const l = lds + cur * C::SLAB;
+    u32x4_t xa[2][C::MI], xb[2][C::NJ];
+    int sa[C::MI], sb[C::NJ];
+#pragma unroll
+    for (int i = 0; i < C::MI; ++i) sa[i] = *(const FM_LDS int*)(l + ga[i]) >> (8 * h);
+#pragma unroll
+    for (int j = 0; j < C::NJ; ++j) sb[j] = *(const FM_LDS int*)(l + gb[j]) >> (8 * h);
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+#pragma unroll
+      for (int i = 0; i < C::MI; ++i) xa[st][i] = *(const FM_LDS u32x4_t*)(l + (fa[i] ^ (st << 5)));
+#pragma unroll
+      for (int j = 0; j < C::NJ; ++j) xb[st][j] = *(const FM_LDS u32x4_t*)(l + (fb[j] ^ (st << 5)));
+    }
+    sched_fence();
+    if (kt + C::NS - 1 < nk) issue(kt + C::NS - 1, nxt);
+    sched_fence();
+    auto wide = [](const u32x4_t& v) { return i32x8_t{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; };
+#pragma unroll
+    for (int j = 0; j < C::NJ; ++j)
+#pragma unroll
+      for (int i = 0; i < C::MI; ++i)
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(xb[0][j]), wide(xa[0][i]), acc[i][j], 4, 4, 0,
+                                                                    sb[j], 0, sa[i]);
+#pragma unroll
+    for (int j = 0; j < C::NJ; ++j)
+#pragma unroll
+      for (int i = 0; i < C::MI; ++i)
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(xb[1][j]), wide(xa[1][i]), acc[i][j], 4, 4, 2,
+                                                                    sb[j], 2, sa[i]);
+    cur = cur + 1 == C::NS ? 0 : cur + 1;
+    nxt = nxt + 1 == C::NS ? 0 : nxt + 1;
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+struct MxArgs {
+  MxPtrs W;
+  MxWs w;
+  const int32_t* perm_token;
+  RowArgs ra;
+  bf16* O;
+};
+
+// H = MX(silu(MX(X) Qg^T) (MX(X) Qu^T)), RB / 2 columns per tile.
+template <class C> __global__ __launch_bounds__(256, C::BPC) void k_mx_gate_up(MxArgs a) {
+  __shared__ __align__(16) char lds_[C::LDS];
+  FM_LDS char* const lds = (FM_LDS char*)lds_;
+  static_assert(C::NJ % 2 == 0, "gate / up pairs");
+  constexpr int CI = C::RB / 2;
+  const RowArgs& ra = a.ra;
+  const int I = ra.I, nI = up128(I) / 128, NT = nI * (128 / CI), kd = up128(ra.d) / 128;
+  const Span sp = row_span(ra.mbase, ra, NT);
+  for (int tt = sp.lo; tt < sp.hi; tt += sp.step) {
+    const RowTile r = row_tile_at(ra.mbase, ra, tt, NT, C::RA);
+    const int n0 = r.n * CI;
+    const int nw = min(n0, I - 1);   // a tile of the rows' padding reads the last row
+    const size_t lw = up32(ra.d) / 2, ls = kd * 4;
+    MxTile t;
+    t.x = a.w.xq + (r.sr.shared ? (size_t)r.m0 * kd * 64 : 0);
+    t.xs = a.w.xs + (r.sr.shared ? (size_t)r.m0 * kd * 4 : 0);
+    t.tok = r.sr.shared ? nullptr : a.perm_token + r.sr.xrow0 + r.m0;
+    t.rows = r.rows;
+    t.Tn = ra.Tn;
+    t.w = ld_scalar(a.W.qg + r.s) + nw * lw;
+    t.w2 = ld_scalar(a.W.qu + r.s) + nw * lw;
+    t.s = ld_scalar(a.W.sg + r.s) + nw * ls;
+    t.s2 = ld_scalar(a.W.su + r.s) + nw * ls;
+    t.wrows = I - nw;
+    t.kx = kd;
+    t.kw = up32(ra.d) / 32;
+    f32x16_t acc[C::MI][C::NJ];
+    mx_gemm<C, true>(t, lds, acc);
+    const int lane = lane_id_here(), wave = wave_id(), h = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < C::MI; ++i) {
+      const int row = (wave % C::WM) * C::TM + 32 * i + (lane & 31);
+#pragma unroll
+      for (int jj = 0; jj < C::NJ / 2; ++jj) {
+        const int col = n0 + (wave / C::WM) * (C::TN / 2) + 32 * jj;   // of the 32-block
+        float v[16];
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float g = acc[i][2 * jj][e];
+          v[e] = col + 16 * h + e < I ? g * sigm_fast(g) * acc[i][2 * jj + 1][e] : 0.f;
+          top = max(top, abs_bits(v[e]));
+        }
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+        const uint32_t byte = mx_byte(top);
+        const float inv = mx_inv(byte);
+        u32x2_t code = {mx_codes8(v, inv), mx_codes8(v + 8, inv)};
+        if (byte == 255) code = u32x2_t{0u, 0u};
+        if (row < r.rows) {
+          *(FM_GLOBAL u32x2_t*)(a.w.hq + (r.ob + row) * nI * 64 + col / 2 + 8 * h) = code;
+          if (h == 0) *(FM_GLOBAL uint8_t*)(a.w.hs + (r.ob + row) * nI * 4 + col / 32) = (uint8_t)byte;
+        }
+      }
+    }
+  }
+}
+
+// O = MX(H) Qd^T.
+template <class C> __global__ __launch_bounds__(256, C::BPC) void k_mx_down(MxArgs a) {
+  __shared__ __align__(16) char lds_[C::LDS];
+  FM_LDS char* const lds = (FM_LDS char*)lds_;
+  const RowArgs& ra = a.ra;
+  const int d = ra.d, nI = up128(ra.I) / 128, NT = (d + C::RB - 1) / C::RB;
+  const Span sp = row_span(ra.mbase, ra, NT);
+  for (int tt = sp.lo; tt < sp.hi; tt += sp.step) {
+    const RowTile r = row_tile_at(ra.mbase, ra, tt, NT, C::RA);
+    const int n0 = r.n * C::RB;
+    MxTile t;
+    t.x = a.w.hq + r.ob * nI * 64;
+    t.xs = a.w.hs + r.ob * nI * 4;
+    t.tok = nullptr;
+    t.rows = r.rows;
+    t.Tn = ra.Tn;
+    t.w = ld_scalar(a.W.qd + r.s) + (size_t)n0 * (up32(ra.I) / 2);
+    t.s = ld_scalar(a.W.sd + r.s) + (size_t)n0 * nI * 4;
+    t.w2 = t.s2 = nullptr;
+    t.wrows = d - n0;
+    t.kx = nI;
+    t.kw = up32(ra.I) / 32;
+    f32x16_t acc[C::MI][C::NJ];
+    mx_gemm<C, false>(t, lds, acc);
+    const int lane = lane_id_here(), wave = wave_id(), h = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < C::MI; ++i) {
+      const int row = (wave % C::WM) * C::TM + 32 * i + (lane & 31);
+#pragma unroll
+      for (int j = 0; j < C::NJ; ++j) {
+        const int col = n0 + (wave / C::WM) * C::TN + 32 * j + 16 * h;
+#pragma unroll
+        for (int e = 0; e < 16; e += 8) {
+          float v[8];
+#pragma unroll
+          for (int x = 0; x < 8; ++x) v[x] = acc[i][j][e + x];
+          if (row < r.rows && col + e < d) st16(a.O + (r.ob + row) * d + col + e, pack16(v, (bf16*)nullptr));
+        }
+      }
+    }
+  }
+}
+
+using M128 = MxCfg<128, 256, 2, 2, 3, 2>;
+
+template <class C> dim3 mx_grid(const RowArgs& ra, int NT) {
+  const long long R = (long long)ra.Tn * ra.k;
+  const long long tiles = (R / C::RA + (R < ra.S_r ? R : ra.S_r) +
+                           (long long)(ra.S - ra.S_r) * ((ra.Tn + C::RA - 1) / C::RA)) * NT;
+  const long long most = (long long)(device_cus() + N_XCD - 1) / N_XCD * N_XCD * C::BPC;
+  const long long g = (tiles + N_XCD - 1) / N_XCD * N_XCD;
+  return dim3((unsigned)(g < most ? g : most));
+}
+
+int check_rows(const void* a, const char* an, const void* b, const char* bn, const void* c, const char* cn, long rows,
+               int cols) {
+  if (rows <= 0 || cols <= 0) return fail(MOE_ERR_ARG, "rows=%ld cols=%d", rows, cols);
+  if (cols % 8) return fail(MOE_ERR_UNSUPPORTED, "cols=%d not a multiple of 8", cols);
+  FM_TRY(need(a, an)); FM_TRY(need(b, bn)); FM_TRY(need(c, cn));
+  FM_TRY(need_aligned(a, an)); FM_TRY(need_aligned(b, bn)); FM_TRY(need_aligned(c, cn));
+  return MOE_OK;
+}
+
+}  // namespace
+}  // namespace fm
+
+using namespace fm;
+
+extern "C" int moe_quantize_mxfp4(const void* W, int dtype, long rows, int cols, uint8_t* codes, uint8_t* scale,
+                                  void* stream) {
+  clear_error();
+  FM_TRY(need_dtype_float(dtype, "dtype"));
+  FM_TRY(check_rows(W, "W", codes, "codes", scale, "scale", rows, cols));
+  const int nb = up128(cols) / 128, es = esize(dtype);
+  // launches of at most 2^31 items, so that the kernel divides 32-bit numbers
+  const long step = 0x7FFFFFF0L / nb;
+  for (long r = 0; r < rows; r += step) {
+    const uint32_t items = (uint32_t)((rows - r < step ? rows - r : step) * nb);
+    const char* w = (const char*)W + (size_t)r * cols * es;
+    uint8_t* q = codes + (size_t)r * (up32(cols) / 2);
+    uint8_t* s = scale + (size_t)r * nb * 4;
+    if (dtype == MOE_BF16)
+      hipLaunchKernelGGL(k_quantize_mx<bf16>, dim3(cdiv(items, 16)), dim3(256), 0, as_stream(stream), (const bf16*)w,
+                         items, cols, nb, q, s);
+    else
+      hipLaunchKernelGGL(k_quantize_mx<float>, dim3(cdiv(items, 16)), dim3(256), 0, as_stream(stream), (const float*)w,
+                         items, cols, nb, q, s);
+  }
+  return check_launch("moe_quantize_mxfp4");
+}
+
+extern "C" int moe_dequant_mxfp4(const uint8_t* codes, const uint8_t* scale, long rows, int cols, int out_dtype,
+                                 void* out, void* stream) {
+  clear_error();
+  FM_TRY(need_dtype_float(out_dtype, "out_dtype"));
+  FM_TRY(check_rows(codes, "codes", scale, "scale", out, "out", rows, cols));
+  const int n8 = cols / 8, es = esize(out_dtype);
+  const long step = 0x7FFFFFF0L / n8;
+  for (long r = 0; r < rows; r += step) {
+    const uint32_t items = (uint32_t)((rows - r < step ? rows - r : step) * n8);
+    const uint8_t* q = codes + (size_t)r * (up32(cols) / 2);
+    const uint8_t* s = scale + (size_t)r * (up128(cols) / 32);
+    char* o = (char*)out + (size_t)r * cols * es;
+    if (out_dtype == MOE_BF16)
+      hipLaunchKernelGGL(k_dequant_mx<bf16>, dim3(cdiv(items, 256)), dim3(256), 0, as_stream(stream), q, s, items, cols,
+                         n8, (bf16*)o);
+    else
+      hipLaunchKernelGGL(k_dequant_mx<float>, dim3(cdiv(items, 256)), dim3(256), 0, as_stream(stream), q, s, items, cols,
+                         n8, (float*)o);
+  }
+  return check_launch("moe_dequant_mxfp4");
+}
+
+extern "C" size_t moe_grouped_swiglu_fwd_mx4_workspace_size(const moe_layer_mx4* L, int T, int k) {
+  if (!L || T < 0 || k <= 0 || L->d <= 0 || L->I <= 0 || L->S_routed < 0 || L->S_shared < 0) return 0;
+  size_t bytes;
+  mx_ws_at(nullptr, L, T, k, &bytes);
+  return bytes;
+}
+
+extern "C" int moe_grouped_swiglu_fwd_mx4(const moe_layer_mx4* L, const void* X, const int32_t* perm_token,
+                                          const int32_t* offsets, int T, int k, void* O, void* ws, size_t ws_bytes,
+                                          void* stream) {
+  clear_error();
+  if (!L) return fail(MOE_ERR_ARG, "layer must not be NULL");
+  if (L->d <= 0 || L->I <= 0) return fail(MOE_ERR_ARG, "layer d=%d I=%d", L->d, L->I);
+  if (L->d % 8 || L->I % 8) return fail(MOE_ERR_UNSUPPORTED, "4-bit layer d=%d I=%d must be multiples of 8", L->d, L->I);
+  if (L->S_routed < 0 || L->S_shared < 0 || L->S_routed + L->S_shared < 1 || L->S_routed > 512 || L->S_shared > 511)
+    return fail(MOE_ERR_ARG, "layer S_routed=%d S_shared=%d", L->S_routed, L->S_shared);
+  // byte offsets within a matrix, and of a token's packed row, are 32 bits wide
+  if ((long long)up128(L->d) * up128(L->I) > (1LL << 32))
+    return fail(MOE_ERR_UNSUPPORTED, "4-bit layer d=%d I=%d: more than 2^32 weights in a matrix", L->d, L->I);
+  FM_TRY(need(L->q_gate, "layer q_gate")); FM_TRY(need(L->q_up, "layer q_up")); FM_TRY(need(L->q_down, "layer q_down"));
+  FM_TRY(need(L->s_gate, "layer s_gate")); FM_TRY(need(L->s_up, "layer s_up")); FM_TRY(need(L->s_down, "layer s_down"));
+  if (T < 0 || k <= 0 || k > 16) return fail(MOE_ERR_ARG, "T=%d k=%d", T, k);
+  if ((long long)T * up128(L->d) > (1LL << 32))
+    return fail(MOE_ERR_UNSUPPORTED, "T=%d tokens of d=%d: more than 2^32 values", T, L->d);
+  if (T == 0) return MOE_OK;
+  FM_TRY(need(X, "X")); FM_TRY(need(offsets, "offsets")); FM_TRY(need(O, "O")); FM_TRY(need(ws, "ws"));
+  if (L->S_routed > 0) FM_TRY(need(perm_token, "perm_token"));
+  FM_TRY(need_aligned(X, "X")); FM_TRY(need_aligned(perm_token, "perm_token")); FM_TRY(need_aligned(offsets, "offsets"));
+  FM_TRY(need_aligned(O, "O")); FM_TRY(need_aligned(ws, "ws"));
+  size_t bytes;
+  const MxWs w = mx_ws_at(ws, L, T, k, &bytes);
+  if (ws_bytes < bytes) return fail(MOE_ERR_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, bytes);
+  hipStream_t st = as_stream(stream);
+  if (debug_checks() && L->S_routed > 0) {
+    int rows = 0;
+    FM_TRY(debug_check_offsets(offsets, L->S_routed, T, k, st));
+    FM_TRY(debug_rows(offsets, L->S_routed, st, &rows));
+    FM_TRY(debug_check_tokens(perm_token, rows, T, st));
+  }
+  const RowArgs ra{offsets, w.mbase, L->S_routed, L->S_routed + L->S_shared, T, k, L->d, L->I, L->I};
+  const MxArgs a{{L->q_gate, L->q_up, L->q_down, L->s_gate, L->s_up, L->s_down}, w, perm_token, ra, (bf16*)O};
+  typedef M128 C;
+  const int nb = up128(L->d) / 128;
+  hipLaunchKernelGGL(k_mx_prep, dim3(cdiv((long)T * nb, 16) + 1), dim3(256), 0, st, (const bf16*)X, ra, C::RA, nb, w.xq,
+                     w.xs, w.mbase);
+  hipLaunchKernelGGL(k_mx_gate_up<C>, mx_grid<C>(ra, up128(L->I) / 128 * (256 / C::RB)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(k_mx_down<C>, mx_grid<C>(ra, cdiv(L->d, C::RB)), dim3(256), 0, st, a);
+  return check_launch("moe_grouped_swiglu_fwd_mx4");
+}

@@ -3,8 +3,9 @@ stack of MoE layers (Section 4.1: a low-bit copy of the model is run over the
 participant's data to learn which experts each layer activates).
 
 ``QuantizedStack`` quantises every layer's router and expert matrices to int8
-with one scale per row (``moe_quantize_int8``) and keeps only the codes and
-scales resident.  ``run`` then passes a batch through the stack, layer by
+with one scale per row (``moe_quantize_int8``), or the experts to microscaled
+4-bit rows (``experts="mxfp4"``, ``moe_quantize_mxfp4``), and keeps only the
+codes and scales resident.  ``run`` then passes a batch through the stack, layer by
 layer, on one stream:
 
   moe_rms_norm        the layer's input: the RMS-normalised stream (fused with
@@ -12,9 +13,11 @@ layer, on one stream:
   moe_profile_route   int8 routing: histogram, top-k indices and gates
   moe_permute         the layer's rows into per-expert buckets
   moe_grouped_swiglu_fwd_q8   the experts straight from their int8 codes
-                      (bf16 activations, d and I multiples of 16); otherwise
-                      moe_dequant_int8 into one reused buffer and
-                      moe_grouped_swiglu_fwd
+                      (bf16 activations, d and I multiples of 16), or
+                      moe_grouped_swiglu_fwd_mx4 from their 4-bit codes
+                      (bf16 activations, quantised on the way); otherwise
+                      moe_dequant_int8 or moe_dequant_mxfp4 into one reused
+                      buffer and moe_grouped_swiglu_fwd
   moe_unpermute       Y_l, then X_{l+1} = X_l + Y_l (moe_rms_norm, which also
                       normalises X_{l+1} for the next layer; moe_residual_add
                       after the last layer)
@@ -34,10 +37,13 @@ from . import api
 class QuantizedStack:
     """layers[l] = dict(Wr [E,d], bias [E] fp32 or None, wg [E,I,d], wu [E,I,d],
     wd [E,d,I], and optionally sg/su/sd for shared experts), device tensors in
-    one float dtype.  Only the int8 codes and fp32 scales are kept."""
+    one float dtype.  Only codes and scales are kept; experts: "int8" or "mxfp4"
+    (the routers are int8 in both)."""
 
     def __init__(self, layers: Sequence[dict], T: int, k: int, device: str = "cuda",
-                 record: bool = False, fused: Optional[bool] = None, eps: float = 1e-6):
+                 record: bool = False, fused: Optional[bool] = None, eps: float = 1e-6, experts: str = "int8"):
+        if experts not in ("int8", "mxfp4"):
+            raise ValueError(f'experts={experts!r}: expected "int8" or "mxfp4"')
         L0 = layers[0]
         self.dt = L0["wg"].dtype
         self.E, self.I, self.d = L0["wg"].shape
@@ -55,18 +61,28 @@ class QuantizedStack:
             api.moe_quantize_int8(W.reshape(-1, cols), q.view(-1, cols), s)
             return q, s
 
+        def quant_mx4(W):
+            W2 = W.reshape(-1, W.shape[-1])
+            cs, ss = api.mxfp4_shapes(*W2.shape)
+            q = torch.empty(cs, dtype=torch.uint8, device=dev)
+            s = torch.empty(ss, dtype=torch.uint8, device=dev)
+            api.moe_quantize_mxfp4(W2, q, s)
+            return q, s
+
+        self.experts = experts
+        mx4 = experts == "mxfp4"
         self.q = []
         for lay in layers:
             ql = {"Wr": quant(lay["Wr"]), "bias": lay.get("bias")}
             for name in ("wg", "wu", "wd", "sg", "su", "sd"):
                 if lay.get(name) is not None:
-                    ql[name] = quant(lay[name])
+                    ql[name] = (quant_mx4 if mx4 else quant)(lay[name])
             self.q.append(ql)
 
-        can_fuse = self.dt == torch.bfloat16 and d % 16 == 0 and I % 16 == 0
+        can_fuse = self.dt == torch.bfloat16 and (mx4 or (d % 16 == 0 and I % 16 == 0))
         self.fused = can_fuse if fused is None else bool(fused)
         if self.fused and not can_fuse:
-            raise ValueError("the int8 forward needs bf16 activations and d, I multiples of 16")
+            raise ValueError("the forward from the codes needs bf16 activations, and for int8 d, I multiples of 16")
         z = lambda *shape, dtype=self.dt: torch.empty(*shape, dtype=dtype, device=dev)
 
         def per_slot(ql, name, sname, rows):
@@ -76,20 +92,22 @@ class QuantizedStack:
                 if n == 0:
                     continue
                 q, sc = ql[nm]
-                out_q += [q[e] for e in range(n)]
+                out_q += [q[e * rows:(e + 1) * rows] if mx4 else q[e] for e in range(n)]
                 out_s += [sc[e * rows:(e + 1) * rows] for e in range(n)]
             return out_q, out_s
         if self.fused:
-            # per-layer tables of the int8 codes and their row scales
+            # per-layer tables of the codes and their scales
             self.qtables = []
             for ql in self.q:
                 gq, gs = per_slot(ql, "wg", "sg", I)
                 uq, us = per_slot(ql, "wu", "su", I)
                 dq, ds = per_slot(ql, "wd", "sd", d)
-                self.qtables.append(api.LayerTablesQ8(d, I, E, n_sh, gq, uq, dq, gs, us, ds, device=dev))
+                tables = api.LayerTablesMX4 if mx4 else api.LayerTablesQ8
+                self.qtables.append(tables(d, I, E, n_sh, gq, uq, dq, gs, us, ds, device=dev))
             # the combine reads only the layer's shape
             self.layer = api.moe_layer(d, I, api.dtype_code(self.dt), E, n_sh, None, None, None, None, None, None)
-            ws_fwd = api.moe_grouped_swiglu_fwd_q8_workspace_size(self.qtables[0], T, k)
+            size = api.moe_grouped_swiglu_fwd_mx4_workspace_size if mx4 else api.moe_grouped_swiglu_fwd_q8_workspace_size
+            ws_fwd = size(self.qtables[0], T, k)
         else:
             # one layer's dequantised experts, reused by every layer
             self.Dg, self.Du, self.Dd = z(E, I, d), z(E, I, d), z(E, d, I)
@@ -113,11 +131,19 @@ class QuantizedStack:
         self.ws_perm = torch.empty(api.moe_permute_workspace_size(T, k, E), dtype=torch.uint8, device=dev)
         if not self.fused:
             self.A_g, self.A_u = z(Rt, I), z(Rt, I)
-        self.H, self.O = z(Rt, I), z(Rt, d)
+        if not (self.fused and mx4):   # the 4-bit forward keeps H in its workspace
+            self.H = z(Rt, I)
+        self.O = z(Rt, d)
         self.Y = z(T, d)
         self.Xa, self.Xb, self.Xn = z(T, d), z(T, d), z(T, d)
         self.ws_fwd = torch.empty(ws_fwd, dtype=torch.uint8, device=dev)
         self.trace: List[dict] = []
+
+    def _dequant(self, q, out):
+        if self.experts == "mxfp4":
+            api.moe_dequant_mxfp4(q[0], q[1], out.view(-1, out.shape[-1]))
+        else:
+            api.moe_dequant_int8(q[0], q[1], out)
 
     def run(self, X0: torch.Tensor, mark=None) -> torch.Tensor:
         """The stack on the batch X0 [T,d]; per-layer histograms land in
@@ -133,13 +159,13 @@ class QuantizedStack:
         mark("norm")
         for l, ql in enumerate(self.q):
             if not self.fused:
-                api.moe_dequant_int8(ql["wg"][0], ql["wg"][1], self.Dg)
-                api.moe_dequant_int8(ql["wu"][0], ql["wu"][1], self.Du)
-                api.moe_dequant_int8(ql["wd"][0], ql["wd"][1], self.Dd)
+                self._dequant(ql["wg"], self.Dg)
+                self._dequant(ql["wu"], self.Du)
+                self._dequant(ql["wd"], self.Dd)
                 if self.n_sh:
-                    api.moe_dequant_int8(ql["sg"][0], ql["sg"][1], self.Sg)
-                    api.moe_dequant_int8(ql["su"][0], ql["su"][1], self.Su)
-                    api.moe_dequant_int8(ql["sd"][0], ql["sd"][1], self.Sd)
+                    self._dequant(ql["sg"], self.Sg)
+                    self._dequant(ql["su"], self.Su)
+                    self._dequant(ql["sd"], self.Sd)
                 mark("dequant")
             Wq, ws = ql["Wr"]
             api.moe_profile_route(Xn, Wq, ws, ql["bias"], k, self.counts[l], self.idx, self.gate)
@@ -147,7 +173,10 @@ class QuantizedStack:
             api.moe_permute(Xn, self.idx, self.gate, None, self.E, self.offsets, self.perm_token, self.perm_gate,
                             self.inv, self.X_perm, self.ws_perm, E=self.E)
             mark("permute")
-            if self.fused:
+            if self.fused and self.experts == "mxfp4":
+                api.moe_grouped_swiglu_fwd_mx4(self.qtables[l], Xn, self.perm_token, self.offsets, T, k, self.O,
+                                               self.ws_fwd)
+            elif self.fused:
                 api.moe_grouped_swiglu_fwd_q8(self.qtables[l], Xn, self.X_perm, self.offsets, T, k, self.H, self.O,
                                               self.ws_fwd)
             else:
