@@ -18,8 +18,8 @@
 // * X and H in the workspace have rows of whole 128-blocks, zero behind the row's
 //   end: a slab past K meets zero codes and needs no case of its own.
 #include "debug.hpp"
+#include "ffn_common.hpp"
 #include "gemm_bf16.hpp"
-#include "tile_sched.hpp"
 
 namespace fm {
 namespace {
@@ -151,13 +151,80 @@ inline MxWs mx_ws_at(void* ws, const moe_layer_mx4* L, int T, int k, size_t* byt
   return w;
 }
 
+// Row tiles before each slot, tiles[s] for s in [0, S]: one block of 256 threads,
+// thread i the slots 4 i to 4 i + 3 (S <= 1023).
+__device__ __forceinline__ void mx_count_tiles(const RowArgs& ra, int tile_rows, int32_t* tiles) {
+  __shared__ int wave_sum[4];
+  const int s0 = threadIdx.x * 4, lane = lane_id(), wave = threadIdx.x >> 6;
+  int n[4], own = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int s = s0 + i;
+    const int rows = s < ra.S_r ? ra.offsets[s + 1] - ra.offsets[s] : s < ra.S ? ra.Tn : 0;
+    n[i] = (rows + tile_rows - 1) / tile_rows;
+    own += n[i];
+  }
+  int before = own;   // inclusive over the wave's lanes
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(before, o);
+    if (lane >= o) before += v;
+  }
+  if (lane == 63) wave_sum[wave] = before;
+  __syncthreads();
+  before -= own;
+  for (int w = 0; w < wave; ++w) before += wave_sum[w];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (s0 + i <= ra.S) tiles[s0 + i] = before;
+    before += n[i];
+  }
+}
+
+// A block's tiles of a grouped product with NT column tiles: XCD x (blocks go to
+// the XCDs in turn) walks its eighth of them, slot by slot, so that the row tiles
+// of a slot, which share its weights, meet in one L2.
+struct MxWalk {
+  int at, end, step;
+};
+__device__ __forceinline__ MxWalk mx_walk(const RowArgs& ra, int NT) {
+  const long long all = (long long)ld_scalar(ra.mbase + ra.S) * NT;
+  const int x = blockIdx.x % N_XCD;
+  return MxWalk{(int)(all * x / N_XCD) + (int)(blockIdx.x / N_XCD), (int)(all * (x + 1) / N_XCD),
+                (int)(gridDim.x / N_XCD)};
+}
+
+struct MxRows {
+  SlotRows sr;
+  int s, m0, n;   // slot, first row in it, column tile
+  int rows;       // rows of the slot from m0 on
+  size_t ob;      // m0's row in the per-row buffers
+};
+__device__ __forceinline__ MxRows mx_rows(const RowArgs& ra, int t, int NT, int tile_rows) {
+  const int m = t / NT;
+  int s = 0;   // the slots that end at or before row tile m
+  for (int b = 0; b < ra.S; b += 64) {
+    const int i = b + lane_id();
+    s += __builtin_popcountll(__ballot(i < ra.S && gptr(ra.mbase)[min(i, ra.S - 1) + 1] <= m));
+  }
+  MxRows r;
+  r.s = __builtin_amdgcn_readfirstlane(s);
+  const int first = ld_scalar(ra.mbase + r.s), count = ld_scalar(ra.mbase + r.s + 1) - first;
+  int mt;
+  band_order(t - first * NT, count, NT, 8, mt, r.n);
+  r.sr = slot_rows(r.s, ra.offsets, ra.S_r, ra.Tn, ra.k);
+  r.m0 = mt * tile_rows;
+  r.rows = r.sr.nrows - r.m0;
+  r.ob = (size_t)(r.sr.orow0 + r.m0);
+  return r;
+}
+
 // X's tokens as packed rows; the last block builds the row-tile prefix instead.
 __global__ __launch_bounds__(256) void k_mx_prep(const bf16* __restrict__ X, RowArgs ra, int tile_rows, int nb,
                                                  uint8_t* __restrict__ xq, uint8_t* __restrict__ xs,
                                                  int32_t* __restrict__ mbase) {
   if (blockIdx.x == gridDim.x - 1) {
-    __shared__ int wsum[4];
-    tile_sched(mbase, wsum, ra, tile_rows);
+    mx_count_tiles(ra, tile_rows, mbase);
     return;
   }
   const uint32_t item = blockIdx.x * 16 + threadIdx.x / 16;   // below 2^25: T up128(d) <= 2^32
@@ -362,9 +429,9 @@ template <class C> __global__ __launch_bounds__(256, C::BPC) void k_mx_gate_up(M
   constexpr int CI = C::RB / 2;
   const RowArgs& ra = a.ra;
   const int I = ra.I, nI = up128(I) / 128, NT = nI * (128 / CI), kd = up128(ra.d) / 128;
-  const Span sp = row_span(ra.mbase, ra, NT);
-  for (int tt = sp.lo; tt < sp.hi; tt += sp.step) {
-    const RowTile r = row_tile_at(ra.mbase, ra, tt, NT, C::RA);
+  const MxWalk walk = mx_walk(ra, NT);
+  for (int tt = walk.at; tt < walk.end; tt += walk.step) {
+    const MxRows r = mx_rows(ra, tt, NT, C::RA);
     const int n0 = r.n * CI;
     const int nw = min(n0, I - 1);   // a tile of the rows' padding reads the last row
     const size_t lw = up32(ra.d) / 2, ls = kd * 4;
@@ -418,9 +485,9 @@ template <class C> __global__ __launch_bounds__(256, C::BPC) void k_mx_down(MxAr
   FM_LDS char* const lds = (FM_LDS char*)lds_;
   const RowArgs& ra = a.ra;
   const int d = ra.d, nI = up128(ra.I) / 128, NT = (d + C::RB - 1) / C::RB;
-  const Span sp = row_span(ra.mbase, ra, NT);
-  for (int tt = sp.lo; tt < sp.hi; tt += sp.step) {
-    const RowTile r = row_tile_at(ra.mbase, ra, tt, NT, C::RA);
+  const MxWalk walk = mx_walk(ra, NT);
+  for (int tt = walk.at; tt < walk.end; tt += walk.step) {
+    const MxRows r = mx_rows(ra, tt, NT, C::RA);
     const int n0 = r.n * C::RB;
     MxTile t;
     t.x = a.w.hq + r.ob * nI * 64;
