@@ -215,22 +215,33 @@ def moe_route_bwd(gate, idx, dgate, Wr, dX, accumulate=False, stream=None):
 def _shaped(name, x, shape):
     """x, or ValueError unless it is None or has this shape: the library takes
     the sizes of one argument and reads the others by them."""
-    if x is not None and tuple(x.shape) != tuple(shape):
+    if x is not None and x.shape != shape:
         raise ValueError(f"{name} has shape {tuple(x.shape)}, expected {tuple(shape)}")
     return x
 
 
-def _here(*tensors):
-    """ValueError for a tensor on another GPU than the current one, whose stream
-    the call is enqueued on."""
-    for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != torch.cuda.current_device():
-            raise ValueError(f"tensor argument is on {t.device}, the current device is "
-                             f"cuda:{torch.cuda.current_device()}")
+def _device() -> int:
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -1
 
 
-def _ws(ws):
-    return (ptr(ws), ws.numel() * ws.element_size()) if ws is not None else (None, 0)
+def _arg(dev, name, x, dt, shape):
+    """Device address of a tensor argument of this dtype and shape (None passes),
+    on the current GPU `dev`, whose stream the call is enqueued on."""
+    if x is None:
+        return None
+    if x.shape == shape and x.is_cuda and x.is_contiguous() and x.dtype is dt and x.get_device() == dev:
+        return x.data_ptr()
+    _shaped(name, x, shape)
+    ptr(x, dt)
+    raise ValueError(f"{name} is on {x.device}, the current device is cuda:{dev}")
+
+
+def _ws(dev, ws):
+    if ws is None:
+        return None, 0
+    if ws.is_cuda and ws.get_device() != dev:
+        raise ValueError(f"ws is on {ws.device}, the current device is cuda:{dev}")
+    return ptr(ws), ws.numel() * ws.element_size()
 
 
 def moe_balance_loss_workspace_size(T, E, B) -> int:
@@ -240,27 +251,22 @@ def moe_balance_loss_workspace_size(T, E, B) -> int:
 def moe_balance_loss(logits, idx, coef, counts, dprob, loss, ws, seg=None, keep=None, stream=None):
     """seg [B+1] int32: the sequences' first tokens and their end; keep [T] uint8, 0 = padding."""
     T, E = logits.shape
-    k, B = idx.shape[1], 1 if seg is None else seg.shape[0] - 1
-    for n, x, shape in (("idx", idx, (T, k)), ("counts", counts, (B, E)), ("dprob", dprob, (B, E)),
-                        ("loss", loss, (1,)), ("keep", keep, (T,))):
-        _shaped(n, x, shape)
-    _here(logits, idx, counts, dprob, loss, ws, seg, keep)
-    return _call("moe_balance_loss", ptr(logits, F32), ptr(idx, I32), ptr(seg, I32), ptr(keep, U8), T, E, k, B,
-                 float(coef), ptr(counts, I32), ptr(dprob, F32), ptr(loss, F32), *_ws(ws), stream_ptr(stream))
+    k, B, v = idx.shape[1], 1 if seg is None else seg.shape[0] - 1, _device()
+    return _call("moe_balance_loss", _arg(v, "logits", logits, F32, (T, E)), _arg(v, "idx", idx, I32, (T, k)),
+                 _arg(v, "seg", seg, I32, (B + 1,)), _arg(v, "keep", keep, U8, (T,)), T, E, k, B, float(coef),
+                 _arg(v, "counts", counts, I32, (B, E)), _arg(v, "dprob", dprob, F32, (B, E)),
+                 _arg(v, "loss", loss, F32, (1,)), *_ws(v, ws), stream_ptr(stream))
 
 
 def moe_balance_loss_bwd(logits, dprob, dloss, dlogits, seg=None, keep=None, gate=None, idx=None, dgate=None,
                          stream=None):
     """gate, idx, dgate [T,k], if given, add the gates' share (all three or none)."""
     T, E = logits.shape
-    B = 1 if seg is None else seg.shape[0] - 1
-    k = 0 if idx is None else idx.shape[1]
-    for n, x, shape in (("dprob", dprob, (B, E)), ("dloss", dloss, (1,)), ("dlogits", dlogits, (T, E)),
-                        ("keep", keep, (T,)), ("gate", gate, (T, k)), ("idx", idx, (T, k)), ("dgate", dgate, (T, k))):
-        _shaped(n, x, shape)
-    _here(logits, dprob, dloss, dlogits, seg, keep, gate, idx, dgate)
-    return _call("moe_balance_loss_bwd", ptr(logits, F32), ptr(dprob, F32), ptr(dloss, F32), ptr(seg, I32),
-                 ptr(keep, U8), ptr(gate, F32), ptr(idx, I32), ptr(dgate, F32), T, E, k, B, ptr(dlogits, F32),
+    B, k, v = 1 if seg is None else seg.shape[0] - 1, 0 if idx is None else idx.shape[1], _device()
+    return _call("moe_balance_loss_bwd", _arg(v, "logits", logits, F32, (T, E)), _arg(v, "dprob", dprob, F32, (B, E)),
+                 _arg(v, "dloss", dloss, F32, (1,)), _arg(v, "seg", seg, I32, (B + 1,)),
+                 _arg(v, "keep", keep, U8, (T,)), _arg(v, "gate", gate, F32, (T, k)), _arg(v, "idx", idx, I32, (T, k)),
+                 _arg(v, "dgate", dgate, F32, (T, k)), T, E, k, B, _arg(v, "dlogits", dlogits, F32, (T, E)),
                  stream_ptr(stream))
 
 
@@ -275,13 +281,11 @@ def moe_router_bwd(dlogits, X, Wr, ws, dX=None, dWr=None, dbias=None, accumulate
     like = next((t for t in (X, Wr, dX, dWr) if t is not None), None)
     d = 8 if like is None else like.shape[1]            # dbias alone has no width
     dt = next((t.dtype for t in (X, Wr, dX) if t is not None), torch.float32)
-    for n, x, shape in (("X", X, (T, d)), ("Wr", Wr, (E, d)), ("dX", dX, (T, d)), ("dWr", dWr, (E, d)),
-                        ("dbias", dbias, (E,))):
-        _shaped(n, x, shape)
-    _here(dlogits, X, Wr, ws, dX, dWr, dbias)
-    return _call("moe_router_bwd", ptr(dlogits, F32), ptr(X, dt), ptr(Wr, dt), dtype_code(dt), T, d, E, ptr(dX, dt),
-                 int(bool(accumulate_dx)), ptr(dWr, F32), ptr(dbias, F32), int(bool(accumulate_dw)), *_ws(ws),
-                 stream_ptr(stream))
+    code, v = dtype_code(dt), _device()
+    return _call("moe_router_bwd", _arg(v, "dlogits", dlogits, F32, (T, E)), _arg(v, "X", X, dt, (T, d)),
+                 _arg(v, "Wr", Wr, dt, (E, d)), code, T, d, E, _arg(v, "dX", dX, dt, (T, d)), int(bool(accumulate_dx)),
+                 _arg(v, "dWr", dWr, F32, (E, d)), _arg(v, "dbias", dbias, F32, (E,)), int(bool(accumulate_dw)),
+                 *_ws(v, ws), stream_ptr(stream))
 
 
 def moe_quantize_int8(W, Wq, scale, stream=None):
@@ -331,15 +335,13 @@ def moe_sublayer_norm(X, Y, S, N, alpha=1.0, gate=None, w_post=None, w_pre=None,
                       rstd_y=None, rstd_s=None, stream=None):
     """S = alpha X + gate (norm(Y) w_post), N = norm(S) w_pre; Y None: the pre-norm
     alone.  rstd_y, rstd_s [T] fp32, if given, are kept for the backward."""
-    T, d = X.shape
-    for n, x, shape in (("Y", Y, (T, d)), ("S", S, (T, d)), ("N", N, (T, d)), ("gate", gate, (T,)),
-                        ("w_post", w_post, (d,)), ("w_pre", w_pre, (d,)), ("rstd_y", rstd_y, (T,)),
-                        ("rstd_s", rstd_s, (T,))):
-        _shaped(n, x, shape)
-    _here(X, Y, S, N, gate, w_post, w_pre, rstd_y, rstd_s)
-    return _call("moe_sublayer_norm", ptr(X, FLOAT), ptr(Y, X.dtype), ptr(gate, F32), ptr(w_post, F32),
-                 ptr(w_pre, F32), T, d, dtype_code(X.dtype), float(alpha), int(bool(post_norm) and Y is not None),
-                 float(eps), ptr(S, X.dtype), ptr(N, X.dtype), ptr(rstd_y, F32), ptr(rstd_s, F32), stream_ptr(stream))
+    T, d = td = X.shape
+    dt, v = X.dtype, _device()
+    code = dtype_code(dt)
+    return _call("moe_sublayer_norm", _arg(v, "X", X, dt, td), _arg(v, "Y", Y, dt, td), _arg(v, "gate", gate, F32, (T,)),
+                 _arg(v, "w_post", w_post, F32, (d,)), _arg(v, "w_pre", w_pre, F32, (d,)), T, d, code, float(alpha),
+                 int(bool(post_norm) and Y is not None), float(eps), _arg(v, "S", S, dt, td), _arg(v, "N", N, dt, td),
+                 _arg(v, "rstd_y", rstd_y, F32, (T,)), _arg(v, "rstd_s", rstd_s, F32, (T,)), stream_ptr(stream))
 
 
 def moe_sublayer_norm_bwd_workspace_size(T, d) -> int:
@@ -351,18 +353,16 @@ def moe_sublayer_norm_bwd(dS, dN, S, Y, rstd_s, dX, dY, ws, alpha=1.0, rstd_y=No
                           stream=None):
     """Backward of moe_sublayer_norm; outputs that are None are not formed."""
     like = next(t for t in (dS, dN, S, Y) if t is not None)
-    T, d = like.shape
-    dt = like.dtype
-    for n, x, shape in (("dS", dS, (T, d)), ("dN", dN, (T, d)), ("S", S, (T, d)), ("Y", Y, (T, d)), ("dX", dX, (T, d)),
-                        ("dY", dY, (T, d)), ("gate", gate, (T,)), ("dgate", dgate, (T,)), ("rstd_y", rstd_y, (T,)),
-                        ("rstd_s", rstd_s, (T,)), ("w_post", w_post, (d,)), ("w_pre", w_pre, (d,)),
-                        ("dw_post", dw_post, (d,)), ("dw_pre", dw_pre, (d,))):
-        _shaped(n, x, shape)
-    _here(dS, dN, S, Y, rstd_s, dX, dY, ws, rstd_y, gate, w_post, w_pre, dgate, dw_post, dw_pre)
-    return _call("moe_sublayer_norm_bwd", ptr(dS, dt), ptr(dN, dt), ptr(S, dt), ptr(Y, dt), ptr(gate, F32),
-                 ptr(w_post, F32), ptr(w_pre, F32), ptr(rstd_y, F32), ptr(rstd_s, F32), T, d, dtype_code(dt),
-                 float(alpha), int(bool(post_norm) and Y is not None), ptr(dX, dt), ptr(dY, dt), ptr(dgate, F32),
-                 ptr(dw_post, F32), ptr(dw_pre, F32), int(bool(accumulate_dw)), *_ws(ws), stream_ptr(stream))
+    T, d = td = like.shape
+    dt, v = like.dtype, _device()
+    code = dtype_code(dt)
+    return _call("moe_sublayer_norm_bwd", _arg(v, "dS", dS, dt, td), _arg(v, "dN", dN, dt, td), _arg(v, "S", S, dt, td),
+                 _arg(v, "Y", Y, dt, td), _arg(v, "gate", gate, F32, (T,)), _arg(v, "w_post", w_post, F32, (d,)),
+                 _arg(v, "w_pre", w_pre, F32, (d,)), _arg(v, "rstd_y", rstd_y, F32, (T,)),
+                 _arg(v, "rstd_s", rstd_s, F32, (T,)), T, d, code, float(alpha),
+                 int(bool(post_norm) and Y is not None), _arg(v, "dX", dX, dt, td), _arg(v, "dY", dY, dt, td),
+                 _arg(v, "dgate", dgate, F32, (T,)), _arg(v, "dw_post", dw_post, F32, (d,)),
+                 _arg(v, "dw_pre", dw_pre, F32, (d,)), int(bool(accumulate_dw)), *_ws(v, ws), stream_ptr(stream))
 
 
 def mxfp4_shapes(rows, cols):
@@ -372,20 +372,18 @@ def mxfp4_shapes(rows, cols):
 
 def moe_quantize_mxfp4(W, codes, scale, stream=None):
     rows, cols = W.shape
-    for n, x, shape in zip(("codes", "scale"), (codes, scale), mxfp4_shapes(rows, cols)):
-        _shaped(n, x, shape)
-    _here(W, codes, scale)
-    return _call("moe_quantize_mxfp4", ptr(W, FLOAT), dtype_code(W.dtype), rows, cols, ptr(codes, U8), ptr(scale, U8),
-                 stream_ptr(stream))
+    cs, ss = mxfp4_shapes(rows, cols)
+    v, code = _device(), dtype_code(W.dtype)
+    return _call("moe_quantize_mxfp4", _arg(v, "W", W, W.dtype, (rows, cols)), code, rows, cols,
+                 _arg(v, "codes", codes, U8, cs), _arg(v, "scale", scale, U8, ss), stream_ptr(stream))
 
 
 def moe_dequant_mxfp4(codes, scale, out, stream=None):
     rows, cols = out.shape
-    for n, x, shape in zip(("codes", "scale"), (codes, scale), mxfp4_shapes(rows, cols)):
-        _shaped(n, x, shape)
-    _here(codes, scale, out)
-    return _call("moe_dequant_mxfp4", ptr(codes, U8), ptr(scale, U8), rows, cols, dtype_code(out.dtype),
-                 ptr(out, FLOAT), stream_ptr(stream))
+    cs, ss = mxfp4_shapes(rows, cols)
+    v, code = _device(), dtype_code(out.dtype)
+    return _call("moe_dequant_mxfp4", _arg(v, "codes", codes, U8, cs), _arg(v, "scale", scale, U8, ss), rows, cols, code,
+                 _arg(v, "out", out, out.dtype, (rows, cols)), stream_ptr(stream))
 
 
 def moe_merge_plan(counts, n_merge, group, total_tokens, expert_map, slot_src, grp_ptr, grp_member,
@@ -537,14 +535,10 @@ def moe_grouped_swiglu_fwd_mx4_workspace_size(layer, T, k) -> int:
 
 
 def moe_grouped_swiglu_fwd_mx4(layer, X, perm_token, offsets, T, k, O, ws, stream=None):
-    st = layer.struct if hasattr(layer, "struct") else layer
-    _shaped("X", X, (T, st.d))
-    _shaped("offsets", offsets, (st.S_routed + 1,))
-    _shaped("perm_token", perm_token, (T * k,))
-    _shaped("O", O, (T * (k + st.S_shared), st.d))
-    _here(X, perm_token, offsets, O, ws)
-    return _call("moe_grouped_swiglu_fwd_mx4", ptr(layer), ptr(X, torch.bfloat16), ptr(perm_token, I32),
-                 ptr(offsets, I32), T, k, ptr(O, torch.bfloat16), *_ws(ws), stream_ptr(stream))
+    st, v, bf = layer.struct if hasattr(layer, "struct") else layer, _device(), torch.bfloat16
+    return _call("moe_grouped_swiglu_fwd_mx4", ptr(layer), _arg(v, "X", X, bf, (T, st.d)),
+                 _arg(v, "perm_token", perm_token, I32, (T * k,)), _arg(v, "offsets", offsets, I32, (st.S_routed + 1,)),
+                 T, k, _arg(v, "O", O, bf, (T * (k + st.S_shared), st.d)), *_ws(v, ws), stream_ptr(stream))
 
 
 def moe_unpermute(layer, O, inv, perm_gate, T, k, Y, stream=None):

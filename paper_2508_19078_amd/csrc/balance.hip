@@ -12,48 +12,63 @@
 // number of tokens at slot block + sequence: going through a block's sequences
 // and on to the next block's, either index grows, so no two pairs share a slot.
 // A block per sequence then adds its slots in a fixed order.  No float atomics.
+#include <type_traits>
+
 #include "common.hpp"
 #include "gemm_bf16.hpp"
 
 namespace fm {
 namespace {
 
-constexpr int BAL_C = 64;        // tokens per block of the first pass
+constexpr int BAL_C = 32;        // tokens per block of the first pass
 constexpr int BAL_MAX_B = 4096;  // sequences
 
-template <int G> __device__ __forceinline__ float group_max(float v) {
-#pragma unroll
-  for (int o = G / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-  return v;
-}
 template <int G> __device__ __forceinline__ float group_sum(float v) {
 #pragma unroll
   for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
 
-// p of a row for this lane's experts sub + 64 i; all 0 for a row of nothing but
-// -inf.  (fmaxf drops a NaN; exp(NaN - m) brings it back.)
-template <int G, int NE>
-__device__ __forceinline__ void row_softmax(const float* row, int sub, int E, float* p) {
-  float m = -INFINITY;
+// The logits of U rows for this lane's experts sub + 64 i (row u at rows[u]; -inf
+// past E), then p in their place; all 0 for a row of nothing but -inf.  The rows'
+// steps are interleaved, so that one row's loads and exchanges cover another's.
+template <int G, int NE, int U>
+__device__ __forceinline__ void rows_softmax(const float* const (&rows)[U], int sub, int E, float (&p)[U][NE]) {
+  float m[U], s[U];
 #pragma unroll
-  for (int i = 0; i < NE; ++i) {
-    p[i] = sub + 64 * i < E ? row[sub + 64 * i] : -INFINITY;
-    m = fmaxf(m, p[i]);
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int i = 0; i < NE; ++i) p[u][i] = sub + 64 * i < E ? gptr(rows[u])[sub + 64 * i] : -INFINITY;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    m[u] = p[u][0];
+#pragma unroll
+    for (int i = 1; i < NE; ++i) m[u] = fmaxf(m[u], p[u][i]);   // drops a NaN; exp(NaN - m) brings it back
   }
-  m = group_max<G>(m);
-  const float base = m == -INFINITY ? 0.f : m;
-  float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < NE; ++i) {
-    p[i] = expf(p[i] - base);
-    s += p[i];
+  for (int o = G / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int u = 0; u < U; ++u) m[u] = fmaxf(m[u], __shfl_xor(m[u], o));
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const float base = m[u] == -INFINITY ? 0.f : m[u];
+    s[u] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NE; ++i) {
+      p[u][i] = expf(p[u][i] - base);
+      s[u] += p[u][i];
+    }
   }
-  s = group_sum<G>(s);
-  const float r = s == 0.f ? 0.f : 1.0f / s;
 #pragma unroll
-  for (int i = 0; i < NE; ++i) p[i] *= r;
+  for (int o = G / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int u = 0; u < U; ++u) s[u] += __shfl_xor(s[u], o);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const float r = s[u] == 0.f ? 0.f : 1.0f / s[u];
+#pragma unroll
+    for (int i = 0; i < NE; ++i) p[u][i] *= r;
+  }
 }
 
 __device__ __forceinline__ int seg_at(const int32_t* seg, int b, int Tn) {
@@ -96,76 +111,80 @@ struct BalArgs {
 };
 
 template <int G, int NE> __global__ __launch_bounds__(256) void k_balance_rows(BalArgs a, BalWs w) {
-  constexpr int NG = 256 / G;   // groups per block
-  __shared__ float ssum[NG][G * NE + 1];
-  __shared__ int scnt[NG][G * NE + 1];
-  __shared__ int sn[NG];
+  constexpr int NG = 256 / G;              // groups per block
+  constexpr int U = BAL_C > NG ? (BAL_C / NG < 4 ? BAL_C / NG : 4) : 1;   // tokens of a group in flight
+  __shared__ float sp[BAL_C][G * NE];      // p of the block's tokens, 0 where not kept
+  __shared__ int scnt[G * NE], skept[BAL_C];
+  extern __shared__ int segs[];            // B + 1 when there are sequences
   const int sub = threadIdx.x % G, grp = threadIdx.x / G;
-  const int t0 = min(blockIdx.x * BAL_C, a.Tn), t1 = min(t0 + BAL_C, a.Tn);
+  const int t0 = min(blockIdx.x * BAL_C, a.Tn), nt = min(BAL_C, a.Tn - t0);
   if (blockIdx.x == 0 && threadIdx.x == 0) *w.done = 0;
-  int b = 0;
+  if (a.seg)
+    for (int i = threadIdx.x; i <= a.B; i += 256) segs[i] = seg_at(a.seg, i, a.Tn);
+  // this thread's choices: every 256th of the block's
+  constexpr int MC = BAL_C * 16 / 256;
+  int ce[MC], ct[MC];
+#pragma unroll
+  for (int c = 0; c < MC; ++c) {
+    const int i = threadIdx.x + 256 * c;
+    ct[c] = i / a.k;
+    ce[c] = ct[c] < nt ? a.idx[(size_t)t0 * a.k + i] : -1;
+    if (ct[c] < nt && a.keep && !a.keep[t0 + ct[c]]) ce[c] = -1;
+  }
+  if (threadIdx.x < BAL_C) skept[threadIdx.x] = (int)threadIdx.x < nt && (!a.keep || a.keep[t0 + threadIdx.x]);
+#pragma unroll
+  for (int r0 = 0; r0 < BAL_C; r0 += U * NG) {
+    const float* rows[U];
+    float p[U][NE];
+    if (r0 + grp >= nt) break;   // whole groups
+#pragma unroll
+    for (int u = 0; u < U; ++u) rows[u] = a.logits + (size_t)(t0 + min(r0 + grp + u * NG, nt - 1)) * a.E;
+    rows_softmax<G, NE, U>(rows, sub, a.E, p);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + grp + u * NG;
+      if (r >= nt) break;
+      const bool kept = !a.keep || a.keep[t0 + r];
+#pragma unroll
+      for (int i = 0; i < NE; ++i) sp[r][sub + G * i] = kept ? p[u][i] : 0.f;
+    }
+  }
+  __syncthreads();
+  int b = 0, total = 0;
   if (a.seg) {   // the first sequence that ends behind t0
     int hi = a.B;
     while (b < hi) {
       const int mid = (b + hi) >> 1;
-      if (seg_at(a.seg, mid + 1, a.Tn) <= t0) b = mid + 1;
+      if (segs[mid + 1] <= t0) b = mid + 1;
       else hi = mid;
     }
   }
-  int total = 0;
   for (; b < a.B; ++b) {
-    const int s0 = a.seg ? max(seg_at(a.seg, b, a.Tn), t0) : t0;
-    const int s1 = a.seg ? min(seg_at(a.seg, b + 1, a.Tn), t1) : t1;
-    if (s0 >= t1) break;
+    const int s0 = a.seg ? max(segs[b] - t0, 0) : 0, s1 = a.seg ? min(segs[b + 1] - t0, nt) : nt;
+    if (s0 >= nt) break;
     if (s1 <= s0) continue;
-    float acc[NE];
-    int cnt[NE], n = 0;
-#pragma unroll
-    for (int i = 0; i < NE; ++i) acc[i] = 0.f, cnt[i] = 0;
-    for (int t = s0 + grp; t < s1; t += NG) {
-      if (a.keep && !a.keep[t]) continue;
-      float p[NE];
-      row_softmax<G, NE>(a.logits + (size_t)t * a.E, sub, a.E, p);
-      ++n;
-#pragma unroll
-      for (int i = 0; i < NE; ++i) acc[i] += p[i];
-      for (int j = 0; j < a.k; ++j) {
-        const int e = a.idx[(size_t)t * a.k + j];
-#pragma unroll
-        for (int i = 0; i < NE; ++i) cnt[i] += e == sub + 64 * i;
-      }
-    }
-    __syncthreads();   // the last sequence's sums are read
-#pragma unroll
-    for (int i = 0; i < NE; ++i) ssum[grp][sub + G * i] = acc[i], scnt[grp][sub + G * i] = cnt[i];
-    if (sub == 0) sn[grp] = n;
+    for (int e = threadIdx.x; e < G * NE; e += 256) scnt[e] = 0;
     __syncthreads();
+    // integer counts: their order does not matter
+#pragma unroll
+    for (int c = 0; c < MC; ++c)
+      if (ct[c] >= s0 && ct[c] < s1 && (unsigned)ce[c] < (unsigned)a.E) atomicAdd(&scnt[ce[c]], 1);
     const size_t slot = (size_t)blockIdx.x + b;
-    for (int e = threadIdx.x; e < a.E; e += 256) {
-      float s = 0.f;
-      int c = 0;
-      for (int g = 0; g < NG; ++g) s += ssum[g][e], c += scnt[g][e];
-      w.psum[slot * a.E + e] = s;
-      w.pcnt[slot * a.E + e] = c;
+    float s = 0.f;
+    if ((int)threadIdx.x < a.E)
+      for (int r = s0; r < s1; ++r) s += sp[r][threadIdx.x];
+    int n = 0;
+    for (int r = s0; r < s1; ++r) n += skept[r];
+    __syncthreads();
+    if ((int)threadIdx.x < a.E) {
+      w.psum[slot * a.E + threadIdx.x] = s;
+      w.pcnt[slot * a.E + threadIdx.x] = scnt[threadIdx.x];
     }
-    n = 0;
-    for (int g = 0; g < NG; ++g) n += sn[g];
     if (threadIdx.x == 0) w.pn[slot] = n;
     total += n;
+    __syncthreads();   // scnt is read
   }
   if (threadIdx.x == 0) w.blockn[blockIdx.x] = total;
-}
-
-// Sum over the block's 1024 threads in a fixed order, in every thread.
-template <typename V> __device__ __forceinline__ V block_sum(V v, V* red) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  __syncthreads();
-  if (lane_id() == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = red[0];
-  for (int i = 1; i < 16; ++i) v += red[i];
-  return v;
 }
 
 // One block per sequence: EP = E rounded up to a power of two, 1024 / EP groups of
@@ -175,48 +194,76 @@ __global__ __launch_bounds__(1024) void k_balance_final(BalArgs a, BalWs w, int 
                                                         float* __restrict__ loss) {
   __shared__ double red[1024];
   __shared__ int redi[1024];
+  __shared__ int wn[16], wb[16];
+  __shared__ double wl[16];
   __shared__ int last;
   const int b = blockIdx.x, e = threadIdx.x & (EP - 1), g = threadIdx.x / EP, ng = 1024 / EP;
+  const int lane = lane_id(), wave = threadIdx.x >> 6;
   const int s0 = a.seg ? seg_at(a.seg, b, a.Tn) : 0, s1 = a.seg ? seg_at(a.seg, b + 1, a.Tn) : a.Tn;
   const int i0 = s0 / BAL_C, i1 = s1 > s0 ? (s1 - 1) / BAL_C + 1 : i0;
-  int n = 0, nbv = 0;
+  int n = 0, own = 0, c = 0;   // tokens of all sequences, of this one; choices of e
   for (int i = threadIdx.x; i < nb; i += 1024) n += w.blockn[i];
-  for (int i = i0 + (int)threadIdx.x; i < i1; i += 1024) nbv += w.pn[i + b];
-  n = block_sum(n, redi);
-  nbv = block_sum(nbv, redi);
+  for (int i = i0 + (int)threadIdx.x; i < i1; i += 1024) own += w.pn[i + b];
   double s = 0.0;
-  int c = 0;
-  if (e < a.E)
+  if (e < a.E) {
+#pragma unroll 4
     for (int i = i0 + g; i < i1; i += ng) {
       s += (double)w.psum[(size_t)(i + b) * a.E + e];
       c += w.pcnt[(size_t)(i + b) * a.E + e];
     }
-  __syncthreads();
+  }
+  // lanes with the same expert, then (below) the waves
+  for (int o = EP; o < 64; o <<= 1) {
+    s += __shfl_xor(s, o);
+    c += __shfl_xor(c, o);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    n += __shfl_xor(n, o);
+    own += __shfl_xor(own, o);
+  }
+  if (lane == 0) wn[wave] = n, wb[wave] = own;
   red[threadIdx.x] = s;
   redi[threadIdx.x] = c;
   __syncthreads();
   double part = 0.0;
   if (threadIdx.x < (unsigned)a.E) {
-    for (int h = 1; h < ng; ++h) s += red[h * EP + e], c += redi[h * EP + e];
-    const double dp = nbv > 0 ? (double)coef * a.E * c / ((double)a.k * n * nbv) : 0.0;
+    const int step = EP < 64 ? 64 : EP;
+    for (int h = threadIdx.x + step; h < 1024; h += step) s += red[h], c += redi[h];
+    n = own = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) n += wn[i], own += wb[i];
+    const double dp = own > 0 ? (double)coef * a.E * c / ((double)a.k * n * own) : 0.0;
     counts[(size_t)b * a.E + e] = c;
     dprob[(size_t)b * a.E + e] = (float)dp;
     part = dp * s;
   }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) part += __shfl_xor(part, o);
+  if (lane == 0) wl[wave] = part;   // E <= 256: 0 from wave 4 on
   __syncthreads();
-  part = block_sum(part, red);
-  // the block that finishes last adds the sequences' shares, in their order
   if (threadIdx.x == 0) {
+    part = wl[0] + wl[1] + wl[2] + wl[3];
+    if (gridDim.x == 1) *loss = (float)part;
     __hip_atomic_store(w.lpart + b, part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    last = __hip_atomic_fetch_add(w.done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+    // the block that finishes last adds the sequences' shares, in their order
+    last = gridDim.x > 1 && __hip_atomic_fetch_add(w.done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
   }
+  if (gridDim.x == 1) return;
   __syncthreads();
   if (!last) return;
   part = 0.0;
   for (int i = threadIdx.x; i < (int)gridDim.x; i += 1024)
     part += __hip_atomic_load(w.lpart + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  part = block_sum(part, red);
-  if (threadIdx.x == 0) *loss = (float)part;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) part += __shfl_xor(part, o);
+  __syncthreads();   // wl is read
+  if (lane == 0) wl[wave] = part;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 16; ++i) part += wl[i];
+    *loss = (float)part;
+  }
 }
 
 struct DlogitArgs {
@@ -230,10 +277,12 @@ struct DlogitArgs {
   float* out;
 };
 
-// One group of lanes per token, BAL_D tokens per group.
-constexpr int BAL_D = 4;
+// One group of lanes per token, U tokens of a group at once.  The k <= E <= G
+// choices of a token lie in the group's first lanes and are dealt from there (E >
+// 64: k <= 16 of 64 lanes).
+template <int G, int NE> constexpr int dlogit_rows() { return G == 64 ? 2 : 1; }
 template <int G, int NE> __global__ __launch_bounds__(256) void k_balance_dlogits(DlogitArgs a) {
-  constexpr int NG = 256 / G;
+  constexpr int NG = 256 / G, U = dlogit_rows<G, NE>();
   extern __shared__ int segs[];   // B + 1 when there are sequences
   const int sub = threadIdx.x % G, grp = threadIdx.x / G;
   if (a.seg) {
@@ -241,50 +290,61 @@ template <int G, int NE> __global__ __launch_bounds__(256) void k_balance_dlogit
     __syncthreads();
   }
   const float up = a.dloss ? *a.dloss : 1.f;
-  for (int u = 0; u < BAL_D; ++u) {
-    const long t = ((long)blockIdx.x * BAL_D + u) * NG + grp;
-    if (t >= a.Tn) return;
-    bool in = !a.keep || a.keep[t];
-    int b = 0;
+  long t[U];
+  const float* rows[U];
+  bool in[U];
+  int b[U];
+  float d[U][NE], w[U][NE];
+  int ei[U];
+  float gv[U], dv[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    t[u] = ((long)blockIdx.x * U + u) * NG + grp;
+    const long tc = min(t[u], (long)a.Tn - 1);
+    rows[u] = a.logits + (size_t)tc * a.E;
+    in[u] = !a.keep || a.keep[tc];
+    b[u] = 0;
     if (a.seg) {   // the sequence with segs[b] <= t < segs[b + 1]
       int lo = 0, hi = a.B;
       while (lo < hi) {
         const int mid = (lo + hi) >> 1;
-        if (segs[mid + 1] <= t) lo = mid + 1;
+        if (segs[mid + 1] <= tc) lo = mid + 1;
         else hi = mid;
       }
-      b = lo;
-      in = in && b < a.B && segs[b] <= t;
+      in[u] = in[u] && lo < a.B && segs[lo] <= tc;
+      b[u] = min(lo, a.B - 1);
     }
-    float d[NE];
 #pragma unroll
-    for (int i = 0; i < NE; ++i) d[i] = 0.f;
-    if (in) {
-      float p[NE], w[NE], q = 0.f;
-      row_softmax<G, NE>(a.logits + (size_t)t * a.E, sub, a.E, p);
+    for (int i = 0; i < NE; ++i) w[u][i] = sub + 64 * i < a.E ? a.dprob[(size_t)b[u] * a.E + sub + 64 * i] : 0.f;
+    const bool chosen = a.gate && sub < a.k;
+    const size_t r = (size_t)tc * a.k + sub;
+    ei[u] = chosen ? a.idx[r] : -1;
+    gv[u] = chosen ? a.gate[r] : 0.f;
+    dv[u] = chosen ? a.dgate[r] : 0.f;
+  }
+  rows_softmax<G, NE, U>(rows, sub, a.E, d);
 #pragma unroll
-      for (int i = 0; i < NE; ++i) {
-        w[i] = sub + 64 * i < a.E ? a.dprob[(size_t)b * a.E + sub + 64 * i] : 0.f;
-        q = fmaf(p[i], w[i], q);
-      }
-      q = group_sum<G>(q);
+  for (int u = 0; u < U; ++u) {
+    float q = 0.f;
 #pragma unroll
-      for (int i = 0; i < NE; ++i) d[i] = up * p[i] * (w[i] - q);
-    }
+    for (int i = 0; i < NE; ++i) q = fmaf(d[u][i], w[u][i], q);
+    q = group_sum<G>(q);
+#pragma unroll
+    for (int i = 0; i < NE; ++i) d[u][i] = in[u] ? up * d[u][i] * (w[u][i] - q) : 0.f;
     if (a.gate) {
-      const size_t r = (size_t)t * a.k;
-      float inner = 0.f;
-      for (int j = 0; j < a.k; ++j) inner = fmaf(a.gate[r + j], a.dgate[r + j], inner);
+      dv[u] = gv[u] * (dv[u] - group_sum<G>(gv[u] * dv[u]));
       for (int j = 0; j < a.k; ++j) {
-        const int e = a.idx[r + j];
-        const float v = a.gate[r + j] * (a.dgate[r + j] - inner);
+        const int e = __shfl(ei[u], j, G);
+        const float v = __shfl(dv[u], j, G);
 #pragma unroll
-        for (int i = 0; i < NE; ++i) d[i] += e == sub + 64 * i ? v : 0.f;
+        for (int i = 0; i < NE; ++i) d[u][i] += e == sub + 64 * i ? v : 0.f;
       }
     }
+    if (t[u] < a.Tn) {
 #pragma unroll
-    for (int i = 0; i < NE; ++i)
-      if (sub + 64 * i < a.E) a.out[(size_t)t * a.E + sub + 64 * i] = d[i];
+      for (int i = 0; i < NE; ++i)
+        if (sub + 64 * i < a.E) a.out[(size_t)t[u] * a.E + sub + 64 * i] = d[u][i];
+    }
   }
 }
 
@@ -302,14 +362,29 @@ template <typename Fn> void with_expert_lanes(int E, Fn fn) {
 }
 
 // ------------------------------------------------- products of the backward --
-// Both products on v_mfma_f32_32x32x2_f32 (operands exact in fp32).  An operand
-// lane holds one value, row lane % 32 at k = lane / 32, which is a coalesced read
-// of the row-major inputs whichever of them runs along k.  Output rows m of a tile
-// (the first operand's) are dealt to columns so that a lane's 16 sums are 16
-// consecutive columns: column(m) = 16 ((m / 4) % 2) + 4 (m / 8) + m % 4.
+// A block of 4 waves owns 128 columns (32 per wave) and a part of the token range,
+// and walks it in slabs of 64 tokens, of which it forms dX and adds to its part of
+// dWr at once: the slab's dlogits are read and taken apart once for both.
+//
+// bf16.  dlogits are fp32, the other operand is bf16: an fp32 value is the sum of
+// three bf16 (high, middle, low: 8 bits each), whose products with a bf16 are exact
+// in fp32, so dWr is three MFMAs with fp32 accuracy (v_mfma_f32_32x32x16_bf16, 16
+// times the rate of the fp32 MFMA) and dX, rounded to bf16 itself, two (16 bits).
+// The three planes lie in LDS as [64 tokens][32 experts], X as [64 tokens][32 columns]
+// per wave: dWr sums over tokens and reads both transposed (ds_read_b64_tr_b16), dX
+// sums over experts and reads the planes along their rows (16-byte chunks of a row
+// swizzled by (row / 4) % 4, so that 16 rows read at one chunk cover the 64 banks
+// once).  Wr's fragments stay in registers.
+//
+// fp32.  v_mfma_f32_32x32x2_f32: an operand lane holds one value, row lane % 32 at k
+// = lane / 32, a coalesced read of the row-major inputs whichever of them runs along k.
+//
+// Both: rows m of dX's first operand are dealt to columns so that a lane's 16 sums are
+// 16 consecutive columns: column(m) = 16 ((m / 4) % 2) + 4 (m / 8) + m % 4.
 __device__ __forceinline__ int tile_column(int m) { return 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
 
-constexpr int RB_SPLITS = 32;   // most parts of the token range in dWr
+constexpr int RB_SLAB = 64;     // tokens
+constexpr int RB_SPLITS = 32;   // most parts of the token range
 
 struct RouterBwd {
   const float* dl;
@@ -318,21 +393,205 @@ struct RouterBwd {
   void* dX;
   int acc_dx;
   float *part, *partb;   // [splits][E][d], [splits][E], or NULL
-  int splits, span;      // tokens per split
-  int n_dw;              // blocks of the weight gradient, before those of dX
-  int xt;                // token tiles per block of dX
+  int span;              // tokens per split, a multiple of RB_SLAB
 };
 
+// The old dX of a lane's 16 columns plus r, or r alone, to dX.
+template <typename T> __device__ __forceinline__ void put_dx(T* o, int cols, bool add, const f32x16_t& acc) {
+  constexpr int V = 16 / sizeof(T);
+#pragma unroll
+  for (int i = 0; i < 16; i += V) {
+    if (i >= cols) continue;
+    float r[V];
+#pragma unroll
+    for (int x = 0; x < V; ++x) r[x] = acc[i + x];
+    if (add) {
+      float old[V];
+      unpack16(ld16(o + i), old, (T*)nullptr);
+#pragma unroll
+      for (int x = 0; x < V; ++x) r[x] += old[x];
+    }
+    st16(o + i, pack16(r, (T*)nullptr));
+  }
+}
+
+// a, b, c with a + b + c = v to 24 bits, each a bf16 (an infinity stays in a).
+__device__ __forceinline__ void split3(f32x4_t v, u32x2_t (&p)[3]) {
+  float r[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    p[k] = u32x2_t{pk_bf16(r[0], r[1]), pk_bf16(r[2], r[3])};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float h = __uint_as_float(i & 1 ? p[k][i >> 1] & 0xFFFF0000u : p[k][i >> 1] << 16);
+      r[i] = fabsf(h) == INFINITY ? 0.f : r[i] - h;
+    }
+  }
+}
+
 // NT = expert tiles of 32.
-template <typename T, int NT> __global__ __launch_bounds__(256) void k_router_bwd(RouterBwd a) {
+template <int NT> __global__ __launch_bounds__(256, NT <= 4 ? 2 : 1) void k_router_bf16(RouterBwd a) {
+  constexpr int BLK = RB_SLAB * 64;   // bytes of a block [64 tokens][32 bf16]
+  __shared__ __align__(16) char lds_[2 * 4 * BLK + 3 * NT * BLK];
+  FM_LDS char* const xs = (FM_LDS char*)lds_;
+  FM_LDS char* const pl = xs + 2 * 4 * BLK;
   const int lane = lane_id(), wave = wave_id(), m = lane & 31, h = lane >> 5;
-  const int ct = (a.d + 127) / 128;   // blocks of 4 column tiles
-  if ((int)blockIdx.x < a.n_dw) {
-    const int split = blockIdx.x / ct, c0 = (blockIdx.x % ct) * 128 + wave * 32;
-    const int t0 = split * a.span, t1 = min(t0 + a.span, a.Tn);
+  const int ct = (a.d + 127) / 128, split = blockIdx.x / ct;
+  const int c0 = (blockIdx.x % ct) * 128 + wave * 32;
+  const int t0 = split * a.span, t1 = min(t0 + a.span, a.Tn);
+  const bool on = c0 < a.d, dw = a.part && on, dx = a.dX && on;
+  const bool bias = a.partb && blockIdx.x % ct == 0;
+  const bf16* const X = (const bf16*)a.X;
+
+  // X: this wave's columns, 16 tokens per instruction; columns past d repeat the last
+  const int xc = min(c0 + 8 * (lane & 3), a.d - 8);
+  auto load_x = [&](int t, int buf) {
+    if (!dw) return;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int r = min(t + 16 * u + (lane >> 2), t1 - 1);   // a row past the end meets zero dlogits
+      dma16(X + (size_t)r * a.d + xc, xs + (buf * 4 + wave) * BLK + u * 1024);
+    }
+  };
+  // dlogits: thread q of the slab's quads, 4 experts of token q / (8 NT)
+  constexpr int QT = 8 * NT, QN = RB_SLAB * QT / 256;
+  const int quad = threadIdx.x % QT, e0 = 4 * quad;
+  f32x4_t dl[QN], bsum = {0.f, 0.f, 0.f, 0.f};
+  auto load_dl = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < QN; ++i) {
+      const int r = t + threadIdx.x / QT + i * (256 / QT);
+      const FM_GLOBAL float* const p = gptr(a.dl) + (size_t)min(r, t1 - 1) * a.E;
+      if (a.E % 4 == 0) {   // whole quads, 16-byte aligned
+        dl[i] = *(const FM_GLOBAL f32x4_t*)(p + min(e0, a.E - 4));
+        if (r >= t1 || e0 >= a.E) dl[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        continue;
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const float v = p[min(e0 + x, a.E - 1)];
+        dl[i][x] = r < t1 && e0 + x < a.E ? v : 0.f;
+      }
+    }
+  };
+  // Wr: lane m's column, experts 16 s + 8 h + [0, 8)
+  bf16x8_t wf[2 * NT];
+  if (dx) {
+    const FM_GLOBAL uint16_t* const Wr = (const FM_GLOBAL uint16_t*)a.Wr + min(c0 + tile_column(m), a.d - 1);
+#pragma unroll
+    for (int s = 0; s < 2 * NT; ++s) {
+      uint32_t v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int e = 16 * s + 8 * h + i;
+        v[i] = Wr[(size_t)min(e, a.E - 1) * a.d];
+        if (e >= a.E) v[i] = 0;
+      }
+      wf[s] = __builtin_bit_cast(bf16x8_t, u32x4_t{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16});
+    }
+  }
+  f32x16_t acc[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
+  B16Frag<false, 32, 1> fr;
+  fr.init(0);
+  // as fr, for the swizzled planes: rows 8 (lane / 32) + [0, 4) and + [4, 8) of a step
+  const int sw = 2 * h;
+  const uint32_t f0 = (fr.off[0] & ~48u) | (((fr.off[0] >> 4) & 3) ^ sw) << 4, f1 = f0 ^ 16;
+  auto read_pl = [&](const FM_LDS char* blk, int ks) {
+    const FM_LDS char* const p = blk + ks * 1024;
+    const u32x2_t w0 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((FM_LDS i16x4_t*)(p + f0)));
+    const u32x2_t w1 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((FM_LDS i16x4_t*)(p + 256 + f1)));
+    return __builtin_bit_cast(bf16x8_t, u32x4_t{w0[0], w0[1], w1[0], w1[1]});
+  };
+
+  load_x(t0, 0);
+  load_dl(t0);
+  int buf = 0;
+  for (int t = t0; t < t1; t += RB_SLAB, buf ^= 1) {
+    wait_vmcnt<0>();
+    __syncthreads();   // the planes of the last slab are read
+#pragma unroll
+    for (int i = 0; i < QN; ++i) {
+      u32x2_t p[3];
+      split3(dl[i], p);
+      const int r = threadIdx.x / QT + i * (256 / QT);
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        *(FM_LDS u32x2_t*)(pl + (k * NT + (quad >> 3)) * BLK + r * 64 + ((((quad & 7) >> 1) ^ ((r >> 2) & 3)) << 4) + (quad & 1) * 8) = p[k];
+      if (bias) bsum += dl[i];
+    }
+    __syncthreads();
+    if (t + RB_SLAB < t1) {
+      load_x(t + RB_SLAB, buf ^ 1);
+      load_dl(t + RB_SLAB);
+    }
+    if (dw) {
+#pragma unroll
+      for (int ks = 0; ks < RB_SLAB / 16; ++ks) {
+        const bf16x8_t x = fr.read(xs + (buf * 4 + wave) * BLK, 0, ks);
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int k = 0; k < 3; ++k)
+            acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_pl(pl + (k * NT + j) * BLK, ks), x, acc[j], 0, 0, 0);
+      }
+    }
+    if (dx) {
+#pragma unroll
+      for (int tb = 0; tb < RB_SLAB / 32; ++tb) {
+        f32x16_t o;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[i] = 0.f;
+#pragma unroll
+        for (int s = 0; s < 2 * NT; ++s)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const FM_LDS char* const p = pl + (k * NT + (s >> 1)) * BLK + (32 * tb + m) * 64 +
+                                     (((2 * (s & 1) + h) ^ ((m >> 2) & 3)) << 4);
+            o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[s], __builtin_bit_cast(bf16x8_t, *(const FM_LDS u32x4_t*)p), o, 0, 0, 0);
+          }
+        const int r = t + 32 * tb + m, c = c0 + 16 * h;
+        if (r < t1) put_dx((bf16*)a.dX + (size_t)r * a.d + c, a.d - c, a.acc_dx, o);
+      }
+    }
+  }
+  if (dw) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int e = 32 * j + 8 * (i >> 2) + 4 * h + (i & 3);
+        if (e < a.E && c0 + m < a.d) gptr(a.part)[((size_t)split * a.E + e) * a.d + c0 + m] = acc[j][i];
+      }
+  }
+  if (bias) {   // the block's threads with the same experts, in order
+    __syncthreads();
+    FM_LDS f32x4_t* const b4 = (FM_LDS f32x4_t*)xs;
+    b4[threadIdx.x] = bsum;
+    __syncthreads();
+    if (threadIdx.x < QT) {
+      for (int g = 1; g < 256 / QT; ++g) bsum += b4[threadIdx.x + g * QT];
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        if (e0 + x < a.E) gptr(a.partb)[(size_t)split * a.E + e0 + x] = bsum[x];
+    }
+  }
+}
+
+template <int NT> __global__ __launch_bounds__(256) void k_router_f32(RouterBwd a) {
+  const int lane = lane_id(), wave = wave_id(), m = lane & 31, h = lane >> 5;
+  const int ct = (a.d + 127) / 128, split = blockIdx.x / ct;
+  const int c0 = (blockIdx.x % ct) * 128 + wave * 32;
+  if (c0 >= a.d) return;
+  const int t0 = split * a.span, t1 = min(t0 + a.span, a.Tn);
+  const FM_GLOBAL float* const dl = gptr(a.dl);
+  if (a.part || a.partb) {
     const int c = min(c0 + tile_column(m), a.d - 1);
-    const bool bias = a.partb && c0 == 0, on = c0 < a.d;
-    if (!on) return;
+    const bool bias = a.partb && c0 == 0;
+    const FM_GLOBAL float* const X = (const FM_GLOBAL float*)a.X;
     f32x16_t acc[NT];
     float bs[NT];
 #pragma unroll
@@ -341,18 +600,26 @@ template <typename T, int NT> __global__ __launch_bounds__(256) void k_router_bw
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
     }
-    const T* X = (const T*)a.X;
-    for (int t = t0; t < t1; t += 2) {
-      const int tt = t + h;
-      const bool in = tt < t1;
-      const float x = in && X ? to_float(X[(size_t)tt * a.d + c]) : 0.f;
+    constexpr int U = NT <= 2 ? 8 : 4;   // steps (2 tokens each) whose loads are in flight together
+    for (int t = t0; t < t1; t += 2 * U) {
+      float x[U], v[U][NT];
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const int e = 32 * j + m;
-        const float v = in && e < a.E ? a.dl[(size_t)tt * a.E + e] : 0.f;
-        bs[j] += v;
-        acc[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, v, acc[j], 0, 0, 0);
+      for (int u = 0; u < U; ++u) {
+        const int r = t + 2 * u + h, rc = min(r, t1 - 1);
+        x[u] = a.X ? X[(size_t)rc * a.d + c] : 0.f;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          v[u][j] = dl[(size_t)rc * a.E + min(32 * j + m, a.E - 1)];
+          if (r >= t1 || 32 * j + m >= a.E) v[u][j] = 0.f;
+        }
       }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          bs[j] += v[u][j];
+          acc[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[u], v[u][j], acc[j], 0, 0, 0);
+        }
     }
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
@@ -360,79 +627,69 @@ template <typename T, int NT> __global__ __launch_bounds__(256) void k_router_bw
       if (e >= a.E) continue;
       if (bias) {
         const float s = bs[j] + __shfl_xor(bs[j], 32);
-        if (h == 0) a.partb[(size_t)split * a.E + e] = s;
+        if (h == 0) gptr(a.partb)[(size_t)split * a.E + e] = s;
       }
       if (a.part) {
         float* o = a.part + ((size_t)split * a.E + e) * a.d + c0 + 16 * h;
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
-          if (c0 + 16 * h + i < a.d)
-            st16(o + i, u32x4_t{__float_as_uint(acc[j][i]), __float_as_uint(acc[j][i + 1]),
-                                __float_as_uint(acc[j][i + 2]), __float_as_uint(acc[j][i + 3])});
+          if (c0 + 16 * h + i < a.d) store4(o + i, f32x4_t{acc[j][i], acc[j][i + 1], acc[j][i + 2], acc[j][i + 3]});
       }
     }
-    return;
   }
-  const int blk = blockIdx.x - a.n_dw;
-  const int c0 = (blk % ct) * 128 + wave * 32, c = min(c0 + tile_column(m), a.d - 1);
-  if (c0 >= a.d) return;
+  if (!a.dX) return;
   // this wave's 32 columns of Wr: half h holds experts 32 j + 16 h + [0, 16)
-  const T* Wr = (const T*)a.Wr;
+  const int c = min(c0 + tile_column(m), a.d - 1);
+  const FM_GLOBAL float* const Wr = (const FM_GLOBAL float*)a.Wr;
   float w[NT][16];
 #pragma unroll
   for (int j = 0; j < NT; ++j)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int e = 32 * j + 16 * h + i;
-      w[j][i] = e < a.E ? to_float(Wr[(size_t)e * a.d + c]) : 0.f;
+      w[j][i] = e < a.E ? Wr[(size_t)min(e, a.E - 1) * a.d + c] : 0.f;
     }
-  T* dX = (T*)a.dX;
-  constexpr int V = 16 / sizeof(T);
-  for (int u = 0; u < a.xt; ++u) {
-    const long t0 = ((long)(blk / ct) * a.xt + u) * 32;
-    if (t0 >= a.Tn) break;
-    const long t = t0 + m < a.Tn ? t0 + m : a.Tn - 1;
+  for (int t = t0; t < t1; t += 32) {
+    const int r = min(t + m, t1 - 1);
     f32x16_t acc;
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[i] = 0.f;
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int j = 0; j < NT; ++j) {
+      float v[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int e = 32 * j + 16 * h + i;
-        const float v = e < a.E ? a.dl[(size_t)t * a.E + e] : 0.f;
-        acc = __builtin_amdgcn_mfma_f32_32x32x2f32(w[j][i], v, acc, 0, 0, 0);
+        v[i] = e < a.E ? dl[(size_t)r * a.E + min(e, a.E - 1)] : 0.f;
       }
-    if (t0 + m >= a.Tn) continue;
-    T* o = dX + (size_t)t * a.d + c0 + 16 * h;
 #pragma unroll
-    for (int i = 0; i < 16; i += V) {
-      if (c0 + 16 * h + i >= a.d) continue;
-      float r[V];
-#pragma unroll
-      for (int x = 0; x < V; ++x) r[x] = acc[i + x];
-      if (a.acc_dx) {
-        float old[V];
-        unpack16(ld16(o + i), old, (T*)nullptr);
-#pragma unroll
-        for (int x = 0; x < V; ++x) r[x] += old[x];
-      }
-      st16(o + i, pack16(r, (T*)nullptr));
+      for (int i = 0; i < 16; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(w[j][i], v[i], acc, 0, 0, 0);
     }
+    if (t + m < t1) put_dx((float*)a.dX + (size_t)r * a.d + c0 + 16 * h, a.d - c0 - 16 * h, a.acc_dx, acc);
   }
 }
 
-// dWr and dbias from their parts, in split order; 4 columns per thread.
+// dWr and dbias from their parts: a block takes 64 quads of columns, its 4 groups of
+// threads every fourth part, and the groups' sums are added in order.
 __global__ __launch_bounds__(256) void k_router_dw(const float* __restrict__ part, const float* __restrict__ partb,
                                                    int splits, long n, int E, int accumulate, float* __restrict__ dWr,
                                                    float* __restrict__ dbias) {
-  const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 4;
-  if (dWr && i < n) {
-    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
-    if (accumulate) s = load4(dWr + i);
+  __shared__ f32x4_t red[4][64];
+  const int q = threadIdx.x & 63, g = threadIdx.x >> 6;
+  const long i = ((long)blockIdx.x * 64 + q) * 4;
+  if (dWr) {
     f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < splits; ++p) v += load4(part + (size_t)p * n + i);
-    store4(dWr + i, s + v);
+    if (i < n) {
+#pragma unroll 8
+      for (int p = g; p < splits; p += 4) v += load4(part + (size_t)p * n + i);
+    }
+    red[g][q] = v;
+    __syncthreads();
+    if (g == 0 && i < n) {
+      v = red[0][q] + red[1][q] + red[2][q] + red[3][q];
+      if (accumulate) v += load4(dWr + i);
+      store4(dWr + i, v);
+    }
   }
   if (dbias && blockIdx.x == 0 && threadIdx.x < (unsigned)E) {
     float v = 0.f;
@@ -441,22 +698,25 @@ __global__ __launch_bounds__(256) void k_router_dw(const float* __restrict__ par
   }
 }
 
-// Parts of the token range for dWr: enough blocks for the card, 64 tokens at
-// least in each.
+// Parts of the token range: two blocks per compute unit, whole slabs in each.
 inline int router_splits(int T, int d) {
-  const int ct = cdiv(d, 128);
+  const int ct = cdiv(d, 128), slabs = cdiv(T, RB_SLAB);
   int s = cdiv(512, ct);
   if (s > RB_SPLITS) s = RB_SPLITS;
-  const int most = cdiv(T, 64);
-  return s < most ? s : most;
+  return slabs < s ? slabs : s;
 }
 
-template <typename T> void launch_router_bwd(RouterBwd a, int blocks, hipStream_t st) {
+void launch_router_bwd(const RouterBwd& a, bool is_bf16, int blocks, hipStream_t st) {
   const dim3 g(blocks), b(256);
-  if (a.E <= 32) hipLaunchKernelGGL((k_router_bwd<T, 1>), g, b, 0, st, a);
-  else if (a.E <= 64) hipLaunchKernelGGL((k_router_bwd<T, 2>), g, b, 0, st, a);
-  else if (a.E <= 128) hipLaunchKernelGGL((k_router_bwd<T, 4>), g, b, 0, st, a);
-  else hipLaunchKernelGGL((k_router_bwd<T, 8>), g, b, 0, st, a);
+  auto run = [&](auto nt) {
+    constexpr int NT = decltype(nt)::value;
+    if (is_bf16) hipLaunchKernelGGL((k_router_bf16<NT>), g, b, 0, st, a);
+    else hipLaunchKernelGGL((k_router_f32<NT>), g, b, 0, st, a);
+  };
+  if (a.E <= 32) run(std::integral_constant<int, 1>{});
+  else if (a.E <= 64) run(std::integral_constant<int, 2>{});
+  else if (a.E <= 128) run(std::integral_constant<int, 4>{});
+  else run(std::integral_constant<int, 8>{});
 }
 
 int check_balance_shape(int T, int E, int B, const void* seg) {
@@ -498,7 +758,7 @@ extern "C" int moe_balance_loss(const float* logits, const int32_t* idx, const i
   const int nb = bal_blocks(T);
   with_expert_lanes(E, [&](auto l) {
     typedef decltype(l) L;
-    hipLaunchKernelGGL((k_balance_rows<L::G, L::NE>), dim3(nb), dim3(256), 0, st, a, w);
+    hipLaunchKernelGGL((k_balance_rows<L::G, L::NE>), dim3(nb), dim3(256), seg ? (B + 1) * sizeof(int) : 0, st, a, w);
   });
   FM_TRY(check_launch("moe_balance_loss"));
   int EP = 1;
@@ -524,7 +784,7 @@ extern "C" int moe_balance_loss_bwd(const float* logits, const float* dprob, con
   const DlogitArgs a{logits, dprob, dloss, seg, keep, gate, idx, dgate, T, E, k, B, dlogits};
   with_expert_lanes(E, [&](auto l) {
     typedef decltype(l) L;
-    hipLaunchKernelGGL((k_balance_dlogits<L::G, L::NE>), dim3(cdiv(T, BAL_D * (256 / L::G))), dim3(256),
+    hipLaunchKernelGGL((k_balance_dlogits<L::G, L::NE>), dim3(cdiv(T, dlogit_rows<L::G, L::NE>() * (256 / L::G))), dim3(256),
                        seg ? (B + 1) * sizeof(int) : 0, as_stream(stream), a);
   });
   return check_launch("moe_balance_loss_bwd");
@@ -560,27 +820,21 @@ extern "C" int moe_router_bwd(const float* dlogits, const void* X, const void* W
   }
   if (T == 0 && (!dw || accumulate_dw)) return MOE_OK;
   hipStream_t st = as_stream(stream);
-  const int ct = cdiv(d, 128), splits = T > 0 && dw ? router_splits(T, d) : 0;
+  const int splits = T > 0 ? router_splits(T, d) : 0;
   RouterBwd a{};
   a.dl = dlogits; a.X = dWr ? X : nullptr; a.Wr = Wr;
   a.Tn = T; a.d = d; a.E = E;
   a.dX = dX; a.acc_dx = accumulate_dx;
   a.part = dWr ? (float*)ws : nullptr;
   a.partb = dbias ? (float*)ws + (size_t)splits * E * d : nullptr;
-  a.splits = splits;
-  a.span = splits ? cdiv(cdiv(T, splits), 2) * 2 : 0;
-  a.n_dw = splits * ct;
-  const int tiles = cdiv(T, 32);
-  a.xt = cdiv(tiles, cdiv(1024, ct));
-  const long blocks = a.n_dw + (dX && T > 0 ? (long)ct * cdiv(tiles, a.xt) : 0);
-  if (blocks > 0) {
-    if (dtype == MOE_BF16) launch_router_bwd<bf16>(a, (int)blocks, st);
-    else launch_router_bwd<float>(a, (int)blocks, st);
+  if (T > 0) {
+    a.span = cdiv(cdiv(T, splits), RB_SLAB) * RB_SLAB;
+    launch_router_bwd(a, dtype == MOE_BF16, splits * cdiv(d, 128), st);
     FM_TRY(check_launch("moe_router_bwd"));
   }
   if (dw) {
     const long n = (long)E * d;
-    hipLaunchKernelGGL(k_router_dw, dim3(dWr ? cdiv(n, 1024) : 1), dim3(256), 0, st, a.part, a.partb, splits, n, E,
+    hipLaunchKernelGGL(k_router_dw, dim3(dWr ? cdiv(n, 256) : 1), dim3(256), 0, st, a.part, a.partb, splits, n, E,
                        accumulate_dw, dWr, dbias);
     FM_TRY(check_launch("moe_router_bwd"));
   }

@@ -288,25 +288,31 @@ __global__ __launch_bounds__(NT) void k_sublayer_bwd(NormBwd a) {
   }
 }
 
-// out[c] = (accumulate ? out[c] : 0) + the partial sums of column c in block
-// order within each of 16 groups, then the groups; 16 columns per block.
-__global__ __launch_bounds__(256) void k_sublayer_dw(const float* __restrict__ part, int blocks, int d, int accumulate,
-                                                     float* __restrict__ dw_post,
-                                                     float* __restrict__ dw_pre) {
-  __shared__ float red[16][17];
-  const int which = blockIdx.y, col = threadIdx.x & 15, grp = threadIdx.x >> 4, c = blockIdx.x * 16 + col;
+// out[c] = (accumulate ? out[c] : 0) + the partial sums of column c: 32 columns per
+// block (8 quads), its 128 groups of threads every 128th block's sums, which are then
+// added pairwise.
+__global__ __launch_bounds__(1024) void k_sublayer_dw(const float* __restrict__ part, int blocks, int d,
+                                                      int accumulate, float* __restrict__ dw_post,
+                                                      float* __restrict__ dw_pre) {
+  typedef float f4 __attribute__((ext_vector_type(4)));
+  __shared__ f4 red[128][8];
+  const int which = blockIdx.y, q = threadIdx.x & 7, grp = threadIdx.x >> 3, c = blockIdx.x * 32 + 4 * q;
   float* const out = which ? dw_pre : dw_post;
   if (!out) return;
-  float s = 0.f;
-  if (c < d)
-    for (int b = grp; b < blocks; b += 16) s += part[((size_t)b * 2 + which) * d + c];
-  red[grp][col] = s;
-  __syncthreads();
-  if (grp == 0 && c < d) {
-    s = 0.f;
+  f4 s = {0.f, 0.f, 0.f, 0.f};
+  if (c < d) {
+#pragma unroll 4
+    for (int b = grp; b < blocks; b += 128) s += *(const FM_GLOBAL f4*)(part + ((size_t)b * 2 + which) * d + c);
+  }
+  red[grp][q] = s;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s += red[r][col];
-    out[c] = accumulate ? out[c] + s : s;
+  for (int h = 64; h > 0; h >>= 1) {
+    __syncthreads();
+    if (grp < h) red[grp][q] = s += red[grp + h][q];
+  }
+  if (grp == 0 && c < d) {
+    if (accumulate) s += *(const FM_GLOBAL f4*)(out + c);
+    *(FM_GLOBAL f4*)(out + c) = s;
   }
 }
 
@@ -430,7 +436,7 @@ extern "C" int moe_sublayer_norm_bwd(const void* dS, const void* dN, const void*
     FM_TRY(check_launch("moe_sublayer_norm_bwd"));
   }
   if (dw) {
-    hipLaunchKernelGGL(k_sublayer_dw, dim3(cdiv(d, 16), 2), dim3(256), 0, st, (const float*)ws, blocks, d, accumulate_dw,
+    hipLaunchKernelGGL(k_sublayer_dw, dim3(cdiv(d, 32), 2), dim3(1024), 0, st, (const float*)ws, blocks, d, accumulate_dw,
                        dw_post, dw_pre);
     FM_TRY(check_launch("moe_sublayer_norm_bwd"));
   }

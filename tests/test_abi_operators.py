@@ -164,8 +164,23 @@ def test_mx4_forward_without_tokens_and_workspace_sizes(L):
     assert L.moe_sublayer_norm_bwd_workspace_size(0, 64) == 0
 
 
-def test_binding_refuses_shapes_it_would_misread():
+def test_binding_refuses_memory_the_library_cannot_read():
     t = lambda *s, dt=F: torch.zeros(*s, dtype=dt)  # noqa: E731
+    with pytest.raises(ValueError, match="device memory"):
+        api.moe_quantize_mxfp4(t(4, 40), t(4, 32, dt=U8), t(4, 4, dt=U8))
+    with pytest.raises(ValueError, match="device memory"):
+        api.moe_sublayer_norm(t(4, 16), None, t(4, 16), None)
+    with pytest.raises(ValueError, match="q_gate"):
+        api.LayerTablesMX4(64, 32, 2, 0, *[[t(1, dt=U8)] * 2] * 6, device="cpu")
+    with pytest.raises(ValueError, match="2 slots"):
+        api.LayerTablesMX4(64, 32, 2, 0, *[[t(1, dt=U8)]] * 6, device="cpu")
+    assert api.mxfp4_shapes(7, 688) == ((7, 352), (7, 24))
+
+
+@pytest.mark.gpu
+def test_binding_refuses_tensors_it_would_misread():
+    """Wrong shapes, types and layouts, before anything is enqueued."""
+    t = lambda *s, dt=F: torch.zeros(*s, dtype=dt, device="cuda")  # noqa: E731
     with pytest.raises(ValueError, match="counts"):
         api.moe_balance_loss(t(4, 8), t(4, 2, dt=I32), 0.1, t(2, 8, dt=I32), t(1, 8), t(1), t(64))
     with pytest.raises(ValueError, match="dprob"):
@@ -180,11 +195,11 @@ def test_binding_refuses_shapes_it_would_misread():
         api.moe_quantize_mxfp4(t(4, 40), t(4, 32, dt=U8), t(4, 2, dt=U8))
     with pytest.raises(ValueError, match="codes"):
         api.moe_dequant_mxfp4(t(4, 20, dt=U8), t(4, 4, dt=U8), t(4, 40))
-    with pytest.raises(ValueError, match="q_gate"):
-        api.LayerTablesMX4(64, 32, 2, 0, *[[t(1, dt=U8)] * 2] * 6, device="cpu")
-    with pytest.raises(ValueError, match="2 slots"):
-        api.LayerTablesMX4(64, 32, 2, 0, *[[t(1, dt=U8)]] * 6, device="cpu")
-    # right shapes, but memory the library cannot read
-    with pytest.raises(ValueError, match="device memory"):
-        api.moe_quantize_mxfp4(t(4, 40), t(4, 32, dt=U8), t(4, 4, dt=U8))
-    assert api.mxfp4_shapes(7, 688) == ((7, 352), (7, 24))
+    with pytest.raises(TypeError, match="int64"):
+        api.moe_balance_loss(t(4, 8), t(4, 2, dt=torch.int64), 0.1, t(1, 8, dt=I32), t(1, 8), t(1), t(64))
+    with pytest.raises(TypeError, match="float32"):
+        api.moe_sublayer_norm(t(4, 16, dt=torch.bfloat16), t(4, 16), t(4, 16, dt=torch.bfloat16), None)
+    with pytest.raises(ValueError, match="contiguous"):
+        api.moe_sublayer_norm(t(4, 32)[:, ::2], None, t(4, 16), None)
+    with pytest.raises(api.MoeError, match="aligned"):
+        api.moe_sublayer_norm(t(4, 16), t(4, 16), t(4, 16), None, gate=t(5)[1:])

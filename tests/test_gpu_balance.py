@@ -193,7 +193,9 @@ def test_router_backward(T, d, E, dt):
     check_router(router(dl, X, Wr, old=old), dl, X, Wr, old)
     for how in (dict(dx=False), dict(dw=False), dict(db=False), dict(dw=False, db=False), dict(dx=False, dw=False)):
         part = router(dl, X, Wr, **how)
-        assert all(v is None or torch.equal(v, out[n]) for n, v in part.items()), how
+        check_router(part, dl, X, Wr)
+        if not (part["dX"] is None and part["dWr"] is None):   # dbias alone has no type: the fp32 kernel sums it
+            assert all(v is None or torch.equal(v, out[n]) for n, v in part.items()), how
 
 
 def test_router_backward_without_tokens_and_sparse():
