@@ -362,9 +362,9 @@ template <typename Fn> void with_expert_lanes(int E, Fn fn) {
 }
 
 // ------------------------------------------------- products of the backward --
-// A block of 4 waves owns 128 columns (32 per wave) and a part of the token range,
-// and walks it in slabs of 64 tokens, of which it forms dX and adds to its part of
-// dWr at once: the slab's dlogits are read and taken apart once for both.
+// A block owns some columns and a part of the token range; bf16 blocks walk it in
+// slabs of 64 tokens, of which they form dX and add to their part of dWr at once: the
+// slab's dlogits are read and taken apart once for both.
 //
 // bf16.  dlogits are fp32, the other operand is bf16: an fp32 value is the sum of
 // three bf16 (high, middle, low: 8 bits each), whose products with a bf16 are exact
@@ -385,6 +385,7 @@ __device__ __forceinline__ int tile_column(int m) { return 16 * ((m >> 2) & 1) +
 
 constexpr int RB_SLAB = 64;     // tokens
 constexpr int RB_SPLITS = 32;   // most parts of the token range
+constexpr int RB_PAD = 320;     // floats between them
 
 struct RouterBwd {
   const float* dl;
@@ -392,7 +393,8 @@ struct RouterBwd {
   int Tn, d, E;
   void* dX;
   int acc_dx;
-  float *part, *partb;   // [splits][E][d], [splits][E], or NULL
+  float *part, *partb;   // [splits][E][d], stride apart, and [splits][E], or NULL
+  long stride;
   int span;              // tokens per split, a multiple of RB_SLAB
 };
 
@@ -429,38 +431,52 @@ __device__ __forceinline__ void split3(f32x4_t v, u32x2_t (&p)[3]) {
   }
 }
 
-// NT = expert tiles of 32.
-template <int NT> __global__ __launch_bounds__(256, NT <= 4 ? 2 : 1) void k_router_bf16(RouterBwd a) {
-  constexpr int BLK = RB_SLAB * 64;   // bytes of a block [64 tokens][32 bf16]
-  __shared__ __align__(16) char lds_[2 * 4 * BLK + 3 * NT * BLK];
+// NT = expert tiles of 32.  8 waves: wave w takes columns 32 CB (w % 4) + [0, 32 CB)
+// and tokens 32 (w / 4) + [0, 32) of each slab; the two halves of dWr meet in LDS at
+// the end.  CB = 2 where the sums fit the registers: a plane's fragment then serves
+// two MFMAs.
+template <int NT> struct RouterTile {
+  static constexpr int CB = NT <= 2 ? 2 : 1, COLS = 128 * CB;
+  static constexpr int X_BYTES = CB * 32 * 64;         // a wave's part of a slab, [CB][32 tokens][32 columns]
+  static constexpr int BLK = RB_SLAB * 64;             // a plane's [64 tokens][32 experts]
+  static constexpr int LDS = 2 * 8 * X_BYTES + 3 * NT * BLK;
+  static_assert(LDS <= 160 * 1024 && 4 * NT * CB * 4096 <= LDS, "slab, and half of the sums");
+};
+template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(RouterBwd a) {
+  typedef RouterTile<NT> C;
+  constexpr int CB = C::CB, BLK = C::BLK;
+  __shared__ __align__(16) char lds_[C::LDS];
   FM_LDS char* const xs = (FM_LDS char*)lds_;
-  FM_LDS char* const pl = xs + 2 * 4 * BLK;
-  const int lane = lane_id(), wave = wave_id(), m = lane & 31, h = lane >> 5;
-  const int ct = (a.d + 127) / 128, split = blockIdx.x / ct;
-  const int c0 = (blockIdx.x % ct) * 128 + wave * 32;
+  FM_LDS char* const pl = xs + 2 * 8 * C::X_BYTES;
+  const int lane = lane_id(), wave = wave_id(), m = lane & 31, h = lane >> 5, th = wave >> 2;
+  const int ct = (a.d + C::COLS - 1) / C::COLS, split = blockIdx.x / ct;
+  const int c0 = (blockIdx.x % ct) * C::COLS + (wave & 3) * 32 * CB;
   const int t0 = split * a.span, t1 = min(t0 + a.span, a.Tn);
   const bool on = c0 < a.d, dw = a.part && on, dx = a.dX && on;
   const bool bias = a.partb && blockIdx.x % ct == 0;
   const bf16* const X = (const bf16*)a.X;
 
-  // X: this wave's columns, 16 tokens per instruction; columns past d repeat the last
-  const int xc = min(c0 + 8 * (lane & 3), a.d - 8);
+  // X: this wave's columns and tokens, 16 tokens of a column block per instruction;
+  // columns past d repeat the last
   auto load_x = [&](int t, int buf) {
     if (!dw) return;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int r = min(t + 16 * u + (lane >> 2), t1 - 1);   // a row past the end meets zero dlogits
-      dma16(X + (size_t)r * a.d + xc, xs + (buf * 4 + wave) * BLK + u * 1024);
-    }
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        const int r = min(t + 32 * th + 16 * u + (lane >> 2), t1 - 1);   // a row past the end meets zero dlogits
+        const int c = min(c0 + 32 * cb + 8 * (lane & 3), a.d - 8);
+        dma16(X + (size_t)r * a.d + c, xs + (buf * 8 + wave) * C::X_BYTES + cb * 2048 + u * 1024);
+      }
   };
   // dlogits: thread q of the slab's quads, 4 experts of token q / (8 NT)
-  constexpr int QT = 8 * NT, QN = RB_SLAB * QT / 256;
+  constexpr int QT = 8 * NT, QN = RB_SLAB * QT / 512;
   const int quad = threadIdx.x % QT, e0 = 4 * quad;
   f32x4_t dl[QN], bsum = {0.f, 0.f, 0.f, 0.f};
   auto load_dl = [&](int t) {
 #pragma unroll
     for (int i = 0; i < QN; ++i) {
-      const int r = t + threadIdx.x / QT + i * (256 / QT);
+      const int r = t + threadIdx.x / QT + i * (512 / QT);
       const FM_GLOBAL float* const p = gptr(a.dl) + (size_t)min(r, t1 - 1) * a.E;
       if (a.E % 4 == 0) {   // whole quads, 16-byte aligned
         dl[i] = *(const FM_GLOBAL f32x4_t*)(p + min(e0, a.E - 4));
@@ -474,32 +490,38 @@ template <int NT> __global__ __launch_bounds__(256, NT <= 4 ? 2 : 1) void k_rout
       }
     }
   };
-  // Wr: lane m's column, experts 16 s + 8 h + [0, 8)
-  bf16x8_t wf[2 * NT];
+  load_x(t0, 0);
+  load_dl(t0);
+  // Wr: lane m's columns, experts 16 s + 8 h + [0, 8)
+  bf16x8_t wf[CB][2 * NT];
   if (dx) {
-    const FM_GLOBAL uint16_t* const Wr = (const FM_GLOBAL uint16_t*)a.Wr + min(c0 + tile_column(m), a.d - 1);
 #pragma unroll
-    for (int s = 0; s < 2 * NT; ++s) {
-      uint32_t v[8];
+    for (int cb = 0; cb < CB; ++cb) {
+      const FM_GLOBAL uint16_t* const Wr = (const FM_GLOBAL uint16_t*)a.Wr + min(c0 + 32 * cb + tile_column(m), a.d - 1);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int e = 16 * s + 8 * h + i;
-        v[i] = Wr[(size_t)min(e, a.E - 1) * a.d];
-        if (e >= a.E) v[i] = 0;
+      for (int s = 0; s < 2 * NT; ++s) {
+        uint32_t v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int e = 16 * s + 8 * h + i;
+          v[i] = Wr[(size_t)min(e, a.E - 1) * a.d];
+          if (e >= a.E) v[i] = 0;
+        }
+        wf[cb][s] = __builtin_bit_cast(bf16x8_t, u32x4_t{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16});
       }
-      wf[s] = __builtin_bit_cast(bf16x8_t, u32x4_t{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16});
     }
   }
-  f32x16_t acc[NT];
+  f32x16_t acc[NT][CB];
 #pragma unroll
   for (int j = 0; j < NT; ++j)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[j][cb][i] = 0.f;
   B16Frag<false, 32, 1> fr;
   fr.init(0);
   // as fr, for the swizzled planes: rows 8 (lane / 32) + [0, 4) and + [4, 8) of a step
-  const int sw = 2 * h;
-  const uint32_t f0 = (fr.off[0] & ~48u) | (((fr.off[0] >> 4) & 3) ^ sw) << 4, f1 = f0 ^ 16;
+  const uint32_t f0 = fr.off[0] ^ (uint32_t)(2 * h) << 4, f1 = f0 ^ 16;
   auto read_pl = [&](const FM_LDS char* blk, int ks) {
     const FM_LDS char* const p = blk + ks * 1024;
     const u32x2_t w0 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((FM_LDS i16x4_t*)(p + f0)));
@@ -507,8 +529,6 @@ template <int NT> __global__ __launch_bounds__(256, NT <= 4 ? 2 : 1) void k_rout
     return __builtin_bit_cast(bf16x8_t, u32x4_t{w0[0], w0[1], w1[0], w1[1]});
   };
 
-  load_x(t0, 0);
-  load_dl(t0);
   int buf = 0;
   for (int t = t0; t < t1; t += RB_SLAB, buf ^= 1) {
     wait_vmcnt<0>();
@@ -517,7 +537,7 @@ template <int NT> __global__ __launch_bounds__(256, NT <= 4 ? 2 : 1) void k_rout
     for (int i = 0; i < QN; ++i) {
       u32x2_t p[3];
       split3(dl[i], p);
-      const int r = threadIdx.x / QT + i * (256 / QT);
+      const int r = threadIdx.x / QT + i * (512 / QT);
 #pragma unroll
       for (int k = 0; k < 3; ++k)
         *(FM_LDS u32x2_t*)(pl + (k * NT + (quad >> 3)) * BLK + r * 64 + ((((quad & 7) >> 1) ^ ((r >> 2) & 3)) << 4) + (quad & 1) * 8) = p[k];
@@ -530,42 +550,74 @@ template <int NT> __global__ __launch_bounds__(256, NT <= 4 ? 2 : 1) void k_rout
     }
     if (dw) {
 #pragma unroll
-      for (int ks = 0; ks < RB_SLAB / 16; ++ks) {
-        const bf16x8_t x = fr.read(xs + (buf * 4 + wave) * BLK, 0, ks);
+      for (int ks = 0; ks < 2; ++ks) {
+        bf16x8_t x[CB];
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) x[cb] = fr.read(xs + (buf * 8 + wave) * C::X_BYTES + cb * 2048, 0, ks);
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-          for (int k = 0; k < 3; ++k)
-            acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_pl(pl + (k * NT + j) * BLK, ks), x, acc[j], 0, 0, 0);
+          for (int k = 0; k < 3; ++k) {
+            const bf16x8_t v = read_pl(pl + (k * NT + j) * BLK, 2 * th + ks);
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) acc[j][cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, x[cb], acc[j][cb], 0, 0, 0);
+          }
       }
     }
     if (dx) {
+      f32x16_t o[CB];
 #pragma unroll
-      for (int tb = 0; tb < RB_SLAB / 32; ++tb) {
-        f32x16_t o;
+      for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[i] = 0.f;
+        for (int i = 0; i < 16; ++i) o[cb][i] = 0.f;
 #pragma unroll
-        for (int s = 0; s < 2 * NT; ++s)
+      for (int s = 0; s < 2 * NT; ++s)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const FM_LDS char* const p = pl + (k * NT + (s >> 1)) * BLK + (32 * tb + m) * 64 +
-                                     (((2 * (s & 1) + h) ^ ((m >> 2) & 3)) << 4);
-            o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[s], __builtin_bit_cast(bf16x8_t, *(const FM_LDS u32x4_t*)p), o, 0, 0, 0);
-          }
-        const int r = t + 32 * tb + m, c = c0 + 16 * h;
-        if (r < t1) put_dx((bf16*)a.dX + (size_t)r * a.d + c, a.d - c, a.acc_dx, o);
+        for (int k = 0; k < 2; ++k) {
+          const FM_LDS char* const p = pl + (k * NT + (s >> 1)) * BLK + (32 * th + m) * 64 +
+                                       (((2 * (s & 1) + h) ^ ((m >> 2) & 3)) << 4);
+          const bf16x8_t v = __builtin_bit_cast(bf16x8_t, *(const FM_LDS u32x4_t*)p);
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[cb][s], v, o[cb], 0, 0, 0);
+        }
+      const int r = t + 32 * th + m;
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        const int c = c0 + 32 * cb + 16 * h;
+        if (r < t1) put_dx((bf16*)a.dX + (size_t)r * a.d + c, a.d - c, a.acc_dx, o[cb]);
       }
     }
   }
-  if (dw) {
+  if (a.part) {   // the tokens' halves add up through LDS: [wave % 4][tile][quad][lane]
+    __syncthreads();
+    auto at = [&](int j, int cb, int q) {
+      return (FM_LDS f32x4_t*)(xs + ((((wave & 3) * NT + j) * CB + cb) * 4 + q) * 1024 + lane * 16);
+    };
+    if (th == 1) {
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+      for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int e = 32 * j + 8 * (i >> 2) + 4 * h + (i & 3);
-        if (e < a.E && c0 + m < a.d) gptr(a.part)[((size_t)split * a.E + e) * a.d + c0 + m] = acc[j][i];
-      }
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            *at(j, cb, q) = f32x4_t{acc[j][cb][4 * q], acc[j][cb][4 * q + 1], acc[j][cb][4 * q + 2], acc[j][cb][4 * q + 3]};
+    }
+    __syncthreads();
+    if (th == 0 && dw) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x4_t v = *at(j, cb, q);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int e = 32 * j + 8 * q + 4 * h + i, c = c0 + 32 * cb + m;
+              if (e < a.E && c < a.d) gptr(a.part)[(size_t)split * a.stride + (size_t)e * a.d + c] = acc[j][cb][4 * q + i] + v[i];
+            }
+          }
+    }
   }
   if (bias) {   // the block's threads with the same experts, in order
     __syncthreads();
@@ -573,7 +625,7 @@ template <int NT> __global__ __launch_bounds__(256, NT <= 4 ? 2 : 1) void k_rout
     b4[threadIdx.x] = bsum;
     __syncthreads();
     if (threadIdx.x < QT) {
-      for (int g = 1; g < 256 / QT; ++g) bsum += b4[threadIdx.x + g * QT];
+      for (int g = 1; g < 512 / QT; ++g) bsum += b4[threadIdx.x + g * QT];
 #pragma unroll
       for (int x = 0; x < 4; ++x)
         if (e0 + x < a.E) gptr(a.partb)[(size_t)split * a.E + e0 + x] = bsum[x];
@@ -630,7 +682,7 @@ template <int NT> __global__ __launch_bounds__(256) void k_router_f32(RouterBwd 
         if (h == 0) gptr(a.partb)[(size_t)split * a.E + e] = s;
       }
       if (a.part) {
-        float* o = a.part + ((size_t)split * a.E + e) * a.d + c0 + 16 * h;
+        float* o = a.part + (size_t)split * a.stride + (size_t)e * a.d + c0 + 16 * h;
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
           if (c0 + 16 * h + i < a.d) store4(o + i, f32x4_t{acc[j][i], acc[j][i + 1], acc[j][i + 2], acc[j][i + 3]});
@@ -672,7 +724,8 @@ template <int NT> __global__ __launch_bounds__(256) void k_router_f32(RouterBwd 
 // dWr and dbias from their parts: a block takes 64 quads of columns, its 4 groups of
 // threads every fourth part, and the groups' sums are added in order.
 __global__ __launch_bounds__(256) void k_router_dw(const float* __restrict__ part, const float* __restrict__ partb,
-                                                   int splits, long n, int E, int accumulate, float* __restrict__ dWr,
+                                                   int splits, long stride, long n, int E, int accumulate,
+                                                   float* __restrict__ dWr,
                                                    float* __restrict__ dbias) {
   __shared__ f32x4_t red[4][64];
   const int q = threadIdx.x & 63, g = threadIdx.x >> 6;
@@ -681,7 +734,7 @@ __global__ __launch_bounds__(256) void k_router_dw(const float* __restrict__ par
     f32x4_t v = {0.f, 0.f, 0.f, 0.f};
     if (i < n) {
 #pragma unroll 8
-      for (int p = g; p < splits; p += 4) v += load4(part + (size_t)p * n + i);
+      for (int p = g; p < splits; p += 4) v += load4(part + (size_t)p * stride + i);
     }
     red[g][q] = v;
     __syncthreads();
@@ -698,20 +751,26 @@ __global__ __launch_bounds__(256) void k_router_dw(const float* __restrict__ par
   }
 }
 
-// Parts of the token range: two blocks per compute unit, whole slabs in each.
-inline int router_splits(int T, int d) {
-  const int ct = cdiv(d, 128), slabs = cdiv(T, RB_SLAB);
-  int s = cdiv(512, ct);
+// Columns of a block.
+inline int router_cols(int E, bool is_bf16) { return is_bf16 && E <= 64 ? 256 : 128; }
+// Parts of the token range: blocks of 8 waves for every compute unit (bf16; fp32: two
+// of 4 waves), whole slabs in each.
+inline int router_splits(int T, int d, int E, bool is_bf16) {
+  const int slabs = cdiv(T, RB_SLAB);
+  int s = cdiv(is_bf16 ? 256 : 512, cdiv(d, router_cols(E, is_bf16)));
   if (s > RB_SPLITS) s = RB_SPLITS;
   return slabs < s ? slabs : s;
 }
+// Floats between two parts: not a power of two, which would put the same place of all
+// parts on one memory channel.
+inline long router_stride(int d, int E) { return (long)E * d + RB_PAD; }
 
-void launch_router_bwd(const RouterBwd& a, bool is_bf16, int blocks, hipStream_t st) {
-  const dim3 g(blocks), b(256);
+void launch_router_bwd(const RouterBwd& a, bool is_bf16, int splits, hipStream_t st) {
+  const dim3 g(splits * cdiv(a.d, router_cols(a.E, is_bf16)));
   auto run = [&](auto nt) {
     constexpr int NT = decltype(nt)::value;
-    if (is_bf16) hipLaunchKernelGGL((k_router_bf16<NT>), g, b, 0, st, a);
-    else hipLaunchKernelGGL((k_router_f32<NT>), g, b, 0, st, a);
+    if (is_bf16) hipLaunchKernelGGL((k_router_bf16<NT>), g, dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((k_router_f32<NT>), g, dim3(256), 0, st, a);
   };
   if (a.E <= 32) run(std::integral_constant<int, 1>{});
   else if (a.E <= 64) run(std::integral_constant<int, 2>{});
@@ -792,7 +851,8 @@ extern "C" int moe_balance_loss_bwd(const float* logits, const float* dprob, con
 
 extern "C" size_t moe_router_bwd_workspace_size(int T, int d, int E) {
   if (T < 0 || d <= 0 || E <= 0) return 0;
-  return (size_t)router_splits(T, d) * E * ((size_t)d + 1) * sizeof(float);
+  const int a = router_splits(T, d, E, true), b = router_splits(T, d, E, false);   // for either type
+  return (size_t)(a > b ? a : b) * (router_stride(d, E) + E) * sizeof(float);
 }
 
 extern "C" int moe_router_bwd(const float* dlogits, const void* X, const void* Wr, int dtype, int T, int d, int E,
@@ -820,22 +880,24 @@ extern "C" int moe_router_bwd(const float* dlogits, const void* X, const void* W
   }
   if (T == 0 && (!dw || accumulate_dw)) return MOE_OK;
   hipStream_t st = as_stream(stream);
-  const int splits = T > 0 ? router_splits(T, d) : 0;
+  const bool is_bf16 = dtype == MOE_BF16;
+  const int splits = T > 0 ? router_splits(T, d, E, is_bf16) : 0;
   RouterBwd a{};
   a.dl = dlogits; a.X = dWr ? X : nullptr; a.Wr = Wr;
   a.Tn = T; a.d = d; a.E = E;
   a.dX = dX; a.acc_dx = accumulate_dx;
   a.part = dWr ? (float*)ws : nullptr;
-  a.partb = dbias ? (float*)ws + (size_t)splits * E * d : nullptr;
+  a.stride = router_stride(d, E);
+  a.partb = dbias ? (float*)ws + (size_t)splits * a.stride : nullptr;
   if (T > 0) {
     a.span = cdiv(cdiv(T, splits), RB_SLAB) * RB_SLAB;
-    launch_router_bwd(a, dtype == MOE_BF16, splits * cdiv(d, 128), st);
+    launch_router_bwd(a, is_bf16, splits, st);
     FM_TRY(check_launch("moe_router_bwd"));
   }
   if (dw) {
     const long n = (long)E * d;
-    hipLaunchKernelGGL(k_router_dw, dim3(dWr ? cdiv(n, 256) : 1), dim3(256), 0, st, a.part, a.partb, splits, n, E,
-                       accumulate_dw, dWr, dbias);
+    hipLaunchKernelGGL(k_router_dw, dim3(dWr ? cdiv(n, 256) : 1), dim3(256), 0, st, a.part, a.partb, splits, a.stride,
+                       n, E, accumulate_dw, dWr, dbias);
     FM_TRY(check_launch("moe_router_bwd"));
   }
   return MOE_OK;
