@@ -51,13 +51,8 @@ __device__ __forceinline__ uint32_t mx_codes8(const float* v, float s) {
 
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
-// Columns [128 blk, 128 blk + 128) of a row by 16 lanes (q: lane within them), 8
-// columns each; codes are written up to column code_cols (0 past cols).
-template <typename T>
-__device__ __forceinline__ void quantize128(const T* row, int cols, int blk, int q, int code_cols, uint8_t* codes,
-                                            uint8_t* scale) {
-  const int c = blk * 128 + q * 8;
-  float v[8];
+// 8 columns from c of a row (0 past cols).
+template <typename T> __device__ __forceinline__ void load8(const T* row, int c, int cols, float (&v)[8]) {
   if (c < cols) {
     unpack16(ld16(row + c), v, (T*)nullptr);
     if constexpr (sizeof(T) == 4) unpack16(ld16(row + c + 4), v + 4, (T*)nullptr);
@@ -65,17 +60,34 @@ __device__ __forceinline__ void quantize128(const T* row, int cols, int blk, int
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = 0.f;
   }
+}
+
+// 128 columns of a row in 16 lanes, 8 each (q: lane within them): this lane's codes, and
+// the four blocks' scale bytes in every lane.
+__device__ __forceinline__ uint32_t quantize128(const float (&v)[8], int q, uint32_t& scales) {
   uint32_t top = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) top = max(top, abs_bits(v[i]));
   top = max(top, (uint32_t)__shfl_xor((int)top, 1));
   top = max(top, (uint32_t)__shfl_xor((int)top, 2));
   const uint32_t byte = mx_byte(top);
-  const uint32_t code = byte == 255 ? 0u : mx_codes8(v, mx_inv(byte));
-  if (c < code_cols) *(FM_GLOBAL uint32_t*)(codes + c / 2) = code;
   uint32_t s = byte << (8 * (q >> 2));
   s |= (uint32_t)__shfl_xor((int)s, 4);
   s |= (uint32_t)__shfl_xor((int)s, 8);
+  scales = s;
+  return byte == 255 ? 0u : mx_codes8(v, mx_inv(byte));
+}
+
+// Columns [128 blk, 128 blk + 128) of a row to memory; codes up to column code_cols.
+template <typename T>
+__device__ __forceinline__ void quantize_row(const T* row, int cols, int blk, int q, int code_cols, uint8_t* codes,
+                                             uint8_t* scale) {
+  const int c = blk * 128 + q * 8;
+  float v[8];
+  load8(row, c, cols, v);
+  uint32_t s;
+  const uint32_t code = quantize128(v, q, s);
+  if (c < code_cols) *(FM_GLOBAL uint32_t*)(codes + c / 2) = code;
   if (q == 0) *(FM_GLOBAL uint32_t*)(scale + blk * 4) = s;
 }
 
@@ -85,7 +97,7 @@ __global__ __launch_bounds__(256) void k_quantize_mx(const T* __restrict__ W, ui
   const uint32_t item = blockIdx.x * 16 + threadIdx.x / 16;
   if (item >= items) return;
   const uint32_t r = item / nb;
-  quantize128(W + (size_t)r * cols, cols, (int)(item - r * nb), threadIdx.x % 16, up32(cols),
+  quantize_row(W + (size_t)r * cols, cols, (int)(item - r * nb), threadIdx.x % 16, up32(cols),
               codes + (size_t)r * (up32(cols) / 2), scale + (size_t)r * nb * 4);
 }
 
@@ -126,10 +138,13 @@ struct MxPtrs {
   const uint8_t* const* sd;
 };
 
+constexpr int MX_FEW = 16;   // tokens of a call that takes the kernels for few
+
 // Workspace: row-tile prefix, X and H as packed rows of whole 128-blocks.
 struct MxWs {
   int32_t* mbase;
   uint8_t *xq, *xs, *hq, *hs;
+  float* hf;   // H of a call of few tokens, [rows][I]
 };
 inline size_t round256(size_t b) { return (b + 255) / 256 * 256; }
 inline MxWs mx_ws_at(void* ws, const moe_layer_mx4* L, int T, int k, size_t* bytes) {
@@ -147,6 +162,7 @@ inline MxWs mx_ws_at(void* ws, const moe_layer_mx4* L, int T, int k, size_t* byt
   w.xs = (uint8_t*)take((size_t)T * nd * 4);
   w.hq = (uint8_t*)take(R * nI * 64);
   w.hs = (uint8_t*)take(R * nI * 4);
+  w.hf = (float*)take((size_t)(T < MX_FEW ? T : MX_FEW) * (k + L->S_shared) * L->I * 4);
   *bytes = (size_t)(p - (char*)ws);
   return w;
 }
@@ -230,7 +246,7 @@ __global__ __launch_bounds__(256) void k_mx_prep(const bf16* __restrict__ X, Row
   const uint32_t item = blockIdx.x * 16 + threadIdx.x / 16;   // below 2^25: T up128(d) <= 2^32
   if (item >= (uint32_t)ra.Tn * nb) return;
   const uint32_t r = item / nb;
-  quantize128(X + (size_t)r * ra.d, ra.d, (int)(item - r * nb), threadIdx.x % 16, nb * 128, xq + (size_t)r * nb * 64,
+  quantize_row(X + (size_t)r * ra.d, ra.d, (int)(item - r * nb), threadIdx.x % 16, nb * 128, xq + (size_t)r * nb * 64,
               xs + (size_t)r * nb * 4);
 }
 
@@ -522,7 +538,216 @@ template <class C> __global__ __launch_bounds__(256, C::BPC) void k_mx_down(MxAr
   }
 }
 
+// --------------------------------------------------------- a few tokens ----
+// Calls of a few tokens are bound by latency and by the weights' bytes, which have to be
+// spread over all compute units: a block takes 8 columns of H (8 gate and 8 up rows, one
+// fragment of v_mfma_scale_f32_16x16x128_f8f6f4: lane l row l % 16, k block l / 16), or
+// 32 of O, of one slot, and its NW waves split k into consecutive parts whose sums meet
+// in LDS.  No ring: a wave requests BS steps of weights straight into registers, and the
+// block quantises its activation rows into LDS while they are on their way (a launch
+// before, for the activations alone, costs some 3 us; a lane that quantised the 32
+// activations of its own row and k block repeated it for 16 rows, mostly empty ones, and
+// was bound by vector instructions).  H goes through the workspace in fp32 and is
+// quantised the same way.  Rows come 16 at a time.  Blocks exist for the slots that may
+// hold rows only: the i-th of them is found by a ballot over the offsets.
+
+// The i-th slot with rows (s = -1: there is none), and its rows.
+__device__ __forceinline__ int mx_active_slot(const RowArgs& ra, int i, SlotRows& sr) {
+  int before = 0;
+  for (int b = 0; b < ra.S; b += 64) {
+    const int s = b + lane_id(), sc = max(min(s, ra.S_r - 1), 0);
+    int lo = 0, hi = 0;
+    if (ra.S_r > 0) lo = gptr(ra.offsets)[sc], hi = gptr(ra.offsets)[sc + 1];
+    unsigned long long m = __ballot(s < ra.S && (s >= ra.S_r || hi > lo));
+    const int n = __builtin_popcountll(m);
+    if (i < before + n) {
+      for (int drop = i - before; drop > 0; --drop) m &= m - 1;
+      const int at = __builtin_amdgcn_readfirstlane(__builtin_ctzll(m)), sl = b + at;
+      sr.shared = sl >= ra.S_r;
+      const int first = __builtin_amdgcn_readlane(lo, at);
+      sr.nrows = sr.shared ? ra.Tn : __builtin_amdgcn_readlane(hi, at) - first;
+      sr.xrow0 = sr.shared ? 0 : first;
+      sr.orow0 = sr.shared ? (long)ra.Tn * ra.k + (long)(sl - ra.S_r) * ra.Tn : first;
+      return sl;
+    }
+    before += n;
+  }
+  return -1;
+}
+
+// Rows of nb 128-blocks in LDS: codes, then scales; padded so that 16 rows' chunks at
+// one place lie on different banks.
+struct MxFewRows {
+  FM_LDS char* codes;
+  FM_LDS char* scale;
+  int ld, lds;
+};
+__host__ __device__ constexpr int mx_few_row_bytes(int nb) { return nb * 64 + 16 + nb * 4 + 4; }
+__device__ __forceinline__ MxFewRows mx_few_rows(FM_LDS char* at, int nb, int rows) {
+  return MxFewRows{at, at + rows * (nb * 64 + 16), nb * 64 + 16, nb * 4 + 4};
+}
+
+// The block's n rows (row(r): pointer) of cols columns, quantised into LDS.
+template <int THREADS, typename Row>
+__device__ __forceinline__ void mx_few_stage(const MxFewRows& l, int n, int nb, int cols, Row row) {
+  for (int item = threadIdx.x / 16; item < n * nb; item += THREADS / 16) {
+    const int r = item / nb, blk = item - r * nb, q = threadIdx.x % 16;
+    float v[8];
+    load8(row(r), blk * 128 + q * 8, cols, v);
+    uint32_t s;
+    const uint32_t code = quantize128(v, q, s);
+    *(FM_LDS uint32_t*)(l.codes + r * l.ld + blk * 64 + q * 4) = code;
+    if (q == 0) *(FM_LDS uint32_t*)(l.scale + r * l.lds + blk * 4) = s;
+  }
+}
+
+// Sums over this wave's steps [k0, k1) of 128 k: NF fragments of 16 weight rows (codes
+// at w[f], scales at s[f], both of this lane's row) by the 16 activation rows that
+// stage() puts into LDS (n of them are there).
+template <int NF, int BS, typename Stage>
+__device__ __forceinline__ void mx_few_sums(const uint8_t* const (&w)[NF], const uint8_t* const (&s)[NF], int kw,
+                                            const MxFewRows& l, int n, int k0, int k1, Stage stage,
+                                            f32x4_t (&acc)[NF]) {
+  const int kb = lane_id() >> 4, r = min(lane_id() & 15, n - 1);
+  u32x4_t wc[BS][NF];
+  uint32_t ws[BS][NF];
+  auto load = [&](int k) {
+#pragma unroll
+    for (int u = 0; u < BS; ++u) {
+      if (k + u >= k1) break;
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
+        wc[u][f] = ld16(w[f] + 16 * min(4 * (k + u) + kb, kw - 1));   // a chunk behind the row meets zero activations
+        ws[u][f] = *(const FM_GLOBAL uint32_t*)(s[f] + 4 * (k + u));
+      }
+    }
+  };
+  auto wide = [](const u32x4_t& v) { return i32x8_t{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; };
+  load(k0);
+  stage();
+  __syncthreads();
+  for (int k = k0; k < k1; k += BS) {
+    if (k > k0) load(k);
+#pragma unroll
+    for (int u = 0; u < BS; ++u) {
+      if (k + u >= k1) break;
+      const u32x4_t xc = *(const FM_LDS u32x4_t*)(l.codes + r * l.ld + (4 * (k + u) + kb) * 16);
+      const int xb = *(const FM_LDS uint8_t*)(l.scale + r * l.lds + 4 * (k + u) + kb);
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+        acc[f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(wc[u][f]), wide(xc), acc[f], 4, 4, 0,
+                                                                  (int)(ws[u][f] >> (8 * kb)), 0, xb);
+    }
+  }
+}
+
+// The waves' sums through LDS: [wave][f][lane] quads; element (row, weight row n) of
+// fragment f is in quad lane 16 (n / 4) + row, component n % 4.
+template <int NF, int NW>
+__device__ __forceinline__ float mx_few_sum(const FM_LDS f32x4_t* red, int f, int row, int n) {
+  const FM_LDS float* const p = (const FM_LDS float*)(red + f * 64 + 16 * (n >> 2) + row) + (n & 3);
+  float v = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) v += p[w * NF * 256];
+  return v;
+}
+
+// This wave's part of n steps.
+template <int NW> __device__ __forceinline__ void mx_few_part(int n, int& k0, int& k1) {
+  const int per = (n + NW - 1) / NW, w = wave_id();
+  k0 = min(w * per, n);
+  k1 = min(k0 + per, n);
+}
+
+extern __shared__ __align__(16) char mx_few_lds[];
+
+template <int NW, int BS>
+__global__ __launch_bounds__(64 * NW) void k_mx_few_gate_up(MxArgs a, const bf16* __restrict__ X, int NT, int max_rows) {
+  FM_LDS f32x4_t* const red = (FM_LDS f32x4_t*)mx_few_lds;
+  const RowArgs& ra = a.ra;
+  SlotRows sr;
+  const int sl = mx_active_slot(ra, blockIdx.x / NT, sr);
+  if (sl < 0) return;
+  const int n0 = (blockIdx.x % NT) * 8, I = ra.I, kd = up128(ra.d) / 128;
+  const int lane = lane_id(), r16 = lane & 15;
+  const MxFewRows l = mx_few_rows((FM_LDS char*)mx_few_lds + NW * 1024, kd, max_rows);
+  // weight rows: 8 of gate, 8 of up (I % 8 == 0)
+  const size_t wr = n0 + (r16 & 7);
+  const uint8_t* const w[1] = {(r16 < 8 ? ld_scalar(a.W.qg + sl) : ld_scalar(a.W.qu + sl)) + wr * (up32(ra.d) / 2)};
+  const uint8_t* const s[1] = {(r16 < 8 ? ld_scalar(a.W.sg + sl) : ld_scalar(a.W.su + sl)) + wr * kd * 4};
+  int k0, k1;
+  mx_few_part<NW>(kd, k0, k1);
+  for (int m0 = 0; m0 < sr.nrows; m0 += max_rows) {
+    const int n = min(max_rows, sr.nrows - m0);
+    f32x4_t acc[1] = {{0.f, 0.f, 0.f, 0.f}};
+    mx_few_sums<1, BS>(w, s, up32(ra.d) / 32, l, n, k0, k1, [&] {
+      mx_few_stage<64 * NW>(l, n, kd, ra.d, [&](int r) {
+        const size_t tok = sr.shared ? m0 + r : min(max(gptr(a.perm_token)[sr.xrow0 + m0 + r], 0), ra.Tn - 1);
+        return X + tok * ra.d;
+      });
+    }, acc);
+    red[wave_id() * 64 + lane] = acc[0];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 8 * n; i += 64 * NW) {
+      const int row = i >> 3, c = i & 7;
+      const float g = mx_few_sum<1, NW>(red, 0, row, c), u = mx_few_sum<1, NW>(red, 0, row, 8 + c);
+      gptr(a.w.hf)[(size_t)(sr.orow0 + m0 + row) * I + n0 + c] = g * sigm_fast(g) * u;
+    }
+    __syncthreads();   // red and the rows are read
+  }
+}
+
+template <int NW, int BS>
+__global__ __launch_bounds__(64 * NW) void k_mx_few_down(MxArgs a, int NT, int max_rows) {
+  FM_LDS f32x4_t* const red = (FM_LDS f32x4_t*)mx_few_lds;
+  const RowArgs& ra = a.ra;
+  SlotRows sr;
+  const int sl = mx_active_slot(ra, blockIdx.x / NT, sr);
+  if (sl < 0) return;
+  const int n0 = (blockIdx.x % NT) * 32, d = ra.d, nI = up128(ra.I) / 128;
+  const int lane = lane_id(), r16 = lane & 15;
+  const MxFewRows l = mx_few_rows((FM_LDS char*)mx_few_lds + NW * 2048, nI, max_rows);
+  const uint8_t *w[2], *s[2];
+#pragma unroll
+  for (int f = 0; f < 2; ++f) {
+    const size_t r = min(n0 + 16 * f + r16, d - 1);
+    w[f] = ld_scalar(a.W.qd + sl) + r * (up32(ra.I) / 2);
+    s[f] = ld_scalar(a.W.sd + sl) + r * nI * 4;
+  }
+  int k0, k1;
+  mx_few_part<NW>(nI, k0, k1);
+  for (int m0 = 0; m0 < sr.nrows; m0 += max_rows) {
+    const int n = min(max_rows, sr.nrows - m0);
+    const size_t row0 = (size_t)(sr.orow0 + m0);
+    f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    mx_few_sums<2, BS>(w, s, up32(ra.I) / 32, l, n, k0, k1, [&] {
+      mx_few_stage<64 * NW>(l, n, nI, ra.I, [&](int r) { return (const float*)a.w.hf + (row0 + r) * ra.I; });
+    }, acc);
+#pragma unroll
+    for (int f = 0; f < 2; ++f) red[(wave_id() * 2 + f) * 64 + lane] = acc[f];
+    __syncthreads();
+    // 16 lanes per row, two columns each
+    for (int r = threadIdx.x >> 4; r < n; r += 4 * NW) {
+      const int c = (threadIdx.x & 15) * 2;
+      if (n0 + c >= d) break;
+      const float v0 = mx_few_sum<2, NW>(red, c >> 4, r, c & 15), v1 = mx_few_sum<2, NW>(red, c >> 4, r, (c & 15) + 1);
+      *(FM_GLOBAL uint32_t*)((uint16_t*)a.O + (row0 + r) * d + n0 + c) = pk_bf16(v0, v1);
+    }
+    __syncthreads();   // red and the rows are read
+  }
+}
+
 using M128 = MxCfg<128, 256, 2, 2, 3, 2>;
+
+// Whether a call takes the kernels for a few tokens.  us there and on the tiles: one
+// token, d = 4096, I = 688, 4 of 16 slots 13 and 37; d = 2048, I = 1408, 6 of 64 and 2
+// shared 19 and 30; 4 tokens of that layer (26 slots, 4576 blocks) 32 and 33, 16 tokens
+// (66 slots, 11616) 70 and 53; 16 tokens of the first 37 and 40; 16 tokens, d = 512, I =
+// 256, 8 slots 10 and 18.  A block's rows have to fit the LDS.
+bool mx_few_tokens(const moe_layer_mx4* L, int T, long active) {
+  return T <= MX_FEW && active * (L->I / 8) <= 4096 && T * mx_few_row_bytes(up128(L->d) / 128) <= 56 * 1024 &&
+         T * mx_few_row_bytes(up128(L->I) / 128) <= 52 * 1024;
+}
 
 template <class C> dim3 mx_grid(const RowArgs& ra, int NT) {
   const long long R = (long long)ra.Tn * ra.k;
@@ -633,10 +858,24 @@ extern "C" int moe_grouped_swiglu_fwd_mx4(const moe_layer_mx4* L, const void* X,
   }
   const RowArgs ra{offsets, w.mbase, L->S_routed, L->S_routed + L->S_shared, T, k, L->d, L->I, L->I};
   const MxArgs a{{L->q_gate, L->q_up, L->q_down, L->s_gate, L->s_up, L->s_down}, w, perm_token, ra, (bf16*)O};
-  typedef M128 C;
   const int nb = up128(L->d) / 128;
-  hipLaunchKernelGGL(k_mx_prep, dim3(cdiv((long)T * nb, 16) + 1), dim3(256), 0, st, (const bf16*)X, ra, C::RA, nb, w.xq,
-                     w.xs, w.mbase);
+  const bf16* const Xb = (const bf16*)X;
+  auto prep = [&](int tile_rows) {
+    hipLaunchKernelGGL(k_mx_prep, dim3(cdiv((long)T * nb, 16) + 1), dim3(256), 0, st, Xb, ra, tile_rows, nb, w.xq, w.xs,
+                       w.mbase);
+  };
+  const long R = (long)T * k;
+  const long active = (R < L->S_routed ? R : L->S_routed) + L->S_shared;   // slots that may hold rows
+  if (mx_few_tokens(L, T, active)) {
+    const int ng = L->I / 8, nd = cdiv(L->d, 32);
+    hipLaunchKernelGGL((k_mx_few_gate_up<4, 4>), dim3(active * ng), dim3(256), T * mx_few_row_bytes(nb) + 4 * 1024, st, a,
+                       Xb, ng, T);
+    hipLaunchKernelGGL((k_mx_few_down<4, 2>), dim3(active * nd), dim3(256),
+                       T * mx_few_row_bytes(up128(L->I) / 128) + 4 * 2048, st, a, nd, T);
+    return check_launch("moe_grouped_swiglu_fwd_mx4");
+  }
+  typedef M128 C;
+  prep(C::RA);
   hipLaunchKernelGGL(k_mx_gate_up<C>, mx_grid<C>(ra, up128(L->I) / 128 * (256 / C::RB)), dim3(256), 0, st, a);
   hipLaunchKernelGGL(k_mx_down<C>, mx_grid<C>(ra, cdiv(L->d, C::RB)), dim3(256), 0, st, a);
   return check_launch("moe_grouped_swiglu_fwd_mx4");
