@@ -7,16 +7,22 @@
 // exactly that block, lane l row l % 32 and k block l / 32, so packed rows are
 // MFMA fragments as they lie in memory.
 //
-// * 16 x 64 slabs (128 k of a row) go global -> LDS with global_load_lds_dwordx4
-//   into a ring of NS slabs, the scales beside them (one dword per row and slab);
-//   one block barrier per slab, several blocks per compute unit.
+// * Slabs of 256 k go global -> LDS with global_load_lds_dwordx4, whole 128-byte lines
+//   of 8 rows per instruction, into two buffers; the scales of 512 k of a row (16
+//   bytes) follow through registers.  What bounds such a product is the number of
+//   requests its operands make to L2, not their bytes: with half lines and a scale
+//   dword per row and 128 k (128 x 256 tiles, a ring of three, two blocks per compute
+//   unit) the same products took 2.03 and 1.15 ms at 262144 rows, d = 4096, I = 1024,
+//   and half of that with the loads taken out.
 // * Weights are the first operand, so a lane's 16 sums of a 32 x 32 tile belong to
 //   one activation row; weight rows are dealt to the operand's rows so that they
 //   are 16 consecutive columns (tile_column).  Two lanes then hold a whole
 //   32-block of H: its maximum is 15 comparisons and one exchange, and H is
 //   quantised in registers.
-// * X and H in the workspace have rows of whole 128-blocks, zero behind the row's
-//   end: a slab past K meets zero codes and needs no case of its own.
+// * X and H in the workspace have rows of whole 256-blocks, zero behind the row's
+//   end, so weight chunks past K (clamped reads) meet zero codes.
+#include <type_traits>
+
 #include "debug.hpp"
 #include "ffn_common.hpp"
 #include "gemm_bf16.hpp"
@@ -28,6 +34,8 @@ typedef int i32x8_t __attribute__((ext_vector_type(8)));
 
 __host__ __device__ constexpr int up32(int n) { return (n + 31) / 32 * 32; }
 __host__ __device__ constexpr int up128(int n) { return (n + 127) / 128 * 128; }
+// 128-blocks of an activation row in the workspace: an even number.
+__host__ __device__ constexpr int act_blocks(int n) { return (n + 255) / 256 * 2; }
 
 // Block scale of a largest magnitude, given as the bits of its absolute value:
 // floor(log2) - 2, biased by 127; 255 for infinities and NaN.
@@ -140,7 +148,7 @@ struct MxPtrs {
 
 constexpr int MX_FEW = 16;   // tokens of a call that takes the kernels for few
 
-// Workspace: row-tile prefix, X and H as packed rows of whole 128-blocks.
+// Workspace: row-tile prefix, X and H as packed rows of whole 256-blocks.
 struct MxWs {
   int32_t* mbase;
   uint8_t *xq, *xs, *hq, *hs;
@@ -149,7 +157,7 @@ struct MxWs {
 inline size_t round256(size_t b) { return (b + 255) / 256 * 256; }
 inline MxWs mx_ws_at(void* ws, const moe_layer_mx4* L, int T, int k, size_t* bytes) {
   const size_t S = L->S_routed + L->S_shared, R = (size_t)T * (k + L->S_shared);
-  const size_t nd = up128(L->d) / 128, nI = up128(L->I) / 128;
+  const size_t nd = act_blocks(L->d), nI = act_blocks(L->I);
   MxWs w;
   char* p = (char*)ws;
   auto take = [&](size_t b) {
@@ -243,50 +251,30 @@ __global__ __launch_bounds__(256) void k_mx_prep(const bf16* __restrict__ X, Row
     mx_count_tiles(ra, tile_rows, mbase);
     return;
   }
-  const uint32_t item = blockIdx.x * 16 + threadIdx.x / 16;   // below 2^25: T up128(d) <= 2^32
+  const uint32_t item = blockIdx.x * 16 + threadIdx.x / 16;   // below 2^26: T up128(d) <= 2^32
   if (item >= (uint32_t)ra.Tn * nb) return;
   const uint32_t r = item / nb;
   quantize_row(X + (size_t)r * ra.d, ra.d, (int)(item - r * nb), threadIdx.x % 16, nb * 128, xq + (size_t)r * nb * 64,
               xs + (size_t)r * nb * 4);
 }
 
-// 4 bytes per lane from base + off to LDS l + 4 * lane (see dma16s).
-__device__ __forceinline__ void dma4s(const void* base, uint32_t off, FM_LDS void* l) {
-  base = uniform_ptr(base);
-  uint32_t saved;
-  asm volatile(
-      "s_mov_b32 %0, m0\n\t"
-      "s_mov_b32 m0, %3\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dword %1, %2\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(saved)
-      : "v"(off), "s"(base), "s"((uint32_t)(uintptr_t)l)
-      : "memory");
-}
-
-// RA activation rows x RB weight rows by WM x WN waves, NS slabs in the ring, BPC
-// blocks per compute unit.
-template <int RA_, int RB_, int WM_, int WN_, int NS_, int BPC_> struct MxCfg {
-  static constexpr int RA = RA_, RB = RB_, WM = WM_, WN = WN_, NS = NS_, BPC = BPC_;
-  static constexpr int TM = RA / WM, TN = RB / WN, MI = TM / 32, NJ = TN / 32;
-  static constexpr int A_BYTES = RA * 64, B_BYTES = RB * 64;
-  static constexpr int SLAB = A_BYTES + B_BYTES + (RA + RB) * 4;
-  static constexpr int A_INS = RA / 64, B_INS = RB / 64;   // 16 rows each, per wave
-  static constexpr int S_ALL = (RA + RB) / 64;             // scale instructions of a slab
-  static constexpr int S_INS = (S_ALL + 3) / 4;            // per wave (some twice)
-  static constexpr int INS = A_INS + B_INS + S_INS;
-  static constexpr int LDS = NS * SLAB;
-  static_assert(WM * WN == 4 && RA % 64 == 0 && RB % 64 == 0 && TM % 32 == 0 && TN % 32 == 0, "4 waves of 32-multiples");
-  static_assert(NS >= 2 && (NS - 2) * INS < 64 && BPC * LDS <= 160 * 1024, "ring");
+// RA activation rows x RB = 256 weight rows by 2 x 4 waves.
+template <int RA_> struct MxCfg {
+  static constexpr int RA = RA_, RB = 256;
+  static constexpr int TM = RA / 2, TN = RB / 4, MI = TM / 32, NJ = TN / 32;
+  static constexpr int A_BYTES = RA * 128, SLAB = A_BYTES + RB * 128;   // 256 k
+  static constexpr int A_INS = RA / 64, B_INS = RB / 64;                // 8 rows each, per wave
+  static constexpr int SCALES = (RA + RB) * 16;                         // 512 k
+  static constexpr int LDS = 2 * (SLAB + SCALES);
+  static_assert(RA % 64 == 0 && NJ == 2 && LDS <= 160 * 1024, "tile");
 };
 
 __device__ __forceinline__ int mx_column(int m) { return 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
-// Chunk swizzles of a 64-byte slab row: 16 consecutive lanes' rows at one logical
+// Chunk swizzles of a 128-byte slab row: 16 consecutive lanes' rows at one logical
 // chunk on 16 distinct 4-bank groups; lanes read activation rows in order, weight
 // rows in the order of mx_column.
-__device__ __forceinline__ int mx_swz_a(int r) { return (r >> 2) & 3; }
-__device__ __forceinline__ int mx_swz_b(int r) { return ((r >> 2) & 1) * 2 | ((r >> 4) & 1); }
+__device__ __forceinline__ int mx_swz_a(int r) { return (r >> 1) & 7; }
+__device__ __forceinline__ int mx_swz_b(int r) { return ((r >> 1) & 3) | ((r >> 2) & 4); }
 
 // One operand pair of a tile, rows relative to it.  w2: the second of two matrices
 // whose 32-row blocks alternate (gate, up).
@@ -296,15 +284,21 @@ struct MxTile {
   int rows, Tn;                 // activation rows of the tile's slot from the tile on
   const uint8_t *w, *w2, *s, *s2;
   int wrows;                    // weight rows (per matrix) from the tile on
-  int kx, kw;                   // 128-blocks of an activation row; 32-blocks of a weight row
+  int kx, kw;                   // 128-blocks of an activation row (even); 32-blocks of a weight row
 };
 
+// acc += X W^T.  LDS: two slabs, then two groups of scales [RA + RB rows][16 bytes].
+// The barrier at the top of slab kt says that it has landed and that every wave has
+// read slab kt - 1, whose buffer then takes slab kt + 1.  Scales of group g (slabs 2 g
+// and 2 g + 1) are requested at slab 2 g - 2 and put into LDS at slab 2 g - 1.
 template <class C, bool PAIR>
 __device__ __forceinline__ void mx_gemm(const MxTile& t, FM_LDS char* lds, f32x16_t (&acc)[C::MI][C::NJ]) {
   const int lane = lane_id(), wave = wave_id();
-  const int nk = t.kx;
-  const uint32_t ldx = t.kx * 64, ldxs = t.kx * 4, ldw = t.kw * 16, ldws = (t.kw + 3) / 4 * 4;
-  uint32_t oa[C::A_INS], ob[C::B_INS], kb[C::B_INS], os[C::S_INS];
+  const int nk = t.kx / 2;   // slabs
+  const uint32_t ldx = t.kx * 64, ldw = t.kw * 16;
+  const int sx = t.kx, sw = (t.kw + 3) / 4;   // dwords of scale rows
+  FM_LDS char* const sc = lds + 2 * C::SLAB;
+  uint32_t oa[C::A_INS], ob[C::B_INS];
   auto xrow = [&](int r) {
     r = min(r, t.rows - 1);
     return (uint32_t)(t.tok ? min(max(gptr(t.tok)[r], 0), t.Tn - 1) : r);
@@ -312,71 +306,65 @@ __device__ __forceinline__ void mx_gemm(const MxTile& t, FM_LDS char* lds, f32x1
   auto wrow = [&](int r) { return (uint32_t)min(PAIR ? 32 * (r >> 6) + (r & 31) : r, t.wrows - 1); };
 #pragma unroll
   for (int u = 0; u < C::A_INS; ++u) {
-    const int r = 16 * (wave * C::A_INS + u) + (lane >> 2);
-    oa[u] = xrow(r) * ldx + 16 * ((lane & 3) ^ mx_swz_a(r));
+    const int r = 8 * (wave * C::A_INS + u) + (lane >> 3);
+    oa[u] = xrow(r) * ldx + 16 * ((lane & 7) ^ mx_swz_a(r));
   }
 #pragma unroll
   for (int u = 0; u < C::B_INS; ++u) {
-    const int r = 16 * (wave * C::B_INS + u) + (lane >> 2);
-    kb[u] = (lane & 3) ^ mx_swz_b(r);
-    ob[u] = wrow(r) * ldw;
+    const int r = 8 * (wave * C::B_INS + u) + (lane >> 3);
+    ob[u] = wrow(r) * ldw + 16 * ((lane & 7) ^ mx_swz_b(r));
   }
+  // behind a row's end, weights repeat their row's last chunk (it meets zeros)
+  auto issue = [&](int slab) {
+    FM_LDS char* const l = lds + (slab & 1) * C::SLAB;
 #pragma unroll
-  for (int u = 0; u < C::S_INS; ++u) {
-    const int ins = (wave + 4 * u) % C::S_ALL, r = 64 * ins + lane;
-    os[u] = r < C::RA ? xrow(r) * ldxs : wrow(r - C::RA) * ldws;
-  }
-  auto issue = [&](int slab, int buf) {
-    FM_LDS char* const l = lds + buf * C::SLAB;
-#pragma unroll
-    for (int u = 0; u < C::A_INS; ++u) dma16s(t.x + (size_t)slab * 64, oa[u], l + (wave * C::A_INS + u) * 1024);
+    for (int u = 0; u < C::A_INS; ++u)
+      dma16s(t.x + (size_t)slab * 128, oa[u], l + (wave * C::A_INS + u) * 1024);
 #pragma unroll
     for (int u = 0; u < C::B_INS; ++u) {
       const int ins = wave * C::B_INS + u;
-      const uint8_t* const m = PAIR && ((ins >> 1) & 1) ? t.w2 : t.w;
-      // a chunk behind the row's end meets zero activations: any valid one
-      dma16s(m, ob[u] + 16 * min(4 * slab + (int)kb[u], t.kw - 1), l + C::A_BYTES + ins * 1024);
-    }
-#pragma unroll
-    for (int u = 0; u < C::S_INS; ++u) {
-      const int ins = (wave + 4 * u) % C::S_ALL;
-      FM_LDS char* const at = l + C::A_BYTES + C::B_BYTES + ins * 256;
-      if (ins * 64 < C::RA) {
-        dma4s(t.xs + (size_t)slab * 4, os[u], at);
-      } else if (PAIR) {
-        // 64 scales: 32 rows of each matrix
-        const uintptr_t second = (uintptr_t)t.s2 - (uintptr_t)t.s;
-        const uint8_t* const p = t.s + (size_t)slab * 4 + os[u] + ((lane >> 5) ? second : 0);
-        uint32_t saved;
-        asm volatile(
-            "s_mov_b32 %0, m0\n\t"
-            "s_mov_b32 m0, %2\n\t"
-            "s_nop 0\n\t"
-            "global_load_lds_dword %1, off\n\t"
-            "s_mov_b32 m0, %0"
-            : "=&s"(saved)
-            : "v"(p), "s"((uint32_t)(uintptr_t)at)
-            : "memory");
-      } else {
-        dma4s(t.s + (size_t)slab * 4, os[u], at);
+      const uint8_t* const w = (PAIR && ((ins >> 2) & 1) ? t.w2 : t.w) + (size_t)slab * 128;
+      uint32_t o = ob[u];
+      if (8 * slab + 8 > t.kw) {
+        const int k = (lane & 7) ^ mx_swz_b(8 * ins + (lane >> 3));
+        o += 16 * (min(k, t.kw - 1 - 8 * slab) - k);
       }
+      dma16s(w, o, l + C::A_BYTES + ins * 1024);
     }
   };
-  const int row0 = (wave % C::WM) * C::TM, col0 = (wave / C::WM) * C::TN;
+  // this lane's scale row (waves past the rows repeat the last)
+  const int sr = min(64 * wave + lane, C::RA + C::RB - 1), br = sr - C::RA;
+  const bool wside = 64 * wave >= C::RA;
+  const uint8_t* const sp = wside ? (PAIR && ((br >> 5) & 1) ? t.s2 : t.s) + (size_t)wrow(br) * sw * 4
+                                  : t.xs + (size_t)xrow(sr) * sx * 4;
+  const int slen = wside ? sw : sx;
+  typedef u32x4_t u32x4_a4 __attribute__((aligned(4)));
+  // dwords [4 g, 4 g + 4) of a row of n, the last group moved back to end with the row
+  auto group_at = [](int g, int n) { return max(min(4 * g, n - 4), 0); };
+  auto load_scales = [&](int g) {
+    u32x4_t v;
+    if (slen >= 4) return (u32x4_t)*(const FM_GLOBAL u32x4_a4*)(sp + 4 * group_at(g, slen));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = *(const FM_GLOBAL uint32_t*)(sp + 4 * min(i, slen - 1));
+    return v;
+  };
+  auto put_scales = [&](int g, const u32x4_t& v) {
+    if (64 * wave < C::RA + C::RB) *(FM_LDS u32x4_t*)(sc + (g & 1) * C::SCALES + sr * 16) = v;
+  };
+  const int row0 = (wave & 1) * C::TM, col0 = (wave >> 1) * C::TN;
   const int m = lane & 31, h = lane >> 5;
-  uint32_t fa[C::MI], fb[C::NJ], ga[C::MI], gb[C::NJ];
+  uint32_t fa[C::MI], fb[C::NJ];
 #pragma unroll
   for (int i = 0; i < C::MI; ++i) {
     const int r = row0 + 32 * i + m;
-    fa[i] = r * 64 + ((h ^ mx_swz_a(r)) << 4);
-    ga[i] = C::A_BYTES + C::B_BYTES + r * 4;
+    fa[i] = r * 128 + ((h ^ mx_swz_a(r)) << 4);
   }
 #pragma unroll
   for (int j = 0; j < C::NJ; ++j) {
     const int r = col0 + 32 * j + mx_column(m);
-    fb[j] = C::A_BYTES + r * 64 + ((h ^ mx_swz_b(r)) << 4);
-    gb[j] = C::A_BYTES + C::B_BYTES + (C::RA + r) * 4;
+    fb[j] = C::A_BYTES + r * 128 + ((h ^ mx_swz_b(r)) << 4);
   }
+  const uint32_t ga = (row0 + m) * 16, gb = (C::RA + col0 + mx_column(m)) * 16;
 #pragma unroll
   for (int i = 0; i < C::MI; ++i)
 #pragma unroll
@@ -384,47 +372,69 @@ __device__ __forceinline__ void mx_gemm(const MxTile& t, FM_LDS char* lds, f32x1
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-#pragma nounroll
-  for (int s = 0; s < C::NS - 1 && s < nk; ++s) issue(s, s);
-  int cur = 0, nxt = C::NS - 1;
+  issue(0);
+  put_scales(0, load_scales(0));
+  u32x4_t next;
 #pragma nounroll
   for (int kt = 0; kt < nk; ++kt) {
-    // slab kt has landed once at most the slabs after it are in flight
-    if (nk - 1 - kt >= C::NS - 2) wait_vmcnt<(C::NS - 2) * C::INS>();
-    else wait_vmcnt<0>();
+    wait_vmcnt<0>();
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    FM_LDS char* const l = lds + cur * C::SLAB;
-    u32x4_t xa[2][C::MI], xb[2][C::NJ];
-    int sa[C::MI], sb[C::NJ];
-#pragma unroll
-    for (int i = 0; i < C::MI; ++i) sa[i] = *(const FM_LDS int*)(l + ga[i]) >> (8 * h);
-#pragma unroll
-    for (int j = 0; j < C::NJ; ++j) sb[j] = *(const FM_LDS int*)(l + gb[j]) >> (8 * h);
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {
-#pragma unroll
-      for (int i = 0; i < C::MI; ++i) xa[st][i] = *(const FM_LDS u32x4_t*)(l + (fa[i] ^ (st << 5)));
-#pragma unroll
-      for (int j = 0; j < C::NJ; ++j) xb[st][j] = *(const FM_LDS u32x4_t*)(l + (fb[j] ^ (st << 5)));
+    if (kt + 1 < nk) issue(kt + 1);
+    if (!(kt & 1)) {
+      if (kt + 2 < nk) next = load_scales(kt / 2 + 1);
+    } else if (kt + 1 < nk) {
+      put_scales(kt / 2 + 1, next);
     }
-    sched_fence();
-    if (kt + C::NS - 1 < nk) issue(kt + C::NS - 1, nxt);
-    sched_fence();
+    const FM_LDS char* const l = lds + (kt & 1) * C::SLAB;
+    const FM_LDS char* const s = sc + ((kt >> 1) & 1) * C::SCALES;
+    const FM_LDS char* const s_x = s + 4 * (2 * kt - group_at(kt >> 1, sx));
+    const FM_LDS char* const s_w = s + 4 * (2 * kt - group_at(kt >> 1, sw));
+    const bool half = 2 * kt + 1 == sw;   // the slab's second 128 k lie past the weights: scale 0 there
+    u32x4_t xa[2][C::MI], xb[2][C::NJ];
+    int sa[2][C::MI], sb[2][C::NJ];
+    auto read = [&](int st) {
+      int flip = st << 5;
+      asm volatile("" : "+s"(flip));   // not hoisted: the 24 addresses would take the registers of the sums
+#pragma unroll
+      for (int i = 0; i < C::MI; ++i) xa[st & 1][i] = *(const FM_LDS u32x4_t*)(l + (fa[i] ^ flip));
+#pragma unroll
+      for (int j = 0; j < C::NJ; ++j) xb[st & 1][j] = *(const FM_LDS u32x4_t*)(l + (fb[j] ^ flip));
+    };
+    auto scales = [&](int q) {   // of 128 k: blocks h and h + 2 in bytes 0 and 2
+#pragma unroll
+      for (int i = 0; i < C::MI; ++i) sa[q][i] = *(const FM_LDS int*)(s_x + ga + 512 * i + 4 * q) >> (8 * h);
+#pragma unroll
+      for (int j = 0; j < C::NJ; ++j) {
+        sb[q][j] = *(const FM_LDS int*)(s_w + gb + 512 * j + (half ? 0 : 4 * q)) >> (8 * h);
+        if (q == 1 && half) sb[q][j] = 0;
+      }
+    };
     auto wide = [](const u32x4_t& v) { return i32x8_t{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; };
+    auto multiply = [&](auto st_) {
+      constexpr int st = decltype(st_)::value, by = 2 * (st & 1);
 #pragma unroll
-    for (int j = 0; j < C::NJ; ++j)
+      for (int j = 0; j < C::NJ; ++j)
 #pragma unroll
-      for (int i = 0; i < C::MI; ++i)
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(xb[0][j]), wide(xa[0][i]), acc[i][j], 4, 4, 0,
-                                                                    sb[j], 0, sa[i]);
-#pragma unroll
-    for (int j = 0; j < C::NJ; ++j)
-#pragma unroll
-      for (int i = 0; i < C::MI; ++i)
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(xb[1][j]), wide(xa[1][i]), acc[i][j], 4, 4, 2,
-                                                                    sb[j], 2, sa[i]);
-    cur = cur + 1 == C::NS ? 0 : cur + 1;
-    nxt = nxt + 1 == C::NS ? 0 : nxt + 1;
+        for (int i = 0; i < C::MI; ++i)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(xb[st & 1][j]), wide(xa[st & 1][i]), acc[i][j], 4,
+                                                                      4, by, sb[st >> 1][j], by, sa[st >> 1][i]);
+    };
+    // a step's fragments are read while the one before it multiplies, and not earlier
+    // (two sets of registers)
+    scales(0);
+    read(0);
+    sched_fence();
+    read(1);
+    multiply(std::integral_constant<int, 0>{});
+    sched_fence();
+    scales(1);
+    read(2);
+    multiply(std::integral_constant<int, 1>{});
+    sched_fence();
+    read(3);
+    multiply(std::integral_constant<int, 2>{});
+    sched_fence();
+    multiply(std::integral_constant<int, 3>{});
   }
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
@@ -437,103 +447,107 @@ struct MxArgs {
   bf16* O;
 };
 
-// H = MX(silu(MX(X) Qg^T) (MX(X) Qu^T)), RB / 2 columns per tile.
-template <class C> __global__ __launch_bounds__(256, C::BPC) void k_mx_gate_up(MxArgs a) {
-  __shared__ __align__(16) char lds_[C::LDS];
-  FM_LDS char* const lds = (FM_LDS char*)lds_;
-  static_assert(C::NJ % 2 == 0, "gate / up pairs");
-  constexpr int CI = C::RB / 2;
+// H = MX(silu(MX(X) Qg^T) (MX(X) Qu^T)) of one tile, 128 columns.
+template <class C> __device__ __forceinline__ void mx_gate_up_tile(const MxArgs& a, FM_LDS char* lds, const MxRows& r) {
   const RowArgs& ra = a.ra;
-  const int I = ra.I, nI = up128(I) / 128, NT = nI * (128 / CI), kd = up128(ra.d) / 128;
-  const MxWalk walk = mx_walk(ra, NT);
-  for (int tt = walk.at; tt < walk.end; tt += walk.step) {
-    const MxRows r = mx_rows(ra, tt, NT, C::RA);
-    const int n0 = r.n * CI;
-    const int nw = min(n0, I - 1);   // a tile of the rows' padding reads the last row
-    const size_t lw = up32(ra.d) / 2, ls = kd * 4;
-    MxTile t;
-    t.x = a.w.xq + (r.sr.shared ? (size_t)r.m0 * kd * 64 : 0);
-    t.xs = a.w.xs + (r.sr.shared ? (size_t)r.m0 * kd * 4 : 0);
-    t.tok = r.sr.shared ? nullptr : a.perm_token + r.sr.xrow0 + r.m0;
-    t.rows = r.rows;
-    t.Tn = ra.Tn;
-    t.w = ld_scalar(a.W.qg + r.s) + nw * lw;
-    t.w2 = ld_scalar(a.W.qu + r.s) + nw * lw;
-    t.s = ld_scalar(a.W.sg + r.s) + nw * ls;
-    t.s2 = ld_scalar(a.W.su + r.s) + nw * ls;
-    t.wrows = I - nw;
-    t.kx = kd;
-    t.kw = up32(ra.d) / 32;
-    f32x16_t acc[C::MI][C::NJ];
-    mx_gemm<C, true>(t, lds, acc);
-    const int lane = lane_id_here(), wave = wave_id(), h = lane >> 5;
+  const int I = ra.I, nI = act_blocks(I), kd = act_blocks(ra.d), n0 = r.n * 128;
+  const size_t lw = up32(ra.d) / 2, ls = up128(ra.d) / 32;
+  MxTile t;
+  t.x = a.w.xq + (r.sr.shared ? (size_t)r.m0 * kd * 64 : 0);
+  t.xs = a.w.xs + (r.sr.shared ? (size_t)r.m0 * kd * 4 : 0);
+  t.tok = r.sr.shared ? nullptr : a.perm_token + r.sr.xrow0 + r.m0;
+  t.rows = r.rows;
+  t.Tn = ra.Tn;
+  t.w = ld_scalar(a.W.qg + r.s) + n0 * lw;
+  t.w2 = ld_scalar(a.W.qu + r.s) + n0 * lw;
+  t.s = ld_scalar(a.W.sg + r.s) + n0 * ls;
+  t.s2 = ld_scalar(a.W.su + r.s) + n0 * ls;
+  t.wrows = I - n0;
+  t.kx = kd;
+  t.kw = up32(ra.d) / 32;
+  f32x16_t acc[C::MI][C::NJ];
+  mx_gemm<C, true>(t, lds, acc);
+  const int lane = lane_id_here(), wave = wave_id(), h = lane >> 5;
+  const int col = n0 + (wave >> 1) * 32;   // of this wave's 32-block
 #pragma unroll
-    for (int i = 0; i < C::MI; ++i) {
-      const int row = (wave % C::WM) * C::TM + 32 * i + (lane & 31);
+  for (int i = 0; i < C::MI; ++i) {
+    const int row = (wave & 1) * C::TM + 32 * i + (lane & 31);
+    float v[16];
+    uint32_t top = 0;
 #pragma unroll
-      for (int jj = 0; jj < C::NJ / 2; ++jj) {
-        const int col = n0 + (wave / C::WM) * (C::TN / 2) + 32 * jj;   // of the 32-block
-        float v[16];
-        uint32_t top = 0;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float g = acc[i][2 * jj][e];
-          v[e] = col + 16 * h + e < I ? g * sigm_fast(g) * acc[i][2 * jj + 1][e] : 0.f;
-          top = max(top, abs_bits(v[e]));
-        }
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        const uint32_t byte = mx_byte(top);
-        const float inv = mx_inv(byte);
-        u32x2_t code = {mx_codes8(v, inv), mx_codes8(v + 8, inv)};
-        if (byte == 255) code = u32x2_t{0u, 0u};
-        if (row < r.rows) {
-          *(FM_GLOBAL u32x2_t*)(a.w.hq + (r.ob + row) * nI * 64 + col / 2 + 8 * h) = code;
-          if (h == 0) *(FM_GLOBAL uint8_t*)(a.w.hs + (r.ob + row) * nI * 4 + col / 32) = (uint8_t)byte;
-        }
+    for (int e = 0; e < 16; ++e) {
+      const float g = acc[i][0][e];
+      v[e] = col + 16 * h + e < I ? g * sigm_fast(g) * acc[i][1][e] : 0.f;
+      top = max(top, abs_bits(v[e]));
+    }
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+    const uint32_t byte = mx_byte(top);
+    const float inv = mx_inv(byte);
+    u32x2_t code = {mx_codes8(v, inv), mx_codes8(v + 8, inv)};
+    if (byte == 255) code = u32x2_t{0u, 0u};
+    if (row < r.rows) {
+      *(FM_GLOBAL u32x2_t*)(a.w.hq + (r.ob + row) * nI * 64 + col / 2 + 8 * h) = code;
+      if (h == 0) *(FM_GLOBAL uint8_t*)(a.w.hs + (r.ob + row) * nI * 4 + col / 32) = (uint8_t)byte;
+      if (n0 + 128 >= I && r.n % 2 == 0) {   // the 128 columns behind the last tile
+        *(FM_GLOBAL u32x2_t*)(a.w.hq + (r.ob + row) * nI * 64 + (col + 128) / 2 + 8 * h) = u32x2_t{0u, 0u};
+        if (h == 0) *(FM_GLOBAL uint8_t*)(a.w.hs + (r.ob + row) * nI * 4 + (col + 128) / 32) = 0;
       }
     }
   }
 }
 
-// O = MX(H) Qd^T.
-template <class C> __global__ __launch_bounds__(256, C::BPC) void k_mx_down(MxArgs a) {
-  __shared__ __align__(16) char lds_[C::LDS];
-  FM_LDS char* const lds = (FM_LDS char*)lds_;
+// O = MX(H) Qd^T of one tile, 256 columns.
+template <class C> __device__ __forceinline__ void mx_down_tile(const MxArgs& a, FM_LDS char* lds, const MxRows& r) {
   const RowArgs& ra = a.ra;
-  const int d = ra.d, nI = up128(ra.I) / 128, NT = (d + C::RB - 1) / C::RB;
-  const MxWalk walk = mx_walk(ra, NT);
-  for (int tt = walk.at; tt < walk.end; tt += walk.step) {
-    const MxRows r = mx_rows(ra, tt, NT, C::RA);
-    const int n0 = r.n * C::RB;
-    MxTile t;
-    t.x = a.w.hq + r.ob * nI * 64;
-    t.xs = a.w.hs + r.ob * nI * 4;
-    t.tok = nullptr;
-    t.rows = r.rows;
-    t.Tn = ra.Tn;
-    t.w = ld_scalar(a.W.qd + r.s) + (size_t)n0 * (up32(ra.I) / 2);
-    t.s = ld_scalar(a.W.sd + r.s) + (size_t)n0 * nI * 4;
-    t.w2 = t.s2 = nullptr;
-    t.wrows = d - n0;
-    t.kx = nI;
-    t.kw = up32(ra.I) / 32;
-    f32x16_t acc[C::MI][C::NJ];
-    mx_gemm<C, false>(t, lds, acc);
-    const int lane = lane_id_here(), wave = wave_id(), h = lane >> 5;
+  const int d = ra.d, nI = act_blocks(ra.I), n0 = r.n * C::RB;
+  MxTile t;
+  t.x = a.w.hq + r.ob * nI * 64;
+  t.xs = a.w.hs + r.ob * nI * 4;
+  t.tok = nullptr;
+  t.rows = r.rows;
+  t.Tn = ra.Tn;
+  t.w = ld_scalar(a.W.qd + r.s) + (size_t)n0 * (up32(ra.I) / 2);
+  t.s = ld_scalar(a.W.sd + r.s) + (size_t)n0 * (up128(ra.I) / 32);
+  t.w2 = t.s2 = nullptr;
+  t.wrows = d - n0;
+  t.kx = nI;
+  t.kw = up32(ra.I) / 32;
+  f32x16_t acc[C::MI][C::NJ];
+  mx_gemm<C, false>(t, lds, acc);
+  const int lane = lane_id_here(), wave = wave_id(), h = lane >> 5;
 #pragma unroll
-    for (int i = 0; i < C::MI; ++i) {
-      const int row = (wave % C::WM) * C::TM + 32 * i + (lane & 31);
+  for (int i = 0; i < C::MI; ++i) {
+    const int row = (wave & 1) * C::TM + 32 * i + (lane & 31);
 #pragma unroll
-      for (int j = 0; j < C::NJ; ++j) {
-        const int col = n0 + (wave / C::WM) * C::TN + 32 * j + 16 * h;
+    for (int j = 0; j < C::NJ; ++j) {
+      const int col = n0 + (wave >> 1) * C::TN + 32 * j + 16 * h;
 #pragma unroll
-        for (int e = 0; e < 16; e += 8) {
-          float v[8];
+      for (int e = 0; e < 16; e += 8) {
+        float v[8];
 #pragma unroll
-          for (int x = 0; x < 8; ++x) v[x] = acc[i][j][e + x];
-          if (row < r.rows && col + e < d) st16(a.O + (r.ob + row) * d + col + e, pack16(v, (bf16*)nullptr));
-        }
+        for (int x = 0; x < 8; ++x) v[x] = acc[i][j][e + x];
+        if (row < r.rows && col + e < d) st16(a.O + (r.ob + row) * d + col + e, pack16(v, (bf16*)nullptr));
       }
+    }
+  }
+}
+
+// A tile of at most 128 rows runs as a half-height one.
+typedef MxCfg<256> M256;
+typedef MxCfg<128> M128;
+template <bool DOWN> __global__ __launch_bounds__(512, 2) void k_mx_tiles(MxArgs a) {
+  __shared__ __align__(16) char lds_[M256::LDS];
+  FM_LDS char* const lds = (FM_LDS char*)lds_;
+  const int NT = DOWN ? (a.ra.d + 255) / 256 : (a.ra.I + 127) / 128;
+  const MxWalk walk = mx_walk(a.ra, NT);
+  for (int tt = walk.at; tt < walk.end; tt += walk.step) {
+    const MxRows r = mx_rows(a.ra, tt, NT, M256::RA);
+    if (r.rows <= M128::RA) {
+      if (DOWN) mx_down_tile<M128>(a, lds, r);
+      else mx_gate_up_tile<M128>(a, lds, r);
+    } else {
+      if (DOWN) mx_down_tile<M256>(a, lds, r);
+      else mx_gate_up_tile<M256>(a, lds, r);
     }
   }
 }
@@ -737,8 +751,6 @@ __global__ __launch_bounds__(64 * NW) void k_mx_few_down(MxArgs a, int NT, int m
   }
 }
 
-using M128 = MxCfg<128, 256, 2, 2, 3, 2>;
-
 // Whether a call takes the kernels for a few tokens.  us there and on the tiles: one
 // token, d = 4096, I = 688, 4 of 16 slots 13 and 37; d = 2048, I = 1408, 6 of 64 and 2
 // shared 19 and 30; 4 tokens of that layer (26 slots, 4576 blocks) 32 and 33, 16 tokens
@@ -749,11 +761,12 @@ bool mx_few_tokens(const moe_layer_mx4* L, int T, long active) {
          T * mx_few_row_bytes(up128(L->I) / 128) <= 52 * 1024;
 }
 
-template <class C> dim3 mx_grid(const RowArgs& ra, int NT) {
+// One block per compute unit, a multiple of the XCDs, at most one per tile.
+dim3 mx_grid(const RowArgs& ra, int NT) {
   const long long R = (long long)ra.Tn * ra.k;
-  const long long tiles = (R / C::RA + (R < ra.S_r ? R : ra.S_r) +
-                           (long long)(ra.S - ra.S_r) * ((ra.Tn + C::RA - 1) / C::RA)) * NT;
-  const long long most = (long long)(device_cus() + N_XCD - 1) / N_XCD * N_XCD * C::BPC;
+  const long long tiles = (R / M256::RA + (R < ra.S_r ? R : ra.S_r) +
+                           (long long)(ra.S - ra.S_r) * ((ra.Tn + M256::RA - 1) / M256::RA)) * NT;
+  const long long most = (long long)(device_cus() + N_XCD - 1) / N_XCD * N_XCD;
   const long long g = (tiles + N_XCD - 1) / N_XCD * N_XCD;
   return dim3((unsigned)(g < most ? g : most));
 }
@@ -860,10 +873,6 @@ extern "C" int moe_grouped_swiglu_fwd_mx4(const moe_layer_mx4* L, const void* X,
   const MxArgs a{{L->q_gate, L->q_up, L->q_down, L->s_gate, L->s_up, L->s_down}, w, perm_token, ra, (bf16*)O};
   const int nb = up128(L->d) / 128;
   const bf16* const Xb = (const bf16*)X;
-  auto prep = [&](int tile_rows) {
-    hipLaunchKernelGGL(k_mx_prep, dim3(cdiv((long)T * nb, 16) + 1), dim3(256), 0, st, Xb, ra, tile_rows, nb, w.xq, w.xs,
-                       w.mbase);
-  };
   const long R = (long)T * k;
   const long active = (R < L->S_routed ? R : L->S_routed) + L->S_shared;   // slots that may hold rows
   if (mx_few_tokens(L, T, active)) {
@@ -874,9 +883,9 @@ extern "C" int moe_grouped_swiglu_fwd_mx4(const moe_layer_mx4* L, const void* X,
                        T * mx_few_row_bytes(up128(L->I) / 128) + 4 * 2048, st, a, nd, T);
     return check_launch("moe_grouped_swiglu_fwd_mx4");
   }
-  typedef M128 C;
-  prep(C::RA);
-  hipLaunchKernelGGL(k_mx_gate_up<C>, mx_grid<C>(ra, up128(L->I) / 128 * (256 / C::RB)), dim3(256), 0, st, a);
-  hipLaunchKernelGGL(k_mx_down<C>, mx_grid<C>(ra, cdiv(L->d, C::RB)), dim3(256), 0, st, a);
+  const int na = act_blocks(L->d);
+  hipLaunchKernelGGL(k_mx_prep, dim3(cdiv((long)T * na, 16) + 1), dim3(256), 0, st, Xb, ra, M256::RA, na, w.xq, w.xs, w.mbase);
+  hipLaunchKernelGGL(k_mx_tiles<false>, mx_grid(ra, cdiv(L->I, 128)), dim3(512), 0, st, a);
+  hipLaunchKernelGGL(k_mx_tiles<true>, mx_grid(ra, cdiv(L->d, 256)), dim3(512), 0, st, a);
   return check_launch("moe_grouped_swiglu_fwd_mx4");
 }
