@@ -146,7 +146,7 @@ struct MxPtrs {
   const uint8_t* const* sd;
 };
 
-constexpr int MX_FEW = 16;   // tokens of a call that takes the kernels for few
+constexpr int MX_FEW = 8;   // most tokens of a call that takes the kernels for few
 
 // Workspace: row-tile prefix, X and H as packed rows of whole 256-blocks.
 struct MxWs {
@@ -258,15 +258,16 @@ __global__ __launch_bounds__(256) void k_mx_prep(const bf16* __restrict__ X, Row
               xs + (size_t)r * nb * 4);
 }
 
-// RA activation rows x RB = 256 weight rows by 2 x 4 waves.
-template <int RA_> struct MxCfg {
-  static constexpr int RA = RA_, RB = 256;
-  static constexpr int TM = RA / 2, TN = RB / 4, MI = TM / 32, NJ = TN / 32;
+// RA activation rows x RB weight rows by 2 x WN waves; BPC blocks per compute unit.
+template <int RA_, int RB_, int WN_, int BPC_> struct MxCfg {
+  static constexpr int RA = RA_, RB = RB_, WN = WN_, NW = 2 * WN, BPC = BPC_;
+  static constexpr int TM = RA / 2, TN = RB / WN, MI = TM / 32, NJ = TN / 32;
   static constexpr int A_BYTES = RA * 128, SLAB = A_BYTES + RB * 128;   // 256 k
-  static constexpr int A_INS = RA / 64, B_INS = RB / 64;                // 8 rows each, per wave
+  static constexpr int A_INS = RA / 8 / NW, B_INS = RB / 8 / NW;        // 8 rows each, per wave
   static constexpr int SCALES = (RA + RB) * 16;                         // 512 k
   static constexpr int LDS = 2 * (SLAB + SCALES);
-  static_assert(RA % 64 == 0 && NJ == 2 && LDS <= 160 * 1024, "tile");
+  static_assert(RA % (8 * NW) == 0 && RA % 64 == 0 && RB % (8 * NW) == 0 && NJ == 2 && RA + RB <= 64 * NW, "tile");
+  static_assert(BPC * LDS <= 160 * 1024, "LDS");
 };
 
 __device__ __forceinline__ int mx_column(int m) { return 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
@@ -447,10 +448,10 @@ struct MxArgs {
   bf16* O;
 };
 
-// H = MX(silu(MX(X) Qg^T) (MX(X) Qu^T)) of one tile, 128 columns.
+// H = MX(silu(MX(X) Qg^T) (MX(X) Qu^T)) of one tile, RB / 2 columns.
 template <class C> __device__ __forceinline__ void mx_gate_up_tile(const MxArgs& a, FM_LDS char* lds, const MxRows& r) {
   const RowArgs& ra = a.ra;
-  const int I = ra.I, nI = act_blocks(I), kd = act_blocks(ra.d), n0 = r.n * 128;
+  const int I = ra.I, nI = act_blocks(I), kd = act_blocks(ra.d), n0 = r.n * (C::RB / 2);
   const size_t lw = up32(ra.d) / 2, ls = up128(ra.d) / 32;
   MxTile t;
   t.x = a.w.xq + (r.sr.shared ? (size_t)r.m0 * kd * 64 : 0);
@@ -488,15 +489,17 @@ template <class C> __device__ __forceinline__ void mx_gate_up_tile(const MxArgs&
     if (row < r.rows) {
       *(FM_GLOBAL u32x2_t*)(a.w.hq + (r.ob + row) * nI * 64 + col / 2 + 8 * h) = code;
       if (h == 0) *(FM_GLOBAL uint8_t*)(a.w.hs + (r.ob + row) * nI * 4 + col / 32) = (uint8_t)byte;
-      if (n0 + 128 >= I && r.n % 2 == 0) {   // the 128 columns behind the last tile
-        *(FM_GLOBAL u32x2_t*)(a.w.hq + (r.ob + row) * nI * 64 + (col + 128) / 2 + 8 * h) = u32x2_t{0u, 0u};
-        if (h == 0) *(FM_GLOBAL uint8_t*)(a.w.hs + (r.ob + row) * nI * 4 + (col + 128) / 32) = 0;
-      }
+      // the row's padding, behind the last tile
+      if (n0 + C::RB / 2 >= I)
+        for (int c = col + C::RB / 2; c < nI * 128; c += C::RB / 2) {
+          *(FM_GLOBAL u32x2_t*)(a.w.hq + (r.ob + row) * nI * 64 + c / 2 + 8 * h) = u32x2_t{0u, 0u};
+          if (h == 0) *(FM_GLOBAL uint8_t*)(a.w.hs + (r.ob + row) * nI * 4 + c / 32) = 0;
+        }
     }
   }
 }
 
-// O = MX(H) Qd^T of one tile, 256 columns.
+// O = MX(H) Qd^T of one tile, RB columns.
 template <class C> __device__ __forceinline__ void mx_down_tile(const MxArgs& a, FM_LDS char* lds, const MxRows& r) {
   const RowArgs& ra = a.ra;
   const int d = ra.d, nI = act_blocks(ra.I), n0 = r.n * C::RB;
@@ -532,25 +535,28 @@ template <class C> __device__ __forceinline__ void mx_down_tile(const MxArgs& a,
   }
 }
 
-// A tile of at most 128 rows runs as a half-height one.
-typedef MxCfg<256> M256;
-typedef MxCfg<128> M128;
-template <bool DOWN> __global__ __launch_bounds__(512, 2) void k_mx_tiles(MxArgs a) {
-  __shared__ __align__(16) char lds_[M256::LDS];
+template <class C, bool DOWN> __device__ __forceinline__ void mx_tile(const MxArgs& a, FM_LDS char* lds, const MxRows& r) {
+  if constexpr (DOWN) mx_down_tile<C>(a, lds, r);
+  else mx_gate_up_tile<C>(a, lds, r);
+}
+
+// C: the tile; HALF: its half-height form for tiles with at most half the rows left.
+template <class C, class HALF, bool DOWN> __global__ __launch_bounds__(64 * C::NW, C::BPC * C::NW / 4) void k_mx_tiles(MxArgs a) {
+  __shared__ __align__(16) char lds_[C::LDS];
   FM_LDS char* const lds = (FM_LDS char*)lds_;
-  const int NT = DOWN ? (a.ra.d + 255) / 256 : (a.ra.I + 127) / 128;
+  constexpr int COLS = DOWN ? C::RB : C::RB / 2;
+  const int NT = ((DOWN ? a.ra.d : a.ra.I) + COLS - 1) / COLS;
   const MxWalk walk = mx_walk(a.ra, NT);
   for (int tt = walk.at; tt < walk.end; tt += walk.step) {
-    const MxRows r = mx_rows(a.ra, tt, NT, M256::RA);
-    if (r.rows <= M128::RA) {
-      if (DOWN) mx_down_tile<M128>(a, lds, r);
-      else mx_gate_up_tile<M128>(a, lds, r);
-    } else {
-      if (DOWN) mx_down_tile<M256>(a, lds, r);
-      else mx_gate_up_tile<M256>(a, lds, r);
-    }
+    const MxRows r = mx_rows(a.ra, tt, NT, C::RA);
+    if (HALF::RA < C::RA && r.rows <= HALF::RA) mx_tile<HALF, DOWN>(a, lds, r);
+    else mx_tile<C, DOWN>(a, lds, r);
   }
 }
+
+typedef MxCfg<256, 256, 4, 1> M256;
+typedef MxCfg<128, 256, 4, 1> M128;
+typedef MxCfg<64, 128, 2, 2> M64;
 
 // --------------------------------------------------------- a few tokens ----
 // Calls of a few tokens are bound by latency and by the weights' bytes, which have to be
@@ -751,24 +757,43 @@ __global__ __launch_bounds__(64 * NW) void k_mx_few_down(MxArgs a, int NT, int m
   }
 }
 
-// Whether a call takes the kernels for a few tokens.  us there and on the tiles: one
-// token, d = 4096, I = 688, 4 of 16 slots 13 and 37; d = 2048, I = 1408, 6 of 64 and 2
-// shared 19 and 30; 4 tokens of that layer (26 slots, 4576 blocks) 32 and 33, 16 tokens
-// (66 slots, 11616) 70 and 53; 16 tokens of the first 37 and 40; 16 tokens, d = 512, I =
-// 256, 8 slots 10 and 18.  A block's rows have to fit the LDS.
+// Whether a call takes the kernels for a few tokens.  us there and on 64-row tiles, a
+// pass among others: d = 4096, I = 688, 16 slots, top-4: 1 token 19, 26; 4 tokens 21, 28;
+// 8 27, 29; 16 36, 29.  d = 2048, I = 1408, 64 + 2 slots, top-6: 1 token (1408 blocks)
+// 17, 21; 2 (2464) 24, 24; 4 (4576) 33, 25.  d = 512, I = 256, 8 slots, top-2: 1 token
+// 14, 12; 8 14, 13.  A block's rows have to fit the LDS.
 bool mx_few_tokens(const moe_layer_mx4* L, int T, long active) {
-  return T <= MX_FEW && active * (L->I / 8) <= 4096 && T * mx_few_row_bytes(up128(L->d) / 128) <= 56 * 1024 &&
-         T * mx_few_row_bytes(up128(L->I) / 128) <= 52 * 1024;
+  return T <= MX_FEW && active * (L->I / 8) <= 2048 && (long)L->d * L->I >= 1 << 20 &&
+         T * mx_few_row_bytes(up128(L->d) / 128) <= 56 * 1024 && T * mx_few_row_bytes(up128(L->I) / 128) <= 52 * 1024;
+}
+// Whether it takes 256-row tiles, one block of 8 waves per compute unit, rather than
+// 64-row ones, two of 4 waves: with many rows per slot (each byte of weights feeds more
+// MFMAs) that make tiles enough.  us of 64 and 256-row tiles: the first layer above 700
+// tokens (175 rows per slot, 113 tiles) 56, 71; 1500 (375, 188) 100, 85; 4096 217, 173;
+// the second 333 tokens (35 rows) 90, 110; 700 (74, 551 tiles) 121, 127; 1500 (159, 812) 199, 173;
+// 4096 412, 314; the third 4096 tokens (1024, 72 tiles) 23, 27.
+bool mx_large_tiles(const moe_layer_mx4* L, int T, int k, long active) {
+  const double r = (double)T * (k + L->S_shared) / active;
+  return r >= 100 && active * (r / 256 + 0.5) * ((L->I + 127) / 128) >= 150;
 }
 
-// One block per compute unit, a multiple of the XCDs, at most one per tile.
-dim3 mx_grid(const RowArgs& ra, int NT) {
+// BPC blocks per compute unit, a multiple of the XCDs, at most one per tile.
+template <class C> dim3 mx_grid(const RowArgs& ra, int NT) {
   const long long R = (long long)ra.Tn * ra.k;
-  const long long tiles = (R / M256::RA + (R < ra.S_r ? R : ra.S_r) +
-                           (long long)(ra.S - ra.S_r) * ((ra.Tn + M256::RA - 1) / M256::RA)) * NT;
-  const long long most = (long long)(device_cus() + N_XCD - 1) / N_XCD * N_XCD;
+  const long long tiles = (R / C::RA + (R < ra.S_r ? R : ra.S_r) +
+                           (long long)(ra.S - ra.S_r) * ((ra.Tn + C::RA - 1) / C::RA)) * NT;
+  const long long most = (long long)(device_cus() + N_XCD - 1) / N_XCD * N_XCD * C::BPC;
   const long long g = (tiles + N_XCD - 1) / N_XCD * N_XCD;
   return dim3((unsigned)(g < most ? g : most));
+}
+
+template <class C, class HALF> void mx_tiles(const MxArgs& a, const bf16* X, hipStream_t st) {
+  const RowArgs& ra = a.ra;
+  const int nb = act_blocks(ra.d);
+  hipLaunchKernelGGL(k_mx_prep, dim3(cdiv((long)ra.Tn * nb, 16) + 1), dim3(256), 0, st, X, ra, C::RA, nb, a.w.xq, a.w.xs,
+                     a.w.mbase);
+  hipLaunchKernelGGL((k_mx_tiles<C, HALF, false>), mx_grid<C>(ra, cdiv(ra.I, C::RB / 2)), dim3(64 * C::NW), 0, st, a);
+  hipLaunchKernelGGL((k_mx_tiles<C, HALF, true>), mx_grid<C>(ra, cdiv(ra.d, C::RB)), dim3(64 * C::NW), 0, st, a);
 }
 
 int check_rows(const void* a, const char* an, const void* b, const char* bn, const void* c, const char* cn, long rows,
@@ -883,9 +908,7 @@ extern "C" int moe_grouped_swiglu_fwd_mx4(const moe_layer_mx4* L, const void* X,
                        T * mx_few_row_bytes(up128(L->I) / 128) + 4 * 2048, st, a, nd, T);
     return check_launch("moe_grouped_swiglu_fwd_mx4");
   }
-  const int na = act_blocks(L->d);
-  hipLaunchKernelGGL(k_mx_prep, dim3(cdiv((long)T * na, 16) + 1), dim3(256), 0, st, Xb, ra, M256::RA, na, w.xq, w.xs, w.mbase);
-  hipLaunchKernelGGL(k_mx_tiles<false>, mx_grid(ra, cdiv(L->I, 128)), dim3(512), 0, st, a);
-  hipLaunchKernelGGL(k_mx_tiles<true>, mx_grid(ra, cdiv(L->d, 256)), dim3(512), 0, st, a);
+  if (mx_large_tiles(L, T, k, active)) mx_tiles<M256, M128>(a, Xb, st);
+  else mx_tiles<M64, M64>(a, Xb, st);
   return check_launch("moe_grouped_swiglu_fwd_mx4");
 }
