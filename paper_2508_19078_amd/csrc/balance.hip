@@ -548,22 +548,7 @@ template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(Router
       load_x(t + RB_SLAB, buf ^ 1);
       load_dl(t + RB_SLAB);
     }
-    if (dw) {
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        bf16x8_t x[CB];
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) x[cb] = fr.read(xs + (buf * 8 + wave) * C::X_BYTES + cb * 2048, 0, ks);
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int k = 0; k < 3; ++k) {
-            const bf16x8_t v = read_pl(pl + (k * NT + j) * BLK, 2 * th + ks);
-#pragma unroll
-            for (int cb = 0; cb < CB; ++cb) acc[j][cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, x[cb], acc[j][cb], 0, 0, 0);
-          }
-      }
-    }
+    // dX first: its stores are on their way while dWr multiplies
     if (dx) {
       f32x16_t o[CB];
 #pragma unroll
@@ -585,6 +570,22 @@ template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(Router
       for (int cb = 0; cb < CB; ++cb) {
         const int c = c0 + 32 * cb + 16 * h;
         if (r < t1) put_dx((bf16*)a.dX + (size_t)r * a.d + c, a.d - c, a.acc_dx, o[cb]);
+      }
+    }
+    if (dw) {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        bf16x8_t x[CB];
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) x[cb] = fr.read(xs + (buf * 8 + wave) * C::X_BYTES + cb * 2048, 0, ks);
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int k = 0; k < 3; ++k) {
+            const bf16x8_t v = read_pl(pl + (k * NT + j) * BLK, 2 * th + ks);
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) acc[j][cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, x[cb], acc[j][cb], 0, 0, 0);
+          }
       }
     }
   }

@@ -86,15 +86,58 @@ __device__ __forceinline__ uint32_t quantize128(const float (&v)[8], int q, uint
   return byte == 255 ? 0u : mx_codes8(v, mx_inv(byte));
 }
 
+// x of another lane of the quad.
+template <int CTRL> __device__ __forceinline__ uint32_t quad_u(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, false);
+}
+
+// quantize128 of bf16 as they lie in memory: magnitudes compare as 16-bit integers, and
+// the conversion takes pairs and the scale itself (a power of two that is no subnormal).
+__device__ __forceinline__ uint32_t quantize128(const u32x4_t& x, int q, uint32_t& scales) {
+  typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+  auto mag = [&](int i) { return __builtin_bit_cast(u16x2_t, x[i] & 0x7FFF7FFFu); };
+  const u16x2_t m = __builtin_elementwise_max(__builtin_elementwise_max(mag(0), mag(1)), __builtin_elementwise_max(mag(2), mag(3)));
+  uint32_t top = max((uint32_t)m[0], (uint32_t)m[1]) << 16;
+  top = max(top, quad_u<0xB1>(top));   // quad_perm [1, 0, 3, 2]
+  top = max(top, quad_u<0x4E>(top));   // quad_perm [2, 3, 0, 1]
+  const uint32_t byte = mx_byte(top);
+  uint32_t s = byte << (8 * (q >> 2));
+  s |= (uint32_t)__shfl_xor((int)s, 4);
+  s |= (uint32_t)__shfl_xor((int)s, 8);
+  scales = s;
+  if (byte == 255) return 0u;
+  if (byte == 0) {
+    float v[8];
+    unpack16(x, v, (bf16*)nullptr);
+    return mx_codes8(v, mx_inv(0));
+  }
+  const float f = __uint_as_float(byte << 23);
+  auto pair = [&](int i) {
+    const uint32_t w = x[i];   // (a bit cast of the vector's element itself takes element 0)
+    return __builtin_bit_cast(bf16x2_t, w);
+  };
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, pair(0), f, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, pair(1), f, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, pair(2), f, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, pair(3), f, 3);
+}
+
 // Columns [128 blk, 128 blk + 128) of a row to memory; codes up to column code_cols.
 template <typename T>
 __device__ __forceinline__ void quantize_row(const T* row, int cols, int blk, int q, int code_cols, uint8_t* codes,
                                              uint8_t* scale) {
   const int c = blk * 128 + q * 8;
-  float v[8];
-  load8(row, c, cols, v);
-  uint32_t s;
-  const uint32_t code = quantize128(v, q, s);
+  uint32_t s, code;
+  if constexpr (sizeof(T) == 2) {
+    u32x4_t x = {0, 0, 0, 0};
+    if (c < cols) x = ld16(row + c);
+    code = quantize128(x, q, s);
+  } else {
+    float v[8];
+    load8(row, c, cols, v);
+    code = quantize128(v, q, s);
+  }
   if (c < code_cols) *(FM_GLOBAL uint32_t*)(codes + c / 2) = code;
   if (q == 0) *(FM_GLOBAL uint32_t*)(scale + blk * 4) = s;
 }
@@ -125,14 +168,28 @@ __global__ __launch_bounds__(256) void k_dequant_mx(const uint8_t* __restrict__ 
   const uint32_t r = item / n8, c = (item - r * n8) * 8;
   const uint32_t code = *(const FM_GLOBAL uint32_t*)(codes + (size_t)r * (up32(cols) / 2) + c / 2);
   const uint32_t byte = scale[(size_t)r * (up128(cols) / 32) + c / 32];
-  // 2^(byte - 127): below 2^-126 a subnormal; 255 is NaN
-  const float s = byte == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float(byte ? byte << 23 : 0x00400000u);
-  float v[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = mx_value(code >> (4 * i)) * s;
   T* o = out + (size_t)r * cols + c;
-  st16(o, pack16(v, (T*)nullptr));
-  if constexpr (sizeof(T) == 4) st16(o + 4, pack16(v + 4, (T*)nullptr));
+  if (byte == 255 || byte == 0) {   // NaN, or a scale that is a subnormal
+    const float s = __uint_as_float(byte ? 0x7FC00000u : 0x00400000u);
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = mx_value(code >> (4 * i)) * s;
+    st16(o, pack16(v, (T*)nullptr));
+    if constexpr (sizeof(T) == 4) st16(o + 4, pack16(v + 4, (T*)nullptr));
+    return;
+  }
+  const float s = __uint_as_float(byte << 23);
+  if constexpr (sizeof(T) == 2) {
+    auto pair = [](bf16x2_t v) { return __builtin_bit_cast(uint32_t, v); };
+    st16(o, u32x4_t{pair(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 0)), pair(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 1)),
+                    pair(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 2)), pair(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 3))});
+  } else {
+    auto put = [&](int i, f32x2_t a, f32x2_t b) {
+      st16(o + i, u32x4_t{__float_as_uint(a[0]), __float_as_uint(a[1]), __float_as_uint(b[0]), __float_as_uint(b[1])});
+    };
+    put(0, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 1));
+    put(4, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 3));
+  }
 }
 
 // ------------------------------------------------------- grouped products ----
@@ -556,7 +613,8 @@ template <class C, class HALF, bool DOWN> __global__ __launch_bounds__(64 * C::N
 
 typedef MxCfg<256, 256, 4, 1> M256;
 typedef MxCfg<128, 256, 4, 1> M128;
-typedef MxCfg<64, 128, 2, 2> M64;
+typedef MxCfg<128, 128, 2, 2> Q128;
+typedef MxCfg<64, 128, 2, 2> Q64;
 
 // --------------------------------------------------------- a few tokens ----
 // Calls of a few tokens are bound by latency and by the weights' bytes, which have to be
@@ -766,15 +824,16 @@ bool mx_few_tokens(const moe_layer_mx4* L, int T, long active) {
   return T <= MX_FEW && active * (L->I / 8) <= 2048 && (long)L->d * L->I >= 1 << 20 &&
          T * mx_few_row_bytes(up128(L->d) / 128) <= 56 * 1024 && T * mx_few_row_bytes(up128(L->I) / 128) <= 52 * 1024;
 }
-// Whether it takes 256-row tiles, one block of 8 waves per compute unit, rather than
-// 64-row ones, two of 4 waves: with many rows per slot (each byte of weights feeds more
-// MFMAs) that make tiles enough.  us of 64 and 256-row tiles: the first layer above 700
-// tokens (175 rows per slot, 113 tiles) 56, 71; 1500 (375, 188) 100, 85; 4096 217, 173;
-// the second 333 tokens (35 rows) 90, 110; 700 (74, 551 tiles) 121, 127; 1500 (159, 812) 199, 173;
-// 4096 412, 314; the third 4096 tokens (1024, 72 tiles) 23, 27.
+// Whether it takes 256 x 256 tiles, one block of 8 waves per compute unit, rather than
+// 128 x 128 ones (64 x 128 where few rows are left), two of 4 waves, whose blocks run
+// over each other's tile boundaries but request twice as much per MFMA: with very many
+// rows per slot.  us of the small and the large tiles: d = 4096, I = 1024, 64 slots, top-8:
+// 2048 rows per slot 1421, 1273; 512 401, 403; the first layer above at 375 rows per
+// slot 80, 81; 175 46, 54; 83 38, 35; the second at 384 297, 298; 159 145, 166; 74 102, 114;
+// the third at 8192 58, 68.
 bool mx_large_tiles(const moe_layer_mx4* L, int T, int k, long active) {
   const double r = (double)T * (k + L->S_shared) / active;
-  return r >= 100 && active * (r / 256 + 0.5) * ((L->I + 127) / 128) >= 150;
+  return r >= 1000 && active * (r / 256 + 0.5) * ((L->I + 127) / 128) >= 1024;
 }
 
 // BPC blocks per compute unit, a multiple of the XCDs, at most one per tile.
@@ -909,6 +968,6 @@ extern "C" int moe_grouped_swiglu_fwd_mx4(const moe_layer_mx4* L, const void* X,
     return check_launch("moe_grouped_swiglu_fwd_mx4");
   }
   if (mx_large_tiles(L, T, k, active)) mx_tiles<M256, M128>(a, Xb, st);
-  else mx_tiles<M64, M64>(a, Xb, st);
+  else mx_tiles<Q128, Q64>(a, Xb, st);
   return check_launch("moe_grouped_swiglu_fwd_mx4");
 }
