@@ -15,6 +15,8 @@
  *           16-byte aligned (MOE_ERR_ALIGN otherwise).  The library allocates
  *           nothing: calls that need scratch take (ws, ws_bytes), sized by the
  *           matching *_workspace_size() function; too small -> MOE_ERR_WORKSPACE.
+ *           A workspace serves one call at a time: calls in flight on two streams
+ *           need one each, calls in a row on a stream may share one.
  * Streams.  `stream` is a hipStream_t passed as void* (NULL = default stream).
  *           Every call only enqueues work on it and returns; nothing
  *           synchronises the host.  The library keeps no state between calls.
@@ -116,8 +118,8 @@ int moe_route_bwd(const float* gate, const int32_t* idx, const float* dgate, con
  * T tokens, B = 1.  keep [T] uint8 or NULL (all): tokens with 0 (padding) are
  * left out, and their logits are not looked at.  counts [B,E] int32, dprob
  * [B,E] fp32 and loss [1] fp32 are overwritten, also when T == 0.
- * coef finite; 1 <= B <= 4096; E and k as for moe_route_topk.  Sums over tokens run
- * in a fixed order (fp32 within at most 64 tokens, fp64 above).
+ * coef finite; 1 <= B <= 4096; T <= 2^30; E and k as for moe_route_topk.  Sums over
+ * tokens run in a fixed order (fp32 within 32 tokens, fp64 above).
  */
 int moe_balance_loss(const float* logits, const int32_t* idx, const int32_t* seg, const uint8_t* keep,
                      int T, int E, int k, int B, float coef,
@@ -148,7 +150,7 @@ int moe_balance_loss_bwd(const float* logits, const float* dprob, const float* d
  * Each output may be NULL (not formed); X is read for dWr only, Wr for dX only
  * (NULL where unused).  Sums in fp32, in a fixed order; dlogits keep 24 bits
  * in dWr and 16 in a bf16 dX.  With T == 0, dWr and dbias become 0 unless accumulating.
- * X [T,d] and Wr [E,d] in dtype; dlogits [T,E] fp32.  dX may not alias X.
+ * X [T,d] and Wr [E,d] in dtype; dlogits [T,E] fp32.  dX may not alias X.  T <= 2^30.
  */
 int moe_router_bwd(const float* dlogits, const void* X, const void* Wr, int dtype, int T, int d, int E,
                    void* dX, int accumulate_dx, float* dWr, float* dbias, int accumulate_dw,

@@ -22,6 +22,7 @@ namespace {
 
 constexpr int BAL_C = 32;        // tokens per block of the first pass
 constexpr int BAL_MAX_B = 4096;  // sequences
+constexpr int BAL_MAX_T = 1 << 30;   // tokens: a block's first token and its end are 32-bit
 
 template <int G> __device__ __forceinline__ float group_sum(float v) {
 #pragma unroll
@@ -782,6 +783,7 @@ void launch_router_bwd(const RouterBwd& a, bool is_bf16, int splits, hipStream_t
 int check_balance_shape(int T, int E, int B, const void* seg) {
   if (T < 0 || E <= 0 || B <= 0) return fail(MOE_ERR_ARG, "T=%d E=%d B=%d", T, E, B);
   if (E > 256) return fail(MOE_ERR_UNSUPPORTED, "E=%d > 256", E);
+  if (T > BAL_MAX_T) return fail(MOE_ERR_UNSUPPORTED, "T=%d > 2^30", T);
   if (B > BAL_MAX_B) return fail(MOE_ERR_UNSUPPORTED, "B=%d > %d", B, BAL_MAX_B);
   if (!seg && B != 1) return fail(MOE_ERR_ARG, "B=%d without seg", B);
   return MOE_OK;
@@ -863,6 +865,7 @@ extern "C" int moe_router_bwd(const float* dlogits, const void* X, const void* W
   FM_TRY(need_dtype_float(dtype, "dtype"));
   if (T < 0 || d <= 0 || E <= 0) return fail(MOE_ERR_ARG, "T=%d d=%d E=%d", T, d, E);
   if (E > 256) return fail(MOE_ERR_UNSUPPORTED, "E=%d > 256", E);
+  if (T > BAL_MAX_T) return fail(MOE_ERR_UNSUPPORTED, "T=%d > 2^30", T);
   if (d % 8) return fail(MOE_ERR_UNSUPPORTED, "d=%d not a multiple of 8", d);
   if (T > 0) {
     FM_TRY(need(dlogits, "dlogits"));

@@ -858,7 +858,7 @@ template <class C, class HALF> void mx_tiles(const MxArgs& a, const bf16* X, hip
 int check_rows(const void* a, const char* an, const void* b, const char* bn, const void* c, const char* cn, long rows,
                int cols) {
   if (rows <= 0 || cols <= 0) return fail(MOE_ERR_ARG, "rows=%ld cols=%d", rows, cols);
-  if (cols % 8) return fail(MOE_ERR_UNSUPPORTED, "cols=%d not a multiple of 8", cols);
+  if (cols % 8 || cols > 1 << 30) return fail(MOE_ERR_UNSUPPORTED, "cols=%d not a multiple of 8 up to 2^30", cols);
   FM_TRY(need(a, an)); FM_TRY(need(b, bn)); FM_TRY(need(c, cn));
   FM_TRY(need_aligned(a, an)); FM_TRY(need_aligned(b, bn)); FM_TRY(need_aligned(c, cn));
   return MOE_OK;
@@ -927,7 +927,8 @@ extern "C" int moe_grouped_swiglu_fwd_mx4(const moe_layer_mx4* L, const void* X,
   clear_error();
   if (!L) return fail(MOE_ERR_ARG, "layer must not be NULL");
   if (L->d <= 0 || L->I <= 0) return fail(MOE_ERR_ARG, "layer d=%d I=%d", L->d, L->I);
-  if (L->d % 8 || L->I % 8) return fail(MOE_ERR_UNSUPPORTED, "4-bit layer d=%d I=%d must be multiples of 8", L->d, L->I);
+  if (L->d % 8 || L->I % 8 || L->d > 1 << 30 || L->I > 1 << 30)
+    return fail(MOE_ERR_UNSUPPORTED, "4-bit layer d=%d I=%d must be multiples of 8 up to 2^30", L->d, L->I);
   if (L->S_routed < 0 || L->S_shared < 0 || L->S_routed + L->S_shared < 1 || L->S_routed > 512 || L->S_shared > 511)
     return fail(MOE_ERR_ARG, "layer S_routed=%d S_shared=%d", L->S_routed, L->S_shared);
   // byte offsets within a matrix, and of a token's packed row, are 32 bits wide

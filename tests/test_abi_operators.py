@@ -52,6 +52,7 @@ BAD = [
     ("moe_balance_loss", BALANCE, dict(E=257), UNS, "E=257"),
     ("moe_balance_loss", BALANCE, dict(E=64, k=17), UNS, "k=17"),
     ("moe_balance_loss", BALANCE, dict(T=-1), ARG, "T=-1"),
+    ("moe_balance_loss", BALANCE, dict(T=(1 << 30) + 1), UNS, "2^30"),
     ("moe_balance_loss", BALANCE, dict(B=2), ARG, "without seg"),
     ("moe_balance_loss", BALANCE, dict(B=0), ARG, "B=0"),
     ("moe_balance_loss", BALANCE, dict(seg=FAKE, B=4097), UNS, "B=4097"),
@@ -67,6 +68,7 @@ BAD = [
     ("moe_balance_loss_bwd", DLOGITS, dict(out=MIS), ALI, "dlogits"),
     ("moe_balance_loss_bwd", DLOGITS, dict(E=300), UNS, "E=300"),
     ("moe_router_bwd", ROUTER, dict(d=60), UNS, "d=60"),
+    ("moe_router_bwd", ROUTER, dict(T=2147483647, d=8), UNS, "2^30"),
     ("moe_router_bwd", ROUTER, dict(dtype=api.MOE_I8), UNS, "dtype"),
     ("moe_router_bwd", ROUTER, dict(Wr=None), ARG, "Wr"),
     ("moe_router_bwd", ROUTER, dict(X=None), ARG, "X"),
@@ -94,6 +96,7 @@ BAD = [
     ("moe_sublayer_norm_bwd", NORM_BWD, dict(dw_pre=MIS), ALI, "dw_pre"),
     ("moe_quantize_mxfp4", QUANT, dict(cols=12), UNS, "cols=12"),
     ("moe_quantize_mxfp4", QUANT, dict(rows=0), ARG, "rows=0"),
+    ("moe_quantize_mxfp4", QUANT, dict(cols=2147483640), UNS, "2^30"),
     ("moe_quantize_mxfp4", QUANT, dict(dtype=api.MOE_I8), UNS, "dtype"),
     ("moe_quantize_mxfp4", QUANT, dict(scale=None), ARG, "scale"),
     ("moe_quantize_mxfp4", QUANT, dict(codes=MIS), ALI, "codes"),
@@ -135,6 +138,7 @@ def mx4(L, layer=(), **over):
 
 @pytest.mark.parametrize("layer,over,code,word", [
     (dict(d=60), {}, UNS, "d=60"),
+    (dict(d=2147483640, I=8), {}, UNS, "2^30"),
     (dict(I=0), {}, ARG, "I=0"),
     (dict(d=1 << 20, I=1 << 13), {}, UNS, "2^32 weights"),
     (dict(S_routed=513), {}, ARG, "S_routed=513"),
