@@ -556,8 +556,12 @@ template <class C> __device__ __forceinline__ void mx_gate_up_tile(const MxArgs&
   }
 }
 
-// O = MX(H) Qd^T of one tile, RB columns.
-template <class C> __device__ __forceinline__ void mx_down_tile(const MxArgs& a, FM_LDS char* lds, const MxRows& r) {
+// O = MX(H) Qd^T of one tile, RB columns.  A wave's 32 rows x 64 columns go out through
+// LDS, so that a store covers whole lines of 8 rows (from the registers it touched 32
+// rows, 16 bytes of each).  stage: 4 KB per wave that the next tile's first slab and
+// scales leave alone, whichever its height.
+template <class C>
+__device__ __forceinline__ void mx_down_tile(const MxArgs& a, FM_LDS char* lds, FM_LDS char* stage, const MxRows& r) {
   const RowArgs& ra = a.ra;
   const int d = ra.d, nI = act_blocks(ra.I), n0 = r.n * C::RB;
   MxTile t;
@@ -575,25 +579,34 @@ template <class C> __device__ __forceinline__ void mx_down_tile(const MxArgs& a,
   f32x16_t acc[C::MI][C::NJ];
   mx_gemm<C, false>(t, lds, acc);
   const int lane = lane_id_here(), wave = wave_id(), h = lane >> 5;
+  FM_LDS char* const mine = stage + wave * 4096;   // [32 rows][8 chunks of 16 bytes], chunks swizzled by the row
+  const int m = lane & 31, col = n0 + (wave >> 1) * C::TN + 8 * (lane & 7);
 #pragma unroll
   for (int i = 0; i < C::MI; ++i) {
-    const int row = (wave & 1) * C::TM + 32 * i + (lane & 31);
 #pragma unroll
-    for (int j = 0; j < C::NJ; ++j) {
-      const int col = n0 + (wave >> 1) * C::TN + 32 * j + 16 * h;
+    for (int j = 0; j < C::NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 16; e += 8) {
         float v[8];
 #pragma unroll
         for (int x = 0; x < 8; ++x) v[x] = acc[i][j][e + x];
-        if (row < r.rows && col + e < d) st16(a.O + (r.ob + row) * d + col + e, pack16(v, (bf16*)nullptr));
+        *(FM_LDS u32x4_t*)(mine + m * 128 + (((4 * j + 2 * h + e / 8) ^ (m & 7)) << 4)) = pack16(v, (bf16*)nullptr);
       }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int q = 8 * u + (lane >> 3), row = (wave & 1) * C::TM + 32 * i + q;
+      const u32x4_t v = *(const FM_LDS u32x4_t*)(mine + q * 128 + (((lane & 7) ^ (q & 7)) << 4));
+      if (row < r.rows && col < d) st16(a.O + (r.ob + row) * d + col, v);
     }
   }
 }
 
-template <class C, bool DOWN> __device__ __forceinline__ void mx_tile(const MxArgs& a, FM_LDS char* lds, const MxRows& r) {
-  if constexpr (DOWN) mx_down_tile<C>(a, lds, r);
+template <class C, class BIG, bool DOWN>
+__device__ __forceinline__ void mx_tile(const MxArgs& a, FM_LDS char* lds, const MxRows& r) {
+  // the first 4 KB per wave behind the larger tile's first slab: inside the second slab
+  // of either height, which the next tile requests only behind its first barrier
+  static_assert(BIG::SLAB + BIG::NW * 4096 <= 2 * C::SLAB, "stage");
+  if constexpr (DOWN) mx_down_tile<C>(a, lds, lds + BIG::SLAB, r);
   else mx_gate_up_tile<C>(a, lds, r);
 }
 
@@ -606,8 +619,8 @@ template <class C, class HALF, bool DOWN> __global__ __launch_bounds__(64 * C::N
   const MxWalk walk = mx_walk(a.ra, NT);
   for (int tt = walk.at; tt < walk.end; tt += walk.step) {
     const MxRows r = mx_rows(a.ra, tt, NT, C::RA);
-    if (HALF::RA < C::RA && r.rows <= HALF::RA) mx_tile<HALF, DOWN>(a, lds, r);
-    else mx_tile<C, DOWN>(a, lds, r);
+    if (r.rows <= HALF::RA) mx_tile<HALF, C, DOWN>(a, lds, r);
+    else mx_tile<C, C, DOWN>(a, lds, r);
   }
 }
 
