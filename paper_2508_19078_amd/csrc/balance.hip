@@ -399,22 +399,14 @@ struct RouterBwd {
   int span;              // tokens per split, a multiple of RB_SLAB
 };
 
-// The old dX of a lane's 16 columns plus r, or r alone, to dX.
-template <typename T> __device__ __forceinline__ void put_dx(T* o, int cols, bool add, const f32x16_t& acc) {
-  constexpr int V = 16 / sizeof(T);
+// The old dX of a lane's 16 columns plus the sums, or these alone, to dX (fp32).
+__device__ __forceinline__ void put_dx(float* o, int cols, bool add, const f32x16_t& acc) {
 #pragma unroll
-  for (int i = 0; i < 16; i += V) {
+  for (int i = 0; i < 16; i += 4) {
     if (i >= cols) continue;
-    float r[V];
-#pragma unroll
-    for (int x = 0; x < V; ++x) r[x] = acc[i + x];
-    if (add) {
-      float old[V];
-      unpack16(ld16(o + i), old, (T*)nullptr);
-#pragma unroll
-      for (int x = 0; x < V; ++x) r[x] += old[x];
-    }
-    st16(o + i, pack16(r, (T*)nullptr));
+    f32x4_t r = {acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
+    if (add) r += load4(o + i);
+    store4(o + i, r);
   }
 }
 
@@ -440,7 +432,8 @@ template <int NT> struct RouterTile {
   static constexpr int CB = NT <= 2 ? 2 : 1, COLS = 128 * CB;
   static constexpr int X_BYTES = CB * 32 * 64;         // a wave's part of a slab, [CB][32 tokens][32 columns]
   static constexpr int BLK = RB_SLAB * 64;             // a plane's [64 tokens][32 experts]
-  static constexpr int LDS = 2 * 8 * X_BYTES + 3 * NT * BLK;
+  static constexpr int OUT = 32 * CB * 32 * 4;         // a wave's dX tile, fp32
+  static constexpr int LDS = 2 * 8 * X_BYTES + 3 * NT * BLK + 8 * OUT;
   static_assert(LDS <= 160 * 1024 && 4 * NT * CB * 4096 <= LDS, "slab, and half of the sums");
 };
 template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(RouterBwd a) {
@@ -449,6 +442,7 @@ template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(Router
   __shared__ __align__(16) char lds_[C::LDS];
   FM_LDS char* const xs = (FM_LDS char*)lds_;
   FM_LDS char* const pl = xs + 2 * 8 * C::X_BYTES;
+  FM_LDS char* const out = pl + 3 * NT * BLK + wave_id() * C::OUT;
   const int lane = lane_id(), wave = wave_id(), m = lane & 31, h = lane >> 5, th = wave >> 2;
   const int ct = (a.d + C::COLS - 1) / C::COLS, split = blockIdx.x / ct;
   const int c0 = (blockIdx.x % ct) * C::COLS + (wave & 3) * 32 * CB;
@@ -566,11 +560,35 @@ template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(Router
 #pragma unroll
           for (int cb = 0; cb < CB; ++cb) o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[cb][s], v, o[cb], 0, 0, 0);
         }
-      const int r = t + 32 * th + m;
+      // out through LDS, whole lines of a row at once: [32 tokens][32 CB fp32], chunks
+      // of 16 bytes swizzled by the row
+      constexpr int CH = 8 * CB, PIECES = 4 * CB;   // chunks of a row, 16-byte pieces of it in bf16
 #pragma unroll
-      for (int cb = 0; cb < CB; ++cb) {
-        const int c = c0 + 32 * cb + 16 * h;
-        if (r < t1) put_dx((bf16*)a.dX + (size_t)r * a.d + c, a.d - c, a.acc_dx, o[cb]);
+      for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *(FM_LDS f32x4_t*)(out + m * (CH * 16) + (((8 * cb + 4 * h + q) ^ (m & (CH - 1))) << 4)) =
+              f32x4_t{o[cb][4 * q], o[cb][4 * q + 1], o[cb][4 * q + 2], o[cb][4 * q + 3]};
+#pragma unroll
+      for (int u = 0; u < PIECES / 2; ++u) {
+        const int q = (64 / PIECES) * u + lane / PIECES, pc = lane % PIECES;
+        const int r = t + 32 * th + q, c = c0 + 8 * pc;
+        float v[8];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const f32x4_t w = *(const FM_LDS f32x4_t*)(out + q * (CH * 16) + (((2 * pc + x) ^ (q & (CH - 1))) << 4));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[4 * x + e] = w[e];
+        }
+        if (r >= t1 || c >= a.d) continue;
+        bf16* const at = (bf16*)a.dX + (size_t)r * a.d + c;
+        if (a.acc_dx) {
+          float old[8];
+          unpack16(ld16(at), old, (bf16*)nullptr);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] += old[e];
+        }
+        st16(at, pack16(v, (bf16*)nullptr));
       }
     }
     if (dw) {
