@@ -773,13 +773,22 @@ __global__ __launch_bounds__(256) void k_router_dw(const float* __restrict__ par
 
 // Columns of a block.
 inline int router_cols(int E, bool is_bf16) { return is_bf16 && E <= 64 ? 256 : 128; }
-// Parts of the token range: blocks of 8 waves for every compute unit (bf16; fp32: two
-// of 4 waves), whole slabs in each.
-inline int router_splits(int T, int d, int E, bool is_bf16) {
-  const int slabs = cdiv(T, RB_SLAB);
-  int s = cdiv(is_bf16 ? 256 : 512, cdiv(d, router_cols(E, is_bf16)));
-  if (s > RB_SPLITS) s = RB_SPLITS;
-  return slabs < s ? slabs : s;
+// Parts of the token range, at most: blocks of 8 waves for every compute unit (bf16;
+// fp32: two of 4 waves).  Grows with T, so a workspace for T serves fewer tokens too.
+inline int router_most_parts(int T, int d, int E, bool is_bf16) {
+  const int s = cdiv(is_bf16 ? 256 : 512, cdiv(d, router_cols(E, is_bf16)));
+  const int most = s < RB_SPLITS ? s : RB_SPLITS, slabs = cdiv(T, RB_SLAB);
+  return slabs < most ? slabs : most;
+}
+// The parts: whole slabs in each, at least one.  A part without a slab would leave its
+// block with X still requested into the LDS that the sums pass through at its end.
+struct RouterParts {
+  int n, span;   // parts, tokens of each (the last may hold fewer)
+};
+inline RouterParts router_parts(int T, int d, int E, bool is_bf16) {
+  if (T == 0) return {0, 0};
+  const int slabs = cdiv(T, RB_SLAB), each = cdiv(slabs, router_most_parts(T, d, E, is_bf16));
+  return {cdiv(slabs, each), each * RB_SLAB};
 }
 // Floats between two parts: not a power of two, which would put the same place of all
 // parts on one memory channel.
@@ -872,7 +881,7 @@ extern "C" int moe_balance_loss_bwd(const float* logits, const float* dprob, con
 
 extern "C" size_t moe_router_bwd_workspace_size(int T, int d, int E) {
   if (T < 0 || d <= 0 || E <= 0) return 0;
-  const int a = router_splits(T, d, E, true), b = router_splits(T, d, E, false);   // for either type
+  const int a = router_most_parts(T, d, E, true), b = router_most_parts(T, d, E, false);   // for either type
   return (size_t)(a > b ? a : b) * (router_stride(d, E) + E) * sizeof(float);
 }
 
@@ -903,7 +912,7 @@ extern "C" int moe_router_bwd(const float* dlogits, const void* X, const void* W
   if (T == 0 && (!dw || accumulate_dw)) return MOE_OK;
   hipStream_t st = as_stream(stream);
   const bool is_bf16 = dtype == MOE_BF16;
-  const int splits = T > 0 ? router_splits(T, d, E, is_bf16) : 0;
+  const auto [splits, span] = router_parts(T, d, E, is_bf16);
   RouterBwd a{};
   a.dl = dlogits; a.X = dWr ? X : nullptr; a.Wr = Wr;
   a.Tn = T; a.d = d; a.E = E;
@@ -912,7 +921,7 @@ extern "C" int moe_router_bwd(const float* dlogits, const void* X, const void* W
   a.stride = router_stride(d, E);
   a.partb = dbias ? (float*)ws + (size_t)splits * a.stride : nullptr;
   if (T > 0) {
-    a.span = cdiv(cdiv(T, splits), RB_SLAB) * RB_SLAB;
+    a.span = span;
     launch_router_bwd(a, is_bf16, splits, st);
     FM_TRY(check_launch("moe_router_bwd"));
   }

@@ -207,3 +207,13 @@ def test_binding_refuses_tensors_it_would_misread():
         api.moe_sublayer_norm(t(4, 32)[:, ::2], None, t(4, 16), None)
     with pytest.raises(api.MoeError, match="aligned"):
         api.moe_sublayer_norm(t(4, 16), t(4, 16), t(4, 16), None, gate=t(5)[1:])
+
+
+def test_workspaces_for_more_tokens_serve_fewer(L):
+    for d, E in ((264, 20), (2048, 64), (136, 130)):
+        sizes = [L.moe_router_bwd_workspace_size(T, d, E) for T in range(0, 6400, 32)]
+        assert sizes == sorted(sizes)
+        sizes = [L.moe_balance_loss_workspace_size(T, E, 4) for T in range(0, 6400, 16)]
+        assert sizes == sorted(sizes)
+        sizes = [L.moe_sublayer_norm_bwd_workspace_size(T, d) for T in range(0, 6400, 16)]
+        assert sizes == sorted(sizes)

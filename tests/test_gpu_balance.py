@@ -198,6 +198,14 @@ def test_router_backward(T, d, E, dt):
             assert all(v is None or torch.equal(v, out[n]) for n, v in part.items()), how
 
 
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,d,E", [(33 * 64, 264, 20), (33 * 64, 2048, 64), (35 * 64 + 1, 136, 130), (65 * 64, 512, 33)])
+def test_router_backward_slabs_that_do_not_divide(T, d, E, dt):
+    """More slabs of 64 tokens than parts of the token range, and no multiple of them:
+    whole slabs in each part leave fewer parts."""
+    test_router_backward(T, d, E, dt)
+
+
 def test_router_backward_without_tokens_and_sparse():
     e = torch.empty(0, 8, device=DEV)
     X = torch.empty(0, 16, device=DEV)
