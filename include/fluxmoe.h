@@ -234,7 +234,8 @@ int moe_rms_norm(const void* X, const void* Y, int T, int d, int dtype, float ep
  *   u = post_norm ? Y * rstd_y : Y      rstd_y[t] = 1 / sqrt(mean_i Y[t,i]^2 + eps)
  *   S = alpha * X + gate[t] * (u * w_post)              (fp32, one rounding)
  *   N = S * rstd_s * w_pre              rstd_s[t] = 1 / sqrt(mean_i S[t,i]^2 + eps)
- * (N from the rounded S, one rounding; a zero row with eps = 0 has rstd 0).
+ * (N from the rounded S, one rounding; a zero row with eps = 0 has rstd 0, and so
+ * has a row whose sum of squares passes fp32's range).
  * With post_norm = 0, w_post is a layer scale.  Y NULL: the pre-norm alone, S =
  * alpha * X; gate, w_post and rstd_y must then be NULL and post_norm 0.
  * X, Y, S, N [T,d] in dtype; gate [T], w_post, w_pre [d] fp32 or NULL (1);
