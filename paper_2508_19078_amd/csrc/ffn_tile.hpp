@@ -37,6 +37,10 @@ int q8_tile(const moe_layer_q8* L, int T, int k);
 void tile_fwd_q8(const moe_layer_q8* L, const void* X, const void* Xp, const int32_t* offsets, int T, int k, void* H,
                  void* O, hipStream_t st);
 
+// Rows of the 4-bit forward's row tile: 128 (64 where few are left) or 256 (128), or 0:
+// the kernels for a few tokens.
+int mx4_tile(const moe_layer_mx4* L, int T, int k);
+
 // One block per compute unit, rounded to the XCD count.
 int persistent_blocks();
 

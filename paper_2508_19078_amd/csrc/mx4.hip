@@ -28,6 +28,7 @@
 
 #include "debug.hpp"
 #include "ffn_common.hpp"
+#include "ffn_tile.hpp"
 #include "gemm_bf16.hpp"
 
 namespace fm {
@@ -886,7 +887,19 @@ int check_rows(const void* a, const char* an, const void* b, const char* bn, con
   return MOE_OK;
 }
 
+// Slots that may hold rows.
+long mx_active(const moe_layer_mx4* L, int T, int k) {
+  const long R = (long)T * k;
+  return (R < L->S_routed ? R : L->S_routed) + L->S_shared;
+}
+
 }  // namespace
+
+int mx4_tile(const moe_layer_mx4* L, int T, int k) {
+  const long active = mx_active(L, T, k);
+  return mx_few_tokens(L, T, active) ? 0 : mx_large_tiles(L, T, k, active) ? 256 : 128;
+}
+
 }  // namespace fm
 
 using namespace fm;
@@ -980,9 +993,9 @@ extern "C" int moe_grouped_swiglu_fwd_mx4(const moe_layer_mx4* L, const void* X,
   const MxArgs a{{L->q_gate, L->q_up, L->q_down, L->s_gate, L->s_up, L->s_down}, w, perm_token, ra, (bf16*)O};
   const int nb = up128(L->d) / 128;
   const bf16* const Xb = (const bf16*)X;
-  const long R = (long)T * k;
-  const long active = (R < L->S_routed ? R : L->S_routed) + L->S_shared;   // slots that may hold rows
-  if (mx_few_tokens(L, T, active)) {
+  const int tile = mx4_tile(L, T, k);
+  if (tile == 0) {
+    const long active = mx_active(L, T, k);
     const int ng = L->I / 8, nd = cdiv(L->d, 32);
     hipLaunchKernelGGL((k_mx_few_gate_up<4, 4>), dim3(active * ng), dim3(256), T * mx_few_row_bytes(nb) + 4 * 1024, st, a,
                        Xb, ng, T);
@@ -990,7 +1003,7 @@ extern "C" int moe_grouped_swiglu_fwd_mx4(const moe_layer_mx4* L, const void* X,
                        T * mx_few_row_bytes(up128(L->I) / 128) + 4 * 2048, st, a, nd, T);
     return check_launch("moe_grouped_swiglu_fwd_mx4");
   }
-  if (mx_large_tiles(L, T, k, active)) mx_tiles<M256, M128>(a, Xb, st);
+  if (tile == 256) mx_tiles<M256, M128>(a, Xb, st);
   else mx_tiles<Q128, Q64>(a, Xb, st);
   return check_launch("moe_grouped_swiglu_fwd_mx4");
 }
