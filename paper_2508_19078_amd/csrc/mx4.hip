@@ -910,8 +910,9 @@ extern "C" int moe_quantize_mxfp4(const void* W, int dtype, long rows, int cols,
   FM_TRY(need_dtype_float(dtype, "dtype"));
   FM_TRY(check_rows(W, "W", codes, "codes", scale, "scale", rows, cols));
   const int nb = up128(cols) / 128, es = esize(dtype);
-  // launches of at most 2^31 items, so that the kernel divides 32-bit numbers
-  const long step = 0x7FFFFFF0L / nb;
+  // launches of at most 2^27 items: 16 threads each, and a launch of 2^32 threads or more
+  // runs some of them only, without an error
+  const long step = (1L << 27) / nb;   // nb <= 2^23
   for (long r = 0; r < rows; r += step) {
     const uint32_t items = (uint32_t)((rows - r < step ? rows - r : step) * nb);
     const char* w = (const char*)W + (size_t)r * cols * es;
@@ -933,6 +934,7 @@ extern "C" int moe_dequant_mxfp4(const uint8_t* codes, const uint8_t* scale, lon
   FM_TRY(need_dtype_float(out_dtype, "out_dtype"));
   FM_TRY(check_rows(codes, "codes", scale, "scale", out, "out", rows, cols));
   const int n8 = cols / 8, es = esize(out_dtype);
+  // launches of less than 2^31 items, a thread each, so that the kernel divides 32-bit numbers
   const long step = 0x7FFFFFF0L / n8;
   for (long r = 0; r < rows; r += step) {
     const uint32_t items = (uint32_t)((rows - r < step ? rows - r : step) * n8);
