@@ -17,6 +17,7 @@
 // for the sequences, 8.3 for the logits' gradient (2 and 4 MB: all three are a launch
 // and chains of dependent loads and exchanges).  The first pass with its tokens one
 // after another, without LDS, took 25 us.
+#include <algorithm>
 #include <type_traits>
 
 #include "common.hpp"
@@ -28,6 +29,7 @@ namespace {
 constexpr int BAL_C = 32;        // tokens per block of the first pass
 constexpr int BAL_MAX_B = 4096;  // sequences
 constexpr int BAL_MAX_T = 1 << 30;   // tokens: a block's first token and its end are 32-bit
+constexpr int BAL_GRID = 1 << 23;    // blocks per launch: with 2^32 threads or more, some do not run
 
 template <int G> __device__ __forceinline__ float group_sum(float v) {
 #pragma unroll
@@ -116,15 +118,15 @@ struct BalArgs {
   int Tn, E, k, B;
 };
 
-template <int G, int NE> __global__ __launch_bounds__(256) void k_balance_rows(BalArgs a, BalWs w) {
+template <int G, int NE> __global__ __launch_bounds__(256) void k_balance_rows(BalArgs a, BalWs w, int block0) {
   constexpr int NG = 256 / G;              // groups per block
   constexpr int U = BAL_C > NG ? (BAL_C / NG < 4 ? BAL_C / NG : 4) : 1;   // tokens of a group in flight
   __shared__ float sp[BAL_C][G * NE];      // p of the block's tokens, 0 where not kept
   __shared__ int scnt[G * NE], skept[BAL_C];
   extern __shared__ int segs[];            // B + 1 when there are sequences
-  const int sub = threadIdx.x % G, grp = threadIdx.x / G;
-  const int t0 = min(blockIdx.x * BAL_C, a.Tn), nt = min(BAL_C, a.Tn - t0);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *w.done = 0;
+  const int sub = threadIdx.x % G, grp = threadIdx.x / G, block = block0 + (int)blockIdx.x;
+  const int t0 = min(block * BAL_C, a.Tn), nt = min(BAL_C, a.Tn - t0);
+  if (block == 0 && threadIdx.x == 0) *w.done = 0;
   if (a.seg)
     for (int i = threadIdx.x; i <= a.B; i += 256) segs[i] = seg_at(a.seg, i, a.Tn);
   // this thread's choices: every 256th of the block's
@@ -175,7 +177,7 @@ template <int G, int NE> __global__ __launch_bounds__(256) void k_balance_rows(B
 #pragma unroll
     for (int c = 0; c < MC; ++c)
       if (ct[c] >= s0 && ct[c] < s1 && (unsigned)ce[c] < (unsigned)a.E) atomicAdd(&scnt[ce[c]], 1);
-    const size_t slot = (size_t)blockIdx.x + b;
+    const size_t slot = (size_t)block + b;
     float s = 0.f;
     if ((int)threadIdx.x < a.E)
       for (int r = s0; r < s1; ++r) s += sp[r][threadIdx.x];
@@ -190,7 +192,7 @@ template <int G, int NE> __global__ __launch_bounds__(256) void k_balance_rows(B
     total += n;
     __syncthreads();   // scnt is read
   }
-  if (threadIdx.x == 0) w.blockn[blockIdx.x] = total;
+  if (threadIdx.x == 0) w.blockn[block] = total;
 }
 
 // One block per sequence: EP = E rounded up to a power of two, 1024 / EP groups of
@@ -287,7 +289,7 @@ struct DlogitArgs {
 // choices of a token lie in the group's first lanes and are dealt from there (E >
 // 64: k <= 16 of 64 lanes).
 template <int G, int NE> constexpr int dlogit_rows() { return G == 64 ? 2 : 1; }
-template <int G, int NE> __global__ __launch_bounds__(256) void k_balance_dlogits(DlogitArgs a) {
+template <int G, int NE> __global__ __launch_bounds__(256) void k_balance_dlogits(DlogitArgs a, int block0) {
   constexpr int NG = 256 / G, U = dlogit_rows<G, NE>();
   extern __shared__ int segs[];   // B + 1 when there are sequences
   const int sub = threadIdx.x % G, grp = threadIdx.x / G;
@@ -305,7 +307,7 @@ template <int G, int NE> __global__ __launch_bounds__(256) void k_balance_dlogit
   float gv[U], dv[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    t[u] = ((long)blockIdx.x * U + u) * NG + grp;
+    t[u] = (((long)block0 + blockIdx.x) * U + u) * NG + grp;
     const long tc = min(t[u], (long)a.Tn - 1);
     rows[u] = a.logits + (size_t)tc * a.E;
     in[u] = !a.keep || a.keep[tc];
@@ -857,7 +859,9 @@ extern "C" int moe_balance_loss(const float* logits, const int32_t* idx, const i
   const int nb = bal_blocks(T);
   with_expert_lanes(E, [&](auto l) {
     typedef decltype(l) L;
-    hipLaunchKernelGGL((k_balance_rows<L::G, L::NE>), dim3(nb), dim3(256), seg ? (B + 1) * sizeof(int) : 0, st, a, w);
+    for (int b0 = 0; b0 < nb; b0 += BAL_GRID)
+      hipLaunchKernelGGL((k_balance_rows<L::G, L::NE>), dim3(std::min(nb - b0, BAL_GRID)), dim3(256),
+                         seg ? (B + 1) * sizeof(int) : 0, st, a, w, b0);
   });
   FM_TRY(check_launch("moe_balance_loss"));
   int EP = 1;
@@ -883,8 +887,10 @@ extern "C" int moe_balance_loss_bwd(const float* logits, const float* dprob, con
   const DlogitArgs a{logits, dprob, dloss, seg, keep, gate, idx, dgate, T, E, k, B, dlogits};
   with_expert_lanes(E, [&](auto l) {
     typedef decltype(l) L;
-    hipLaunchKernelGGL((k_balance_dlogits<L::G, L::NE>), dim3(cdiv(T, dlogit_rows<L::G, L::NE>() * (256 / L::G))), dim3(256),
-                       seg ? (B + 1) * sizeof(int) : 0, as_stream(stream), a);
+    const int nb = cdiv(T, dlogit_rows<L::G, L::NE>() * (256 / L::G));
+    for (int b0 = 0; b0 < nb; b0 += BAL_GRID)
+      hipLaunchKernelGGL((k_balance_dlogits<L::G, L::NE>), dim3(std::min(nb - b0, BAL_GRID)), dim3(256),
+                         seg ? (B + 1) * sizeof(int) : 0, as_stream(stream), a, b0);
   });
   return check_launch("moe_balance_loss_bwd");
 }
