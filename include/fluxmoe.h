@@ -150,7 +150,8 @@ int moe_balance_loss_bwd(const float* logits, const float* dprob, const float* d
  * Each output may be NULL (not formed); X is read for dWr only, Wr for dX only
  * (NULL where unused).  Sums in fp32, in a fixed order; dlogits keep 24 bits
  * in dWr and 16 in a bf16 dX.  With T == 0, dWr and dbias become 0 unless accumulating.
- * X [T,d] and Wr [E,d] in dtype; dlogits [T,E] fp32.  dX may not alias X.  T <= 2^30.
+ * X [T,d] and Wr [E,d] in dtype; dlogits [T,E] fp32.  dX may not alias X.  T <= 2^30,
+ * E * d <= 2^30.
  */
 int moe_router_bwd(const float* dlogits, const void* X, const void* Wr, int dtype, int T, int d, int E,
                    void* dX, int accumulate_dx, float* dWr, float* dbias, int accumulate_dw,

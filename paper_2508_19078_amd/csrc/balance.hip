@@ -910,6 +910,8 @@ extern "C" int moe_router_bwd(const float* dlogits, const void* X, const void* W
   if (E > 256) return fail(MOE_ERR_UNSUPPORTED, "E=%d > 256", E);
   if (T > BAL_MAX_T) return fail(MOE_ERR_UNSUPPORTED, "T=%d > 2^30", T);
   if (d % 8) return fail(MOE_ERR_UNSUPPORTED, "d=%d not a multiple of 8", d);
+  // the sum of dWr's parts has a thread for each of its elements
+  if ((long)E * d > 1L << 30) return fail(MOE_ERR_UNSUPPORTED, "E=%d d=%d: more than 2^30 weights", E, d);
   if (T > 0) {
     FM_TRY(need(dlogits, "dlogits"));
     if (dX) FM_TRY(need(Wr, "Wr"));
