@@ -118,13 +118,16 @@ def lib() -> ctypes.CDLL:
             raise RuntimeError(f"{LIB_PATH} is missing: build it with "
                                "`python -m paper_2508_19078_amd.build` (hipcc, gfx950)")
         L = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in _SIGS.items():
-            fn = getattr(L, name)
-            fn.restype, fn.argtypes = res, args
+        rebuild = "rebuild it with `python -m paper_2508_19078_amd.build`"
         v = L.moe_abi_version()
         if v != ABI_VERSION:
-            raise RuntimeError(f"{LIB_PATH} has ABI version {v}, this binding marshals version {ABI_VERSION}: "
-                               "rebuild it with `python -m paper_2508_19078_amd.build`")
+            raise RuntimeError(f"{LIB_PATH} has ABI version {v}, this binding marshals version {ABI_VERSION}: {rebuild}")
+        for name, (res, args) in _SIGS.items():
+            # entry points are added within a version: a library built before one lacks it
+            fn = getattr(L, name, None)
+            if fn is None:
+                raise RuntimeError(f"{LIB_PATH} has no {name}: {rebuild}")
+            fn.restype, fn.argtypes = res, args
         _lib = L
     return _lib
 
