@@ -355,7 +355,9 @@ def moe_sublayer_norm_bwd(dS, dN, S, Y, rstd_s, dX, dY, ws, alpha=1.0, rstd_y=No
                           w_pre=None, post_norm=True, dgate=None, dw_post=None, dw_pre=None, accumulate_dw=False,
                           stream=None):
     """Backward of moe_sublayer_norm; outputs that are None are not formed."""
-    like = next(t for t in (dS, dN, S, Y) if t is not None)
+    like = next((t for t in (dS, dN, S, Y) if t is not None), None)
+    if like is None:
+        raise ValueError("dS, dN, S and Y must not all be None")
     T, d = td = like.shape
     dt, v = like.dtype, _device()
     code = dtype_code(dt)

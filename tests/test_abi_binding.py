@@ -27,3 +27,8 @@ def test_an_older_version_is_named_before_its_symbols_are_looked_up(tmp_path, mo
     monkeypatch.setattr(api, "_lib", None)
     with pytest.raises(RuntimeError, match=f"ABI version {api.ABI_VERSION - 1}.*rebuild it"):
         api.lib()
+
+
+def test_norm_backward_without_any_row():
+    with pytest.raises(ValueError, match="dS, dN, S and Y"):
+        api.moe_sublayer_norm_bwd(None, None, None, None, None, None, None, None)
