@@ -581,6 +581,7 @@ template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(Router
         for (int q = 0; q < 4; ++q)
           *(FM_LDS f32x4_t*)(out + m * (CH * 16) + (((8 * cb + 4 * h + q) ^ (m & (CH - 1))) << 4)) =
               f32x4_t{o[cb][4 * q], o[cb][4 * q + 1], o[cb][4 * q + 2], o[cb][4 * q + 3]};
+      wave_lds_fence();
 #pragma unroll
       for (int u = 0; u < PIECES / 2; ++u) {
         const int q = (64 / PIECES) * u + lane / PIECES, pc = lane % PIECES;
@@ -602,6 +603,7 @@ template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(Router
         }
         st16(at, pack16(v, (bf16*)nullptr));
       }
+      wave_lds_fence();   // the next slab's dX takes the place
     }
     if (dw) {
 #pragma unroll

@@ -143,6 +143,15 @@ __device__ __forceinline__ void st16(void* p, const u32x4_t& v) {
 // Wave64 helpers.
 __device__ __forceinline__ int lane_id() { return (int)(threadIdx.x & 63); }
 
+// Orders this wave's LDS accesses before it against those after it, so that a lane may
+// read what another lane of the wave wrote, or write over what one read.  The hardware
+// runs a wave's LDS instructions in order; this keeps the compiler to it, which looks at
+// each lane's own addresses only.  No instruction comes of it.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // (value desc, index asc) order used by every top-k: true if a ranks before b.
 __device__ __forceinline__ bool ranks_before(float va, int ia, float vb, int ib) {
   return va > vb || (va == vb && ia < ib);

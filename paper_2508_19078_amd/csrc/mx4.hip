@@ -598,12 +598,14 @@ __device__ __forceinline__ void mx_down_tile(const MxArgs& a, FM_LDS char* lds, 
         for (int x = 0; x < 8; ++x) v[x] = acc[i][j][e + x];
         *(FM_LDS u32x4_t*)(mine + m * 128 + (((4 * j + 2 * h + e / 8) ^ (m & 7)) << 4)) = pack16(v, (bf16*)nullptr);
       }
+    wave_lds_fence();
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int q = 8 * u + (lane >> 3), row = (wave & 1) * C::TM + 32 * i + q;
       const u32x4_t v = *(const FM_LDS u32x4_t*)(mine + q * 128 + (((lane & 7) ^ (q & 7)) << 4));
       if (row < r.rows && col < d) st16(a.O + (r.ob + row) * d + col, v);
     }
+    wave_lds_fence();
   }
 }
 
