@@ -376,8 +376,8 @@ template <typename Fn> void with_expert_lanes(int E, Fn fn) {
 //
 // bf16.  dlogits are fp32, the other operand is bf16: an fp32 value is the sum of
 // three bf16 (high, middle, low: 8 bits each), whose products with a bf16 are exact
-// in fp32, so dWr is three MFMAs with fp32 accuracy (v_mfma_f32_32x32x16_bf16, 16
-// times the rate of the fp32 MFMA) and dX, rounded to bf16 itself, two (16 bits).
+// in fp32, so dWr and dX are three MFMAs each with fp32 accuracy
+// (v_mfma_f32_32x32x16_bf16, 16 times the rate of the fp32 MFMA).
 // The three planes lie in LDS as [64 tokens][32 experts], X as [64 tokens][32 columns]
 // per wave: dWr sums over tokens and reads both transposed (ds_read_b64_tr_b16), dX
 // sums over experts and reads the planes along their rows (16-byte chunks of a row
@@ -565,7 +565,7 @@ template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(Router
 #pragma unroll
       for (int s = 0; s < 2 * NT; ++s)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < 3; ++k) {
           const FM_LDS char* const p = pl + (k * NT + (s >> 1)) * BLK + (32 * th + m) * 64 +
                                        (((2 * (s & 1) + h) ^ ((m >> 2) & 3)) << 4);
           const bf16x8_t v = __builtin_bit_cast(bf16x8_t, *(const FM_LDS u32x4_t*)p);
