@@ -377,7 +377,10 @@ template <typename Fn> void with_expert_lanes(int E, Fn fn) {
 // bf16.  dlogits are fp32, the other operand is bf16: an fp32 value is the sum of
 // three bf16 (high, middle, low: 8 bits each), whose products with a bf16 are exact
 // in fp32, so dWr and dX are three MFMAs each with fp32 accuracy
-// (v_mfma_f32_32x32x16_bf16, 16 times the rate of the fp32 MFMA).
+// (v_mfma_f32_32x32x16_bf16, 16 times the rate of the fp32 MFMA).  An infinity or NaN of X
+// meets the first part alone: a later one may be 0 where the sum is not, and 0 times it is
+// no number.  One of Wr is left to the stores, which add its products with the whole
+// dlogits: a second set of products beside the first took the registers of the sums.
 // The three planes lie in LDS as [64 tokens][32 experts], X as [64 tokens][32 columns]
 // per wave: dWr sums over tokens and reads both transposed (ds_read_b64_tr_b16), dX
 // sums over experts and reads the planes along their rows (16-byte chunks of a row
@@ -422,18 +425,38 @@ __device__ __forceinline__ void put_dx(float* o, int cols, bool add, const f32x1
   }
 }
 
-// a, b, c with a + b + c = v to 24 bits, each a bf16 (an infinity stays in a).
+// a + b + c = v exactly, each the upper half of an fp32 and so a bf16 (8 bits of v each,
+// one sign).  Cut off, not rounded: a finite v has finite parts, and an infinity is a.
 __device__ __forceinline__ void split3(f32x4_t v, u32x2_t (&p)[3]) {
-  float r[4] = {v[0], v[1], v[2], v[3]};
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(v[i]);
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
-    p[k] = u32x2_t{pk_bf16(r[0], r[1]), pk_bf16(r[2], r[3])};
+    p[k] = u32x2_t{r[0] >> 16 | (r[1] & 0xFFFF0000u), r[2] >> 16 | (r[3] & 0xFFFF0000u)};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float h = __uint_as_float(i & 1 ? p[k][i >> 1] & 0xFFFF0000u : p[k][i >> 1] << 16);
-      r[i] = fabsf(h) == INFINITY ? 0.f : r[i] - h;
+      const float f = __uint_as_float(r[i]);
+      r[i] = fabsf(f) == INFINITY ? 0u : __float_as_uint(f - __uint_as_float(r[i] & 0xFFFF0000u));
     }
   }
+}
+
+// The halves of x that are infinities or NaN as bits 15 and 31 of the result.
+__device__ __forceinline__ uint32_t none_bits(uint32_t x) { return ((x & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ bool has_none(const bf16x8_t& x) {
+  const u32x4_t v = __builtin_bit_cast(u32x4_t, x);
+  return (none_bits(v[0]) | none_bits(v[1]) | none_bits(v[2]) | none_bits(v[3])) != 0;
+}
+// x with `in` in their places, but with their signs.
+__device__ __forceinline__ bf16x8_t without_none(const bf16x8_t& x, uint32_t in) {
+  u32x4_t v = __builtin_bit_cast(u32x4_t, x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t at = (none_bits(v[i]) >> 15) * 0xFFFFu;
+    v[i] = (v[i] & (~at | 0x80008000u)) | (at & in);
+  }
+  return __builtin_bit_cast(bf16x8_t, v);
 }
 
 // NT = expert tiles of 32.  8 waves: wave w takes columns 32 CB (w % 4) + [0, 32 CB)
@@ -471,7 +494,7 @@ template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(Router
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
-        const int r = min(t + 32 * th + 16 * u + (lane >> 2), t1 - 1);   // a row past the end meets zero dlogits
+        const int r = min(t + 32 * th + 16 * u + (lane >> 2), t1 - 1);
         const int c = min(c0 + 32 * cb + 8 * (lane & 3), a.d - 8);
         dma16(X + (size_t)r * a.d + c, xs + (buf * 8 + wave) * C::X_BYTES + cb * 2048 + u * 1024);
       }
@@ -501,6 +524,7 @@ template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(Router
   load_dl(t0);
   // Wr: lane m's columns, experts 16 s + 8 h + [0, 8)
   bf16x8_t wf[CB][2 * NT];
+  bool wr_none = false;   // an infinity or NaN among the wave's: it takes part as 1 or -1 and is added at the end
   if (dx) {
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
@@ -515,8 +539,11 @@ template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(Router
           if (e >= a.E) v[i] = 0;
         }
         wf[cb][s] = __builtin_bit_cast(bf16x8_t, u32x4_t{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16});
+        wr_none |= has_none(wf[cb][s]);
+        wf[cb][s] = without_none(wf[cb][s], 0x3F803F80u);
       }
     }
+    wr_none = __ballot(wr_none) != 0;
   }
   f32x16_t acc[NT][CB];
 #pragma unroll
@@ -539,6 +566,14 @@ template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(Router
   int buf = 0;
   for (int t = t0; t < t1; t += RB_SLAB, buf ^= 1) {
     wait_vmcnt<0>();
+    if (dw && t + RB_SLAB > t1) {   // rows behind the last token: 0, not 0 times what stands there
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+          if (t + 32 * th + 16 * u + (lane >> 2) >= t1)
+            *(FM_LDS u32x4_t*)(xs + (buf * 8 + wave) * C::X_BYTES + cb * 2048 + u * 1024 + lane * 16) = u32x4_t{0, 0, 0, 0};
+    }
     __syncthreads();   // the planes of the last slab are read
 #pragma unroll
     for (int i = 0; i < QN; ++i) {
@@ -594,6 +629,16 @@ template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(Router
           for (int e = 0; e < 4; ++e) v[4 * x + e] = w[e];
         }
         if (r >= t1 || c >= a.d) continue;
+        if (wr_none) {   // rare: what Wr's infinities and NaN add
+          for (int e = 0; e < a.E; ++e) {
+            const float g = gptr(a.dl)[(size_t)r * a.E + e];
+            float w[8];
+            unpack16(ld16((const bf16*)a.Wr + (size_t)e * a.d + c), w, (bf16*)nullptr);
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+              if (!(fabsf(w[x]) < INFINITY)) v[x] = fmaf(g, w[x], v[x]);
+          }
+        }
         bf16* const at = (bf16*)a.dX + (size_t)r * a.d + c;
         if (a.acc_dx) {
           float old[8];
@@ -611,14 +656,23 @@ template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(Router
         bf16x8_t x[CB];
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) x[cb] = fr.read(xs + (buf * 8 + wave) * C::X_BYTES + cb * 2048, 0, ks);
+        bool none = false;
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int cb = 0; cb < CB; ++cb) none |= has_none(x[cb]);
+        none = __ballot(none) != 0;
 #pragma unroll
-          for (int k = 0; k < 3; ++k) {
+        for (int k = 0; k < 3; ++k) {
+          if (k == 1 && none) {
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) x[cb] = without_none(x[cb], 0u);
+          }
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
             const bf16x8_t v = read_pl(pl + (k * NT + j) * BLK, 2 * th + ks);
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) acc[j][cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, x[cb], acc[j][cb], 0, 0, 0);
           }
+        }
       }
     }
   }
@@ -693,6 +747,7 @@ template <int NT> __global__ __launch_bounds__(256) void k_router_f32(RouterBwd 
       for (int u = 0; u < U; ++u) {
         const int r = t + 2 * u + h, rc = min(r, t1 - 1);
         x[u] = a.X ? X[(size_t)rc * a.d + c] : 0.f;
+        if (r >= t1) x[u] = 0.f;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
           v[u][j] = dl[(size_t)rc * a.E + min(32 * j + m, a.E - 1)];

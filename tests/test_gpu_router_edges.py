@@ -9,6 +9,7 @@ import test_gpu_balance as B
 
 pytestmark = pytest.mark.gpu
 DEV, U = "cuda", 2.0 ** -24
+INF, NAN = float("inf"), float("nan")
 
 
 @pytest.mark.parametrize("T,d,E", [(70, 40, 4), (64, 2048, 64), (200, 136, 130)])
@@ -26,3 +27,48 @@ def test_dx_takes_all_bits_of_dlogits(T, d, E):
     want = a @ w
     tol = 12 * U * (np.abs(a) @ np.abs(w)) + 2.0 ** -8 * np.abs(want)
     assert np.all(np.abs(B.f64(out) - want) <= tol)
+
+
+def products(a, x):
+    """(sum_t a[t,i] x[t,j], the same of magnitudes), term by term in fp64."""
+    with np.errstate(invalid="ignore", over="ignore"):
+        p = a[:, :, None] * x[:, None, :]
+        return p.sum(0), np.abs(p).sum(0)
+
+
+def same(got, want, tol, what):
+    g = B.f64(got)
+    np.testing.assert_array_equal(np.isnan(g), np.isnan(want), err_msg=what)
+    inf = np.isinf(want)
+    np.testing.assert_array_equal(np.isinf(g), inf, err_msg=what)
+    np.testing.assert_array_equal(g[inf], want[inf], err_msg=what)
+    ok = np.isfinite(want)
+    assert np.all(np.abs(g[ok] - want[ok]) <= tol[ok]), what
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,d,E", [(65, 24, 5), (130, 136, 33), (150, 72, 130), (129, 264, 64)])
+def test_infinities_and_nan(T, d, E, dt):
+    """They reach what the formula says and nothing else: an infinity stays one (the fp32
+    dlogits are taken apart for bf16 products, and a part may be 0), and rows behind the
+    last token are no terms of the sum."""
+    g = torch.Generator().manual_seed(T + d)
+    dl, X, Wr = (torch.randn(s, generator=g) for s in ((T, E), (T, d), (E, d)))
+    dl[::3] = dl[::3].bfloat16().float()               # one part holds them
+    dl[dl == 0] = 0.5
+    X[10, 3], X[T - 1, 5], X[4, 9] = INF, -INF, NAN
+    X[20, 7], X[21, 7] = INF, -INF
+    Wr[0] *= 2.0 ** -10
+    Wr[2, 7], Wr[0, 8], Wr[3, 11] = INF, -INF, NAN
+    dl[6, 1], dl[7, 2], dl[8, 3] = INF, -INF, NAN
+    dl[9, 0], X[9] = torch.finfo(torch.float32).max, X[9] * 2.0 ** -20   # rounds to an infinity in 8 bits
+    X, Wr = X.to(dt), Wr.to(dt)
+    out = B.router(dl.to(DEV), X.to(DEV), Wr.to(DEV))
+    a, x, w = B.f64(dl), B.f64(X), B.f64(Wr)
+    want, mag = products(a, x)
+    with np.errstate(invalid="ignore"):
+        same(out["dWr"], want, (T + 40) * U * mag + U * np.abs(want), "dWr")
+        want, mag = products(a.T, w)
+        half = 2.0 ** -8 if dt == torch.bfloat16 else U
+        same(out["dX"], want, (E + 4) * U * mag + half * np.abs(want), "dX")
+        same(out["dbias"], a.sum(0), (T + 40) * U * np.abs(a).sum(0), "dbias")
