@@ -811,32 +811,34 @@ template <int NT> __global__ __launch_bounds__(256) void k_router_f32(RouterBwd 
 }
 
 // dWr and dbias from their parts: a block takes 64 quads of columns, its 4 groups of
-// threads every fourth part, and the groups' sums are added in order.
+// threads every fourth part, and the groups' sums are added in order.  In 64 bits: up to
+// 32 parts of many tokens each, which may nearly cancel.
 __global__ __launch_bounds__(256) void k_router_dw(const float* __restrict__ part, const float* __restrict__ partb,
                                                    int splits, long stride, long n, int E, int accumulate,
                                                    float* __restrict__ dWr,
                                                    float* __restrict__ dbias) {
-  __shared__ f32x4_t red[4][64];
+  typedef double f64x4_t __attribute__((ext_vector_type(4)));
+  __shared__ f64x4_t red[4][64];
   const int q = threadIdx.x & 63, g = threadIdx.x >> 6;
   const long i = ((long)blockIdx.x * 64 + q) * 4;
   if (dWr) {
-    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+    f64x4_t v = {0., 0., 0., 0.};
     if (i < n) {
 #pragma unroll 8
-      for (int p = g; p < splits; p += 4) v += load4(part + (size_t)p * stride + i);
+      for (int p = g; p < splits; p += 4) v += __builtin_convertvector(load4(part + (size_t)p * stride + i), f64x4_t);
     }
     red[g][q] = v;
     __syncthreads();
     if (g == 0 && i < n) {
       v = red[0][q] + red[1][q] + red[2][q] + red[3][q];
-      if (accumulate) v += load4(dWr + i);
-      store4(dWr + i, v);
+      if (accumulate) v += __builtin_convertvector(load4(dWr + i), f64x4_t);
+      store4(dWr + i, __builtin_convertvector(v, f32x4_t));
     }
   }
   if (dbias && blockIdx.x == 0 && threadIdx.x < (unsigned)E) {
-    float v = 0.f;
+    double v = accumulate ? dbias[threadIdx.x] : 0.;
     for (int p = 0; p < splits; ++p) v += partb[(size_t)p * E + threadIdx.x];
-    dbias[threadIdx.x] = accumulate ? dbias[threadIdx.x] + v : v;
+    dbias[threadIdx.x] = (float)v;
   }
 }
 

@@ -72,3 +72,17 @@ def test_infinities_and_nan(T, d, E, dt):
         half = 2.0 ** -8 if dt == torch.bfloat16 else U
         same(out["dX"], want, (E + 4) * U * mag + half * np.abs(want), "dX")
         same(out["dbias"], a.sum(0), (T + 40) * U * np.abs(a).sum(0), "dbias")
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_parts_of_the_tokens_add_up_in_64_bits(dt):
+    """One gradient in each slab of 64 tokens: 2^25, thirty times 1, -2^25.  The slabs lie
+    in different parts of the token range, whose sums meet in 64 bits: 30, exactly."""
+    T, d, E = 2048, 2048, 4
+    dl = torch.zeros(T, E, device=DEV)
+    dl[64:1984:64, 1] = 1.0
+    dl[0, 1], dl[T - 1, 1] = 2.0 ** 25, -2.0 ** 25
+    X = torch.ones(T, d, dtype=dt, device=DEV)
+    out = B.router(dl, X, torch.zeros(E, d, dtype=dt, device=DEV), dx=False)
+    assert bool((out["dWr"][1] == 30).all()) and out["dbias"].tolist() == [0, 30, 0, 0]
+    assert not out["dWr"][[0, 2, 3]].any()
