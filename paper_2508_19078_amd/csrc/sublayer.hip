@@ -296,19 +296,21 @@ __global__ __launch_bounds__(NT) void k_sublayer_bwd(NormBwd a) {
 
 // out[c] = (accumulate ? out[c] : 0) + the partial sums of column c: 32 columns per
 // block (8 quads), its 128 groups of threads every 128th block's sums, which are then
-// added pairwise.
+// added pairwise.  In 64 bits: up to 512 sums of many rows each, which may nearly cancel.
 __global__ __launch_bounds__(1024) void k_sublayer_dw(const float* __restrict__ part, int blocks, int d,
                                                       int accumulate, float* __restrict__ dw_post,
                                                       float* __restrict__ dw_pre) {
   typedef float f4 __attribute__((ext_vector_type(4)));
-  __shared__ f4 red[128][8];
+  typedef double d4 __attribute__((ext_vector_type(4)));
+  __shared__ d4 red[128][8];
   const int which = blockIdx.y, q = threadIdx.x & 7, grp = threadIdx.x >> 3, c = blockIdx.x * 32 + 4 * q;
   float* const out = which ? dw_pre : dw_post;
   if (!out) return;
-  f4 s = {0.f, 0.f, 0.f, 0.f};
+  d4 s = {0., 0., 0., 0.};
   if (c < d) {
 #pragma unroll 4
-    for (int b = grp; b < blocks; b += 128) s += *(const FM_GLOBAL f4*)(part + ((size_t)b * 2 + which) * d + c);
+    for (int b = grp; b < blocks; b += 128)
+      s += __builtin_convertvector(*(const FM_GLOBAL f4*)(part + ((size_t)b * 2 + which) * d + c), d4);
   }
   red[grp][q] = s;
 #pragma unroll
@@ -317,8 +319,8 @@ __global__ __launch_bounds__(1024) void k_sublayer_dw(const float* __restrict__ 
     if (grp < h) red[grp][q] = s += red[grp + h][q];
   }
   if (grp == 0 && c < d) {
-    if (accumulate) s += *(const FM_GLOBAL f4*)(out + c);
-    *(FM_GLOBAL f4*)(out + c) = s;
+    if (accumulate) s += __builtin_convertvector(*(const FM_GLOBAL f4*)(out + c), d4);
+    *(FM_GLOBAL f4*)(out + c) = __builtin_convertvector(s, f4);
   }
 }
 
