@@ -261,8 +261,8 @@ int moe_sublayer_norm(const void* X, const void* Y, const float* gate, const flo
  * as the forward had them.  Each of dX, dY [T,d] dtype, dgate [T], dw_post,
  * dw_pre [d] fp32 may be NULL (not formed); Y NULL: only dX and dw_pre.  dw_pre
  * without dN is 0.  accumulate_dw = 1 adds to dw_post and dw_pre.  dX and dY may
- * alias any of S, Y, dS, dN, not each other.  Row sums and the sums over a block's rows
- * run in fp32, the blocks' sums add up in fp64, all in a fixed order.  Limits as for moe_sublayer_norm; with T == 0, dw_* become
+ * alias any of S, Y, dS, dN, not each other.  Row sums run in fp32, the sums over the rows
+ * in fp64 (a block's sum is kept in fp32), all in a fixed order.  Limits as for moe_sublayer_norm; with T == 0, dw_* become
  * 0 unless accumulating.
  */
 int moe_sublayer_norm_bwd(const void* dS, const void* dN, const void* S, const void* Y, const float* gate,

@@ -8,9 +8,10 @@
 // (16 or 64 lanes of a wave, or the whole block), NCB chunks of 16 bytes each,
 // chunk i of thread r at column (r + i TPR) V; a block of NT threads walks groups
 // of NT / TPR rows, and the gains of a thread's columns stay in its registers over
-// all of them.  The backward keeps its sums for the gains' gradients there too and
-// leaves them, one row of partial sums per block, to a second launch that adds
-// them in a fixed order (no float atomics).
+// all of them.  The backward keeps its sums for the gains' gradients there too, in 64 bits
+// (in 32, the 64 rows of a block at 32768 tokens cost three times the error of one
+// rounding; the time grew by 1-2 %, by 5 % at d = 256), and leaves them, one row of partial sums per
+// block, to a second launch that adds them in a fixed order (no float atomics).
 //
 // Measured at 8192 rows of 2048 bf16, post-norm and gate: forward 23.5 us (134 MB, 5.7
 // TB/s), backward 37.5 us (201 MB, 5.4 TB/s) and 4.6 us for the second launch; 1023
@@ -163,14 +164,15 @@ __global__ __launch_bounds__(NT) void k_sublayer_bwd(NormBwd a) {
   const T *dS = (const T*)a.dS, *dN = (const T*)a.dN, *S = (const T*)a.S, *Y = (const T*)a.Y;
   T *dX = (T*)a.dX, *dY = (T*)a.dY;
   const u32x4_t zero = {0, 0, 0, 0};
-  float wq[NCB][V], wn[NCB][V], gq[NCB][V], gn[NCB][V];
+  float wq[NCB][V], wn[NCB][V];
+  double gq[NCB][V], gn[NCB][V];
 #pragma unroll
   for (int i = 0; i < NCB; ++i) {
     const int c = (sub + i * TPR) * V;
     gains<V>(a.w_post, c, c < a.d, wq[i]);
     gains<V>(a.w_pre, c, c < a.d, wn[i]);
 #pragma unroll
-    for (int e = 0; e < V; ++e) gq[i][e] = gn[i][e] = 0.f;
+    for (int e = 0; e < V; ++e) gq[i][e] = gn[i][e] = 0.;
   }
   const float id = 1.0f / (float)a.d;
   for (long g = blockIdx.x; g * RPB < a.Tn; g += gridDim.x) {
@@ -201,7 +203,7 @@ __global__ __launch_bounds__(NT) void k_sublayer_bwd(NormBwd a) {
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const float xh = s[e] * rs;
-        gn[i][e] = fmaf(n[e], xh, gn[i][e]);
+        gn[i][e] += n[e] * xh;
         m = fmaf(n[e] * wn[i][e], xh, m);
       }
     }
@@ -236,7 +238,7 @@ __global__ __launch_bounds__(NT) void k_sublayer_bwd(NormBwd a) {
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const float Du = D[i][e] * (y[e] * ry);
-        gq[i][e] = fmaf(gt, Du, gq[i][e]);
+        gq[i][e] += gt * Du;
         q = fmaf(Du, wq[i][e], q);
       }
     }
@@ -261,7 +263,7 @@ __global__ __launch_bounds__(NT) void k_sublayer_bwd(NormBwd a) {
   if (!a.part) return;
   // the rows of a block that share columns add up through LDS, group 0 first
   constexpr int WIDE = RPB > 1 ? TPR * NCB * V : 1;
-  __shared__ float acc[WIDE];
+  __shared__ double acc[WIDE];
   float* const part = a.part + (size_t)blockIdx.x * 2 * a.d;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
@@ -274,8 +276,8 @@ __global__ __launch_bounds__(NT) void k_sublayer_bwd(NormBwd a) {
           for (int i = 0; i < NCB; ++i)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-              float& v = which ? gn[i][e] : gq[i][e];
-              float& at = acc[(sub + i * TPR) * V + e];
+              double& v = which ? gn[i][e] : gq[i][e];
+              double& at = acc[(sub + i * TPR) * V + e];
               v = at = r ? at + v : v;
             }
         }
@@ -287,8 +289,12 @@ __global__ __launch_bounds__(NT) void k_sublayer_bwd(NormBwd a) {
         const int c = (sub + i * TPR) * V;
         if (c >= a.d) continue;
 #pragma unroll
-        for (int e = 0; e < V; e += 4)
-          st16(part + which * (size_t)a.d + c + e, pack16((which ? gn[i] : gq[i]) + e, (float*)nullptr));
+        for (int e = 0; e < V; e += 4) {
+          float v[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) v[x] = (float)(which ? gn[i][e + x] : gq[i][e + x]);
+          st16(part + which * (size_t)a.d + c + e, pack16(v, (float*)nullptr));
+        }
       }
     }
   }
