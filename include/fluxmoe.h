@@ -148,10 +148,11 @@ int moe_balance_loss_bwd(const float* logits, const float* dprob, const float* d
  *   dWr   = (accumulate_dw ? dWr : 0) + dlogits^T X      [E,d] fp32
  *   dbias = (accumulate_dw ? dbias : 0) + sum_t dlogits  [E] fp32
  * Each output may be NULL (not formed); X is read for dWr only, Wr for dX only
- * (NULL where unused).  Sums in a fixed order, of dlogits with all their
- * bits: in fp32, over the parts that the token range is cut into in fp64.  With T == 0, dWr and dbias become 0 unless accumulating.
- * X [T,d] and Wr [E,d] in dtype; dlogits [T,E] fp32.  dX may not alias X.  T <= 2^30,
- * E * d <= 2^30.
+ * (NULL where unused).  Sums run in a fixed order, over dlogits with all their
+ * bits: dbias in fp64, the products in fp32 and in fp64 over the parts that the
+ * token range is cut into.  With T == 0, dWr and dbias become 0 unless
+ * accumulating.  X [T,d] and Wr [E,d] in dtype; dlogits [T,E] fp32.  dX may not
+ * alias X.  T <= 2^30, E * d <= 2^30.
  */
 int moe_router_bwd(const float* dlogits, const void* X, const void* Wr, int dtype, int T, int d, int E,
                    void* dX, int accumulate_dx, float* dWr, float* dbias, int accumulate_dw,

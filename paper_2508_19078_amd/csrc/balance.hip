@@ -403,13 +403,16 @@ constexpr int RB_SLAB = 64;     // tokens
 constexpr int RB_SPLITS = 32;   // most parts of the token range
 constexpr int RB_PAD = 320;     // floats between them
 
+typedef double f64x4_t __attribute__((ext_vector_type(4)));
+
 struct RouterBwd {
   const float* dl;
   const void *X, *Wr;
   int Tn, d, E;
   void* dX;
   int acc_dx;
-  float *part, *partb;   // [splits][E][d], stride apart, and [splits][E], or NULL
+  float* part;           // [splits][E][d], stride apart, or NULL
+  double* partb;         // [splits][E], or NULL
   long stride;
   int span;              // tokens per split, a multiple of RB_SLAB
 };
@@ -502,7 +505,8 @@ template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(Router
   // dlogits: thread q of the slab's quads, 4 experts of token q / (8 NT)
   constexpr int QT = 8 * NT, QN = RB_SLAB * QT / 512;
   const int quad = threadIdx.x % QT, e0 = 4 * quad;
-  f32x4_t dl[QN], bsum = {0.f, 0.f, 0.f, 0.f};
+  f32x4_t dl[QN];
+  f64x4_t bsum = {0., 0., 0., 0.};   // the bias's gradient: in 64 bits, like a plain sum over the tokens
   auto load_dl = [&](int t) {
 #pragma unroll
     for (int i = 0; i < QN; ++i) {
@@ -583,7 +587,7 @@ template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(Router
 #pragma unroll
       for (int k = 0; k < 3; ++k)
         *(FM_LDS u32x2_t*)(pl + (k * NT + (quad >> 3)) * BLK + r * 64 + ((((quad & 7) >> 1) ^ ((r >> 2) & 3)) << 4) + (quad & 1) * 8) = p[k];
-      if (bias) bsum += dl[i];
+      if (bias) bsum += __builtin_convertvector(dl[i], f64x4_t);
     }
     __syncthreads();
     if (t + RB_SLAB < t1) {
@@ -709,7 +713,7 @@ template <int NT> __global__ __launch_bounds__(512, 2) void k_router_bf16(Router
   }
   if (bias) {   // the block's threads with the same experts, in order
     __syncthreads();
-    FM_LDS f32x4_t* const b4 = (FM_LDS f32x4_t*)xs;
+    FM_LDS f64x4_t* const b4 = (FM_LDS f64x4_t*)xs;
     b4[threadIdx.x] = bsum;
     __syncthreads();
     if (threadIdx.x < QT) {
@@ -733,10 +737,10 @@ template <int NT> __global__ __launch_bounds__(256) void k_router_f32(RouterBwd 
     const bool bias = a.partb && c0 == 0;
     const FM_GLOBAL float* const X = (const FM_GLOBAL float*)a.X;
     f32x16_t acc[NT];
-    float bs[NT];
+    double bs[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-      bs[j] = 0.f;
+      bs[j] = 0.;
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
     }
@@ -758,7 +762,7 @@ template <int NT> __global__ __launch_bounds__(256) void k_router_f32(RouterBwd 
       for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-          bs[j] += v[u][j];
+          if (bias) bs[j] += v[u][j];
           acc[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[u], v[u][j], acc[j], 0, 0, 0);
         }
     }
@@ -767,7 +771,7 @@ template <int NT> __global__ __launch_bounds__(256) void k_router_f32(RouterBwd 
       const int e = 32 * j + m;
       if (e >= a.E) continue;
       if (bias) {
-        const float s = bs[j] + __shfl_xor(bs[j], 32);
+        const double s = bs[j] + __shfl_xor(bs[j], 32);
         if (h == 0) gptr(a.partb)[(size_t)split * a.E + e] = s;
       }
       if (a.part) {
@@ -813,11 +817,10 @@ template <int NT> __global__ __launch_bounds__(256) void k_router_f32(RouterBwd 
 // dWr and dbias from their parts: a block takes 64 quads of columns, its 4 groups of
 // threads every fourth part, and the groups' sums are added in order.  In 64 bits: up to
 // 32 parts of many tokens each, which may nearly cancel.
-__global__ __launch_bounds__(256) void k_router_dw(const float* __restrict__ part, const float* __restrict__ partb,
+__global__ __launch_bounds__(256) void k_router_dw(const float* __restrict__ part, const double* __restrict__ partb,
                                                    int splits, long stride, long n, int E, int accumulate,
                                                    float* __restrict__ dWr,
                                                    float* __restrict__ dbias) {
-  typedef double f64x4_t __attribute__((ext_vector_type(4)));
   __shared__ f64x4_t red[4][64];
   const int q = threadIdx.x & 63, g = threadIdx.x >> 6;
   const long i = ((long)blockIdx.x * 64 + q) * 4;
@@ -957,7 +960,7 @@ extern "C" int moe_balance_loss_bwd(const float* logits, const float* dprob, con
 extern "C" size_t moe_router_bwd_workspace_size(int T, int d, int E) {
   if (T < 0 || d <= 0 || E <= 0) return 0;
   const int a = router_most_parts(T, d, E, true), b = router_most_parts(T, d, E, false);   // for either type
-  return (size_t)(a > b ? a : b) * (router_stride(d, E) + E) * sizeof(float);
+  return (size_t)(a > b ? a : b) * (router_stride(d, E) * sizeof(float) + E * sizeof(double));
 }
 
 extern "C" int moe_router_bwd(const float* dlogits, const void* X, const void* Wr, int dtype, int T, int d, int E,
@@ -996,7 +999,7 @@ extern "C" int moe_router_bwd(const float* dlogits, const void* X, const void* W
   a.dX = dX; a.acc_dx = accumulate_dx;
   a.part = dWr ? (float*)ws : nullptr;
   a.stride = router_stride(d, E);
-  a.partb = dbias ? (float*)ws + (size_t)splits * a.stride : nullptr;
+  a.partb = dbias ? (double*)((float*)ws + (size_t)splits * a.stride) : nullptr;   // E d and the padding are even
   if (T > 0) {
     a.span = span;
     launch_router_bwd(a, is_bf16, splits, st);

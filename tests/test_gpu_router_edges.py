@@ -86,3 +86,17 @@ def test_parts_of_the_tokens_add_up_in_64_bits(dt):
     out = B.router(dl, X, torch.zeros(E, d, dtype=dt, device=DEV), dx=False)
     assert bool((out["dWr"][1] == 30).all()) and out["dbias"].tolist() == [0, 30, 0, 0]
     assert not out["dWr"][[0, 2, 3]].any()
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,d,E", [(5000, 40, 4), (3001, 2048, 64), (2000, 136, 200)])
+def test_bias_gradient_is_a_sum_in_64_bits(T, d, E, dt):
+    """2^25, ones and -2^25 in each of two columns: the ones' number, exactly."""
+    dl = torch.ones(T, E, device=DEV)
+    dl[0, 1], dl[T - 1, 1] = 2.0 ** 25, -2.0 ** 25
+    dl[5, E - 1], dl[64, E - 1] = -2.0 ** 25, 2.0 ** 25
+    want = torch.full((E,), float(T), device=DEV)
+    want[1] = want[E - 1] = T - 2
+    X, Wr = torch.zeros(T, d, dtype=dt, device=DEV), torch.zeros(E, d, dtype=dt, device=DEV)
+    assert torch.equal(B.router(dl, X, Wr)["dbias"], want)
+    assert torch.equal(B.router(dl, X, Wr, dx=False, dw=False)["dbias"], want)      # the fp32 kernel, of bias alone
