@@ -541,6 +541,8 @@ def moe_grouped_swiglu_fwd_mx4_workspace_size(layer, T, k) -> int:
 
 def moe_grouped_swiglu_fwd_mx4(layer, X, perm_token, offsets, T, k, O, ws, stream=None):
     st, v, bf = layer.struct if hasattr(layer, "struct") else layer, _device(), torch.bfloat16
+    if hasattr(layer, "tabs") and layer.tabs[0].get_device() != v:
+        raise ValueError(f"the layer's tables are on {layer.tabs[0].device}, the current device is cuda:{v}")
     return _call("moe_grouped_swiglu_fwd_mx4", ptr(layer), _arg(v, "X", X, bf, (T, st.d)),
                  _arg(v, "perm_token", perm_token, I32, (T * k,)), _arg(v, "offsets", offsets, I32, (st.S_routed + 1,)),
                  T, k, _arg(v, "O", O, bf, (T * (k + st.S_shared), st.d)), *_ws(v, ws), stream_ptr(stream))
@@ -634,19 +636,29 @@ class LayerTablesMX4:
     """Device pointer tables of a layer's 4-bit experts and the moe_layer_mx4
     struct.  q_*: per-slot code tensors (routed slots, then shared) and s_*
     their scale bytes, as moe_quantize_mxfp4 writes them for W_gate, W_up [I,d]
-    and W_down [d,I]."""
+    and W_down [d,I].  The tensors are kept; the library reads their addresses on
+    the device, so alignment and device are checked here."""
 
     def __init__(self, d: int, I: int, S_routed: int, S_shared: int, q_gate, q_up, q_down, s_gate, s_up, s_down,
                  device="cuda"):
         S = S_routed + S_shared
 
-        def table(name, x, shape):
+        def addresses(name, x, shape, align):
             if len(x) != S:
                 raise ValueError(f"{name} has {len(x)} matrices for {S} slots")
-            return torch.tensor([ptr(_shaped(name, t, shape), U8) for t in x], dtype=torch.int64, device=device)
+            out = [ptr(_shaped(name, t, shape), U8) for t in x]
+            for i, (p, t) in enumerate(zip(out, x)):
+                if p % align:
+                    raise ValueError(f"{name}[{i}] is not {align}-byte aligned")
+                if t.device != dev:
+                    raise ValueError(f"{name}[{i}] is on {t.device}, the tables are on {dev}")
+            return torch.tensor(out, dtype=torch.int64, device=dev)
 
+        dev = torch.device(device)
+        if dev.type == "cuda" and dev.index is None and torch.cuda.is_initialized():
+            dev = torch.device("cuda", _device())
         (cg, sg), (cd, sd) = mxfp4_shapes(I, d), mxfp4_shapes(d, I)
-        self.keep = [q_gate, q_up, q_down, s_gate, s_up, s_down]
-        self.tabs = [table(*a) for a in (("q_gate", q_gate, cg), ("q_up", q_up, cg), ("q_down", q_down, cd),
-                                         ("s_gate", s_gate, sg), ("s_up", s_up, sg), ("s_down", s_down, sd))]
+        self.keep = [list(x) for x in (q_gate, q_up, q_down, s_gate, s_up, s_down)]
+        self.tabs = [addresses(*a) for a in (("q_gate", q_gate, cg, 16), ("q_up", q_up, cg, 16), ("q_down", q_down, cd, 16),
+                                             ("s_gate", s_gate, sg, 4), ("s_up", s_up, sg, 4), ("s_down", s_down, sd, 4))]
         self.struct = moe_layer_mx4(d, I, S_routed, S_shared, *[ptr(t) for t in self.tabs])
