@@ -395,9 +395,7 @@ template <typename Fn> void with_expert_lanes(int E, Fn fn) {
 // fp32.  v_mfma_f32_32x32x2_f32: an operand lane holds one value, row lane % 32 at k
 // = lane / 32, a coalesced read of the row-major inputs whichever of them runs along k.
 //
-// Both: rows m of dX's first operand are dealt to columns so that a lane's 16 sums are
-// 16 consecutive columns: column(m) = 16 ((m / 4) % 2) + 4 (m / 8) + m % 4.
-__device__ __forceinline__ int tile_column(int m) { return 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
+// Both: rows m of dX's first operand are dealt to columns tile_column(m).
 
 constexpr int RB_SLAB = 64;     // tokens
 constexpr int RB_SPLITS = 32;   // most parts of the token range

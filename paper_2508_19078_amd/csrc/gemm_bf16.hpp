@@ -60,6 +60,10 @@ struct AccCoord {
   int row, col4;
 };
 
+// Columns dealt to the 32 rows of a first operand so that a lane's 16 sums of a 32 x 32
+// MFMA (rows 8 q + 4 (lane / 32) + [0, 4)) are 16 consecutive columns.
+__device__ __forceinline__ int tile_column(int m) { return 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
+
 // 4 consecutive values <-> global memory.
 __device__ __forceinline__ void store4(float* p, f32x4_t v) { *(FM_GLOBAL f32x4_t*)(p) = v; }
 __device__ __forceinline__ f32x4_t load4(const float* p) { return *(const FM_GLOBAL f32x4_t*)(p); }

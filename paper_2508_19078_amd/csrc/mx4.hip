@@ -333,10 +333,9 @@ template <int RA_, int RB_, int WN_, int BPC_> struct MxCfg {
   static_assert(BPC * LDS <= 160 * 1024, "LDS");
 };
 
-__device__ __forceinline__ int mx_column(int m) { return 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
 // Chunk swizzles of a 128-byte slab row: 16 consecutive lanes' rows at one logical
 // chunk on 16 distinct 4-bank groups; lanes read activation rows in order, weight
-// rows in the order of mx_column.
+// rows in the order of tile_column.
 __device__ __forceinline__ int mx_swz_a(int r) { return (r >> 1) & 7; }
 __device__ __forceinline__ int mx_swz_b(int r) { return ((r >> 1) & 3) | ((r >> 2) & 4); }
 
@@ -425,10 +424,10 @@ __device__ __forceinline__ void mx_gemm(const MxTile& t, FM_LDS char* lds, f32x1
   }
 #pragma unroll
   for (int j = 0; j < C::NJ; ++j) {
-    const int r = col0 + 32 * j + mx_column(m);
+    const int r = col0 + 32 * j + tile_column(m);
     fb[j] = C::A_BYTES + r * 128 + ((h ^ mx_swz_b(r)) << 4);
   }
-  const uint32_t ga = (row0 + m) * 16, gb = (C::RA + col0 + mx_column(m)) * 16;
+  const uint32_t ga = (row0 + m) * 16, gb = (C::RA + col0 + tile_column(m)) * 16;
 #pragma unroll
   for (int i = 0; i < C::MI; ++i)
 #pragma unroll
