@@ -838,6 +838,7 @@ __global__ __launch_bounds__(256) void k_router_dw(const float* __restrict__ par
   }
   if (dbias && blockIdx.x == 0 && threadIdx.x < (unsigned)E) {
     double v = accumulate ? dbias[threadIdx.x] : 0.;
+#pragma unroll 8
     for (int p = 0; p < splits; ++p) v += partb[(size_t)p * E + threadIdx.x];
     dbias[threadIdx.x] = (float)v;
   }
