@@ -839,14 +839,14 @@ __global__ __launch_bounds__(64 * NW) void k_mx_few_down(MxArgs a, int NT, int m
   }
 }
 
-// Whether a call takes the kernels for a few tokens.  us there and on 64-row tiles, a
-// pass among others: d = 4096, I = 688, 16 slots, top-4: 1 token 19, 26; 4 tokens 21, 28;
-// 8 27, 29; 16 36, 29.  d = 2048, I = 1408, 64 + 2 slots, top-6: 1 token (1408 blocks)
-// 17, 21; 2 (2464) 24, 24; 4 (4576) 33, 25.  d = 512, I = 256, 8 slots, top-2: 1 token
-// 14, 12; 8 14, 13.  A block's rows have to fit the LDS.
+// Whether a call takes the kernels for a few tokens.  us there and on 64-row tiles, replayed
+// from a graph: d = 4096, I = 688, 16 slots, top-4: 1 token 11, 22; 4 tokens 19, 24; 8 27,
+// 26.  d = 2048, I = 1408, 64 + 2 slots, top-6 (calls among others): 1 token (1408 blocks)
+// 16, 20; 2 (2464) 22, 23; 4 (4576) 33, 26.  d = 512, I = 256, 8 slots, top-2: 1 token 6.4,
+// 11.3; 8 7.3, 11.0.  d = 128, I = 64: 6.3, 10.5.  A block's rows have to fit the LDS.
 bool mx_few_tokens(const moe_layer_mx4* L, int T, long active) {
-  return T <= MX_FEW && active * (L->I / 8) <= 2048 && (long)L->d * L->I >= 1 << 20 &&
-         T * mx_few_row_bytes(up128(L->d) / 128) <= 56 * 1024 && T * mx_few_row_bytes(up128(L->I) / 128) <= 52 * 1024;
+  return T <= MX_FEW && active * (L->I / 8) <= 2048 && T * mx_few_row_bytes(up128(L->d) / 128) <= 56 * 1024 &&
+         T * mx_few_row_bytes(up128(L->I) / 128) <= 52 * 1024;
 }
 // Whether it takes 256 x 256 tiles, one block of 8 waves per compute unit, rather than
 // 128 x 128 ones (64 x 128 where few rows are left), two of 4 waves, whose blocks run

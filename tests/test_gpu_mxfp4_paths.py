@@ -46,7 +46,7 @@ FEW_CASES = {
 LIMITS = [
     ((8, 1032, 3, 1, 1024, 0, 3), FEW), ((9, 1032, 3, 1, 1024, 0, 3), SMALL),          # tokens
     ((2, 264, 8, 4, 4096, 0, 4), SMALL), ((2, 264, 2, 2, 4096, 0, 2), FEW),            # slots times I / 8
-    ((2, 1024, 3, 2, 1024, 0, 3), FEW), ((2, 1016, 3, 2, 1024, 0, 3), SMALL),          # d I
+    ((8, 8, 2, 1, 8, 0, 2), FEW), ((9, 8, 2, 1, 8, 0, 2), SMALL),                      # below every block
     ((8, 9216, 2, 1, 120, 1, 2), FEW), ((8, 13824, 2, 1, 120, 1, 2), SMALL),           # rows in LDS
 ]
 
