@@ -13,8 +13,8 @@
 // and on to the next block's, either index grows, so no two pairs share a slot.
 // A block per sequence then adds its slots in a fixed order.  No float atomics.
 //
-// Measured at 8192 tokens, 64 experts, top-6, 4 sequences: 8.4 us for the blocks, 7.3
-// for the sequences, 8.3 for the logits' gradient (2 and 4 MB: all three are a launch
+// Measured at 8192 tokens, 64 experts, top-6, 4 sequences: 8.7 us for the blocks, 6.8
+// for the sequences, 8.4 for the logits' gradient (2 and 4 MB: all three are a launch
 // and chains of dependent loads and exchanges).  The first pass with its tokens one
 // after another, without LDS, took 25 us.
 #include <algorithm>
@@ -385,15 +385,20 @@ template <typename Fn> void with_expert_lanes(int E, Fn fn) {
 // per wave: dWr sums over tokens and reads both transposed (ds_read_b64_tr_b16), dX
 // sums over experts and reads the planes along their rows (16-byte chunks of a row
 // swizzled by (row / 4) % 4, so that 16 rows read at one chunk cover the 64 banks
-// once).  Wr's fragments stay in registers.  8192 tokens, d = 2048, 64 experts: 31 us
-// with the sums of dWr's parts in 8.9 us more (72 MB for both outputs: 14 us at the rate
-// of a copy); dX alone 18, dWr alone 26.6.  A block has 4 slabs, each a chain of loads,
-// conversion, exchange through LDS, products and stores; 32 parts of the token range
-// measured best: with 128 columns per block 33 + 12.5 us, 16 parts 36.7 + 7.4, 64 parts
-// 34.1 + 20.6 (a part of dWr is 512 KB, written and read).  On fp32 MFMAs, dX and dWr by separate blocks, it took 124 + 18 us.
+// once).  Wr's fragments stay in registers.  8192 tokens, d = 2048, 64 experts: 32.9 us
+// with the sums of dWr's parts in 5.2 us more (72 MB for both outputs: 14 us at the rate
+// of a copy); calls for dX alone 20, for dWr and dbias alone 28, for all 36.  A block has 4
+// slabs, each a chain of loads, conversion, exchange through LDS, products and stores (the
+// matrix cores are busy for 14 % of it).  32 parts of the token range measured best at this
+// width (with 128 columns per block, and sums in 32 bits, 33 + 12.5 us, 16 parts 36.7 + 7.4,
+// 64 parts 34.1 + 20.6: a part of dWr is 512 KB, written and read); narrower layers were not
+// measured and leave compute units idle.  128 < E: 166 us at 256 experts, with 372 bytes per lane in
+// scratch.  On fp32 MFMAs, dX and dWr by separate blocks, 64 experts took 124 + 18 us.
 //
 // fp32.  v_mfma_f32_32x32x2_f32: an operand lane holds one value, row lane % 32 at k
 // = lane / 32, a coalesced read of the row-major inputs whichever of them runs along k.
+// The same size: calls for dX alone 71 us, for dWr and dbias alone 44, for all 105.  dX's
+// lanes read their own token's dlogits one by one.
 //
 // Both: rows m of dX's first operand are dealt to columns tile_column(m).
 

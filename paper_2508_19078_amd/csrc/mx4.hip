@@ -9,14 +9,15 @@
 //
 // * Slabs of 256 k go global -> LDS with global_load_lds_dwordx4, whole 128-byte lines
 //   of 8 rows per instruction, into two buffers; the scales of 512 k of a row (16
-//   bytes) follow through registers.  What bounds such a product is the number of
-//   requests its operands make to L2, not their bytes: with half lines and a scale
-//   dword per row and 128 k (128 x 256 tiles, a ring of three, two blocks per compute
-//   unit) the same products took 2.03 and 1.15 ms at 262144 rows, d = 4096, I = 1024,
-//   and half of that with the loads taken out.  Now 1.45 and 0.96 (3.0 and 2.3 PFLOP/s;
-//   the instruction alone, on registers, reaches 7.2).  What remains is a tile's ends:
-//   setup, first slab and epilogue are 19 of the 44 us of a 256 x 256 tile at d = 4096.
-//   With the next tile's setup and first slab before the epilogue it ran 3-8 % slower.
+//   bytes) follow through registers.  The number of requests to L2 counts, not their
+//   bytes alone: with half lines and a scale dword per row and 128 k (128 x 256 tiles, a
+//   ring of three, two blocks per compute unit) the same products took 2.03 and 1.15 ms
+//   at 262144 rows, d = 4096, I = 1024.  Now 1.44 and 0.96 (3.1 and 2.3 PFLOP/s; the
+//   instruction alone, on registers, reaches 7.2): the matrix cores are busy for 37 and
+//   29 % of the cycles, L2's channels take a read in 28 and 16 % of them, HBM moves 2.6
+//   and 3.2 TB/s.  None of them is full: what is left is latency, one slab in flight per
+//   block and the ends of the tiles (44 us each in gate-up).  With the next tile's setup
+//   and first slab before the epilogue it ran 3-8 % slower.
 // * Weights are the first operand, so a lane's 16 sums of a 32 x 32 tile belong to
 //   one activation row; weight rows are dealt to the operand's rows so that they
 //   are 16 consecutive columns (tile_column).  Two lanes then hold a whole

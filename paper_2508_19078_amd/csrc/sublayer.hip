@@ -13,9 +13,9 @@
 // rounding; the time grew by 1-2 %, by 5 % at d = 256), and leaves them, one row of partial sums per
 // block, to a second launch that adds them in a fixed order (no float atomics).
 //
-// Measured at 8192 rows of 2048 bf16, post-norm and gate: forward 23.5 us (134 MB, 5.7
-// TB/s), backward 37.5 us (201 MB, 5.4 TB/s) and 4.6 us for the second launch; 1023
-// rows of 1000 fp32, pre-norm: 7.5 us and 3.8.  A single row of 4096 takes 4.6 us: a
+// Measured at 8192 rows of 2048 bf16, post-norm and gate: forward 24.0 us (134 MB, 5.6
+// TB/s), backward 39.2 us (201 MB, 5.1 TB/s) and 4.6 us for the second launch; 1023
+// rows of 1000 fp32, pre-norm: 7.5 us and 4.2.  A single row of 4096 takes 4.6 us: a
 // launch, one load's latency and two reductions.  (The second launch with 8 groups of
 // threads per block, each adding 64 partial sums one after another, took 9.6 us.)
 #include "common.hpp"
