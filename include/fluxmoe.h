@@ -61,7 +61,7 @@ enum { MOE_F32 = 0, MOE_BF16 = 1, MOE_I8 = 2 };
 
 /* Message of the last failed call on this thread ("" if none). */
 const char* moe_last_error(void);
-/* ABI revision of this header. */
+/* ABI revision of this header (entry points are added within one). */
 int moe_abi_version(void);
 #define FLUXMOE_ABI_VERSION 3
 
@@ -149,10 +149,10 @@ int moe_balance_loss_bwd(const float* logits, const float* dprob, const float* d
  *   dbias = (accumulate_dw ? dbias : 0) + sum_t dlogits  [E] fp32
  * Each output may be NULL (not formed); X is read for dWr only, Wr for dX only
  * (NULL where unused).  Sums run in a fixed order, over dlogits with all their
- * bits: dbias in fp64, the products in fp32 and in fp64 over the parts that the
- * token range is cut into.  With T == 0, dWr and dbias become 0 unless
- * accumulating.  X [T,d] and Wr [E,d] in dtype; dlogits [T,E] fp32.  dX may not
- * alias X.  T <= 2^30, E * d <= 2^30.
+ * bits (beside bf16, down to 2^-133): dbias in fp64, the products in fp32 and in
+ * fp64 over the parts that the token range is cut into.  With T == 0, dWr and
+ * dbias become 0 unless accumulating.  X [T,d] and Wr [E,d] in dtype; dlogits
+ * [T,E] fp32.  dX may not alias X.  T <= 2^30, E * d <= 2^30.
  */
 int moe_router_bwd(const float* dlogits, const void* X, const void* Wr, int dtype, int T, int d, int E,
                    void* dX, int accumulate_dx, float* dWr, float* dbias, int accumulate_dw,

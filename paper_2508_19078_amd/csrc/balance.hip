@@ -431,8 +431,8 @@ __device__ __forceinline__ void put_dx(float* o, int cols, bool add, const f32x1
   }
 }
 
-// a + b + c = v exactly, each the upper half of an fp32 and so a bf16 (8 bits of v each,
-// one sign).  Cut off, not rounded: a finite v has finite parts, and an infinity is a.
+// a + b + c = v exactly (to a multiple of 2^-133, where bf16 ends), each the upper half of
+// an fp32 and so a bf16 (8 bits of v each, one sign).  Cut off, not rounded: a finite v has finite parts, and an infinity is a.
 __device__ __forceinline__ void split3(f32x4_t v, u32x2_t (&p)[3]) {
   uint32_t r[4];
 #pragma unroll

@@ -100,3 +100,27 @@ def test_bias_gradient_is_a_sum_in_64_bits(T, d, E, dt):
     X, Wr = torch.zeros(T, d, dtype=dt, device=DEV), torch.zeros(E, d, dtype=dt, device=DEV)
     assert torch.equal(B.router(dl, X, Wr)["dbias"], want)
     assert torch.equal(B.router(dl, X, Wr, dx=False, dw=False)["dbias"], want)      # the fp32 kernel, of bias alone
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("e", [-60, -100, -118, -126])
+def test_tiny_gradients_keep_their_bits(e, dt):
+    """dlogits down to fp32's smallest normal numbers, whose lower parts are subnormal: off
+    by the products' roundings, or by fp32's smallest step in each of the sum's terms.  In
+    bf16, dlogits are taken apart into bf16 values: the upper halves of what is left, cut at
+    the 16th bit, which for a subnormal stands for 2^-133.  What three cuts leave is below
+    2^-133, whatever the value: a term is off by that times the other factor."""
+    T, d, E = 130, 72, 20
+    g = torch.Generator().manual_seed(-e)
+    dl = (1 + torch.rand(T, E, generator=g)) * 2.0 ** e * (1 - 2 * torch.randint(0, 2, (T, E), generator=g))
+    X, Wr = (torch.randn(n, d, generator=g).to(dt) for n in (T, E))
+    out = B.router(dl.to(DEV), X.to(DEV), Wr.to(DEV))
+    a, x, w = B.f64(dl), B.f64(X), B.f64(Wr)
+    step = 2.0 ** -149
+    for n, (want, mag), terms in (("dWr", products(a, x), T), ("dX", products(a.T, w), E)):
+        half = 2.0 ** -8 if n == "dX" and dt == torch.bfloat16 else U
+        tol = (terms + 40) * U * mag + half * np.abs(want) + (3 * terms + (2.0 ** 15 if half > U else 0)) * step
+        if dt == torch.bfloat16:
+            tol = tol + 2.0 ** -133 * (np.abs(x).sum(0) if n == "dWr" else np.abs(w).sum(0))
+        err = np.abs(B.f64(out[n]) - want)
+        assert np.all(err <= tol), (n, float((err / tol).max()))
