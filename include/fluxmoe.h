@@ -33,8 +33,9 @@
  *           validated on the host before any HIP call, so an invalid call
  *           enqueues nothing.  moe_last_error() gives a message for the last
  *           failure on the calling thread.  No C++ exception crosses the ABI.
- * Outputs.  Fully overwritten, except `counts` of moe_profile_hist and
- *           moe_profile_route (adds) and
+ * Outputs.  Fully overwritten, except `counts` of moe_profile_hist,
+ *           moe_profile_route and moe_route_scored (adds), sel_bias of
+ *           moe_route_bias_update (adds), what `accumulate` adds to, and
  *           the weight gradients of moe_grouped_swiglu_bwd, moe_router_bwd and
  *           moe_sublayer_norm_bwd when accumulate_dw.
  */
@@ -96,6 +97,75 @@ int moe_route_topk(const void* X, const void* Wr, int dtype, const float* bias,
  */
 int moe_route_bwd(const float* gate, const int32_t* idx, const float* dgate, const void* Wr, int dtype,
                   int T, int d, int E, int k, void* dX, int accumulate, void* stream);
+
+/* moe_router_logits: the router's product alone, for moe_route_scored:
+ *   logits[t,e] = sum_i X[t,i] * Wr[e,i] + bias[e]      (fp32 accumulation)
+ * the logits that moe_route_topk writes.  X [T,d], Wr [E,d] in dtype; bias [E] fp32
+ * or NULL; logits [T,E] fp32.  Limits as for moe_route_topk.
+ */
+int moe_router_logits(const void* X, const void* Wr, int dtype, const float* bias, int T, int d, int E,
+                      float* logits, void* stream);
+
+/* moe_gating: how moe_route_scored turns logits into a routing (host struct). */
+enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
+typedef struct moe_gating {
+  int E;            /* experts, 1 to 256 */
+  int k;            /* choices per token, 1 to 16 */
+  int score;        /* MOE_SCORE_SOFTMAX or MOE_SCORE_SIGMOID */
+  int n_group;      /* 1 to 32 groups of E / n_group consecutive experts */
+  int topk_group;   /* groups that stay, 1 to n_group; k <= topk_group * E / n_group */
+  int group_top;    /* a group ranks by its largest key (1) or its two largest (2) */
+  int renorm;       /* gates divided by their sum */
+  float scale;      /* factor on the gates, finite */
+} moe_gating;
+
+/* moe_route_scored: routing from the logits by scores (the gating networks of the
+ * models that are tuned, Section 2.1, beside the softmax over the selected experts
+ * of moe_route_topk):
+ *   s[t,e]    = softmax over all E of logits[t,:], or 1 / (1 + exp(-logits[t,e]))
+ *   key[t,e]  = sel_bias ? s[t,e] + sel_bias[e] : s[t,e]
+ *   rank[t,g] = sum of the group's group_top largest keys
+ *   the topk_group groups of largest rank stay (ties: the lower group), and
+ *   idx[t,:]  = the k experts of largest key among them, in rank order (ties: the
+ *               lower expert)
+ *   gate[t,j] = scale * s[t,idx[t,j]] / (renorm ? sum_j' s[t,idx[t,j']] : 1)
+ *   counts[e] += choices idx[t,j] == e of the tokens whose keep flag is set
+ * sel_bias steers the selection alone, not the gates (balance without a loss; see
+ * moe_route_bias_update).  Selections are those of keys in fp64; where keys are the
+ * scores themselves, which order as the logits do, they are those of the logits
+ * (-0.0 equals +0.0).  Gates are fp32.  A logit of -inf is an expert of score 0, which
+ * is still chosen where no other is left; a NaN logit counts as -inf, a NaN key or rank
+ * too; among softmax scores, logits of +inf share 1 evenly.  A token whose selected
+ * scores are all 0 gets gates 0.
+ * logits [T,E] fp32; sel_bias [E] fp32 or NULL; keep [T] uint8 or NULL (all), read
+ * for counts only; idx [T,k] int32; gate [T,k] fp32; counts [E] int32 or NULL.
+ * T <= 2^30.
+ */
+int moe_route_scored(const moe_gating* g, const float* logits, const float* sel_bias, const uint8_t* keep, int T,
+                     int32_t* idx, float* gate, int32_t* counts, void* stream);
+
+/* moe_route_scored_bwd: the gradient of the logits from the gates' gradients dgate
+ * (moe_unpermute_bwd's), with the selection held fixed; S the sum of the selected
+ * scores:
+ *   ds[t,j] = scale * (renorm ? (dgate[t,j] - sum_i dgate[t,i] s_i / S) / S : dgate[t,j])
+ *   sigmoid:                dlogits[t,idx[t,j]] = s_j (1 - s_j) ds_j, 0 elsewhere
+ *   softmax with renorm:    dlogits[t,idx[t,j]] = s_j ds_j,           0 elsewhere
+ *   softmax without renorm: dlogits[t,e] = s_e (ds of e's choice or 0 - sum_i s_i ds_i)
+ * and 0 for a token whose selected scores are all 0.  accumulate = 1 adds to dlogits
+ * (the balance loss's share of moe_balance_loss_bwd); moe_router_bwd takes the sum.
+ * logits, g, idx as moe_route_scored had and left them (an entry outside [0, E) takes
+ * no part; an expert named twice gets both shares); dgate [T,k], dlogits [T,E] fp32;
+ * dlogits may alias logits unless accumulating.  T <= 2^30.
+ */
+int moe_route_scored_bwd(const moe_gating* g, const float* logits, const int32_t* idx, const float* dgate, int T,
+                         float* dlogits, int accumulate, void* stream);
+
+/* moe_route_bias_update: sel_bias after a step, moved against the load:
+ *   sel_bias[e] += rate * sign(sum_e' counts[e'] / E - counts[e])
+ * (the comparison in whole numbers).  counts [E] int32, not changed; sel_bias [E]
+ * fp32; 1 <= E <= 256; rate finite.
+ */
+int moe_route_bias_update(const int32_t* counts, int E, float rate, float* sel_bias, void* stream);
 
 /* moe_balance_loss: the auxiliary loss that keeps a router from sending every
  * token to a few experts while it is trained (the skew of Section 2.2,
@@ -296,6 +366,26 @@ int moe_quantize_mxfp4(const void* W, int dtype, long rows, int cols, uint8_t* c
  */
 int moe_dequant_mxfp4(const uint8_t* codes, const uint8_t* scale, long rows, int cols, int out_dtype,
                       void* out, void* stream);
+
+/* moe_quantize_fp8: an 8-bit float copy of a matrix (e4m3: sign, 4 exponent bits,
+ * 3 mantissa bits, no infinities, largest 448) with an fp32 scale per block of
+ * block_rows rows by 128 columns (cut short at the matrix's end):
+ *   top   = max(max |W|, 448 * 2^-126) over the block
+ *   scale = top / 448,  code = the e4m3 value nearest to 448 * W / top, ties to even
+ * (the quotient of bf16 values exactly where it lies on a tie).  A zero block has scale
+ * 0 and codes 0 (of W's sign); a block with an infinity or a NaN has scale NaN and codes 0.
+ * block_rows 1 (activations) or 128 (weights).  W [rows, cols] in dtype; codes
+ * [rows, cols] bytes; scale [ceil(rows / block_rows), ceil(cols / 128)] fp32.
+ * rows >= 1, cols % 8 == 0.
+ */
+int moe_quantize_fp8(const void* W, int dtype, long rows, int cols, int block_rows, uint8_t* codes, float* scale,
+                     void* stream);
+
+/* moe_dequant_fp8: out = value(code) * scale of its block (fp32 product, one rounding
+ * to out_dtype); the codes 0x7F and 0xFF are NaN.  Layouts as moe_quantize_fp8's.
+ */
+int moe_dequant_fp8(const uint8_t* codes, const float* scale, long rows, int cols, int block_rows, int out_dtype,
+                    void* out, void* stream);
 
 /* ---------------------------------------------------------------- merging --
  * moe_merge_plan: which experts of one layer are merged, from its histogram
@@ -583,6 +673,41 @@ int moe_grouped_swiglu_fwd_mx4(const moe_layer_mx4* L, const void* X, const int3
                                void* ws, size_t ws_bytes, void* stream);
 size_t moe_grouped_swiglu_fwd_mx4_workspace_size(const moe_layer_mx4* L, int T, int k);
 
+/* moe_grouped_swiglu_fwd_fp8: the forward on 8-bit float experts, both operands of
+ * its products e4m3 with fp32 scales: weights by blocks of 128 x 128, activations by
+ * 1 x 128 (F8, moe_quantize_fp8's rule with block_rows 1):
+ *   H = silu(F8(X_s) Q_gate^T) * (F8(X_s) Q_up^T),   O = F8(H) Q_down^T
+ * Codes are multiplied and summed in fp32 over a block of 128, the sum is multiplied
+ * by the fp32 product of its two scales, and blocks add up in fp32; one rounding.  The
+ * matrix unit aligns the products of 8 consecutive k to the largest of them and drops
+ * what of the others lies below 2^-13 of it (the rounding of that largest product's own
+ * operands to 8 bits weighs 2^-4).  H is quantised from its fp32 values and not written out.  X [T,d] bf16 is quantised once
+ * per token; routed row p reads token perm_token[p] (moe_permute's; values clamped to
+ * [0, T)), so X_perm is not needed.  offsets, the row space and O [R_tot, d] bf16 as
+ * in moe_grouped_swiglu_fwd; O's rows behind the last routed one are left as they
+ * were.  The struct's tables are DEVICE arrays of S_routed + S_shared device pointers
+ * to moe_quantize_fp8's codes (16-byte aligned) and scales (4-byte aligned) of W_gate,
+ * W_up [I,d] and W_down [d,I] with block_rows 128 (read on the device only, not
+ * checked).  d and I multiples of 16; d * I and T * d, both rounded up to 128 columns,
+ * at most 2^32.
+ */
+typedef struct moe_layer_fp8 {
+  int d;
+  int I;
+  int S_routed;
+  int S_shared;
+  const uint8_t* const* q_gate;
+  const uint8_t* const* q_up;
+  const uint8_t* const* q_down;
+  const float* const* s_gate;
+  const float* const* s_up;
+  const float* const* s_down;
+} moe_layer_fp8;
+int moe_grouped_swiglu_fwd_fp8(const moe_layer_fp8* L, const void* X, const int32_t* perm_token,
+                               const int32_t* offsets, int T, int k, void* O,
+                               void* ws, size_t ws_bytes, void* stream);
+size_t moe_grouped_swiglu_fwd_fp8_workspace_size(const moe_layer_fp8* L, int T, int k);
+
 /* moe_unpermute: the gate-weighted combine of the expert outputs, the output
  * of the MoE layer of Section 2.1 (each token's output is the sum of its
  * selected experts' outputs weighted by the gating network's gates; shared
@@ -669,6 +794,47 @@ int moe_expert_utility(const moe_layer* L, const float* x_sq, const float* dy_sq
  */
 int moe_permute_bwd(const moe_layer* L, const void* dX_perm, const int32_t* inv,
                     int T, int k, void* dX, void* stream);
+
+/* ---------------------------------------------------------- gradients ----
+ * A set of tensors (host struct with DEVICE tables): what moe_grad_norm and
+ * moe_grad_clip run over, e.g. the weight gradients that a step's
+ * moe_grouped_swiglu_bwd, moe_router_bwd and moe_sublayer_norm_bwd left (fp32).
+ * data[i] points to start[i+1] - start[i] dense elements, aligned to their size (read
+ * on the device only, not checked), or is NULL: a frozen tensor, which takes no part.
+ * start[0] = 0, start does not decrease, start[n] = total.
+ */
+typedef struct moe_tensor_set {
+  int n;                    /* tensors, 1 to 2^20 */
+  int dtype;                /* MOE_F32 or MOE_BF16, all of them */
+  void* const* data;        /* [n] device pointers or NULL */
+  const int64_t* start;     /* [n+1] elements before each tensor */
+  long long total;          /* elements in all, those of frozen tensors too; <= 2^48 */
+} moe_tensor_set;
+
+/* moe_grad_norm: the global norm of a step's gradients, the participant's local
+ * fine-tuning step (Section 3) before its update:
+ *   sumsq[0] = (accumulate ? sumsq[0] : 0) + sum over all elements of g^2    (fp64)
+ *   norm[0]  = sqrt(sumsq[0])                                               (fp32)
+ * Squares and sums run in fp64, in a fixed order.  sumsq [1] fp64, norm [1] fp32 or
+ * NULL.  accumulate adds further sets (of another dtype, of another layer); ranks
+ * that hold parts of one model add their sumsq.  A set without elements adds 0.
+ */
+int moe_grad_norm(const moe_tensor_set* g, int accumulate, double* sumsq, float* norm, void* ws, size_t ws_bytes,
+                  void* stream);
+size_t moe_grad_norm_workspace_size(void);
+
+/* moe_grad_clip: gradients scaled so that their norm is at most max_norm:
+ *   coef = min(1, max_norm / (sqrt(sumsq[0]) + eps))     (fp64, rounded to fp32)
+ *   out  = coef * g                                      (fp32 product, one rounding)
+ * sumsq [1] fp64 as moe_grad_norm left it, read on the device.  out: a set of the same n,
+ * dtype and start whose tensors take the results (NULL: they are not written), each
+ * either g's own or disjoint from all of g's; out NULL: in place, and with coef = 1
+ * nothing is written.  An infinite norm has coef 0 (infinities become NaN), a NaN
+ * makes coef and all results NaN.  max_norm finite and >= 0, eps finite and >= 0 (0 / 0
+ * counts as coef 1).
+ */
+int moe_grad_clip(const moe_tensor_set* g, const double* sumsq, float max_norm, float eps, const moe_tensor_set* out,
+                  void* stream);
 
 #ifdef __cplusplus
 }

@@ -911,3 +911,175 @@ def sublayer_norm_backward(dS, dN, S, Y, rstd_s, rstd_y=None, gate=None, w_post=
         out["dgate"] = (D * u * w).sum(axis=1)
         out["dw_post"] = (g * D * u).sum(axis=0)
     return out
+
+
+# ------------------------------------------------------- routing from scores ----
+
+def _any64(a) -> np.ndarray:
+    """fp64, infinities and NaN among it."""
+    return np.asarray(a, dtype=F64)
+
+
+def scores(logits, score: str) -> np.ndarray:
+    """Softmax or sigmoid scores; a NaN logit counts as -inf, +inf share a softmax's 1."""
+    z = _any64(logits)
+    z = np.where(np.isnan(z), -np.inf, z)
+    with np.errstate(over="ignore", invalid="ignore"):
+        if score == "sigmoid":
+            return 1.0 / (1.0 + np.exp(-z))
+        m = z.max(axis=1, keepdims=True)
+        p = np.where(np.isposinf(m), (z == np.inf).astype(float), np.where(np.isneginf(z), 0.0, np.exp(z - m)))
+        total = p.sum(axis=1, keepdims=True)
+        return np.divide(p, total, out=np.zeros_like(p), where=total > 0)
+
+
+def _largest(key, n: int, allowed=None) -> np.ndarray:
+    """The n largest of each row in order, ties to the lower index, among the allowed."""
+    key = np.where(np.isnan(key), -np.inf, key) + 0.0
+    out = np.empty((len(key), n), dtype=np.int64)
+    for t, row in enumerate(key):
+        places = np.arange(len(row)) if allowed is None else np.nonzero(allowed[t])[0]
+        out[t] = places[np.argsort(-row[places], kind="stable")[:n]]
+    return out
+
+
+def route_scored(logits, k: int, score="softmax", n_group=1, topk_group=1, group_top=1, renorm=True, scale=1.0,
+                 sel_bias=None):
+    """(idx, gate, keys) of the routing from scores."""
+    s = scores(logits, score)
+    z = np.where(np.isnan(_any64(logits)), -np.inf, _any64(logits))
+    key = z if sel_bias is None else s + _any64(sel_bias)
+    key = np.where(np.isnan(key), -np.inf, key)
+    allowed = None
+    if topk_group < n_group:
+        of = s if sel_bias is None and group_top == 2 else key
+        with np.errstate(invalid="ignore"):
+            rank = np.sort(of.reshape(len(s), n_group, -1), axis=2)[:, :, -group_top:].sum(axis=2)
+        best = _largest(rank, topk_group)
+        allowed = np.zeros((len(s), n_group), dtype=bool)
+        np.put_along_axis(allowed, best, True, axis=1)
+        allowed = np.repeat(allowed, s.shape[1] // n_group, axis=1)
+    idx = _largest(key, k, allowed)
+    return idx, gates_of(logits, idx, score, renorm, scale), key
+
+
+def gates_of(logits, idx, score, renorm, scale) -> np.ndarray:
+    """The gates of chosen experts; 0 where the selected scores are all 0.  Scores that
+    fp64 cannot hold side by side are taken relative to the largest selected one."""
+    sel = np.take_along_axis(scores(logits, score), np.asarray(idx), axis=1)
+    if not renorm:
+        return scale * sel
+    z = np.take_along_axis(_any64(logits), np.asarray(idx), axis=1)
+    z = np.where(np.isnan(z), -np.inf, z)
+    with np.errstate(over="ignore", invalid="ignore"):
+        m = z.max(axis=1, keepdims=True)
+        if score == "softmax":
+            w = np.where(np.isposinf(m), (z == np.inf).astype(float), np.exp(z - m))
+        else:
+            low = np.minimum(m, 0.0)
+            w = np.where(z >= 0, 1.0 / (1.0 + np.exp(-z)), np.exp(z - low) / (1.0 + np.exp(np.minimum(z, 0.0))))
+        w = np.where(np.isneginf(z), 0.0, w)
+    total = w.sum(axis=1, keepdims=True)
+    return scale * np.divide(w, total, out=np.zeros_like(w), where=total > 0)
+
+
+def route_scored_backward(logits, idx, dgate, score="softmax", renorm=True, scale=1.0) -> np.ndarray:
+    """dlogits for a selection held fixed; entries of idx outside the experts take no part."""
+    z, idx = _any64(logits), np.asarray(idx)
+    z = np.where(np.isnan(z), -np.inf, z)
+    T, E = z.shape
+    ok = (idx >= 0) & (idx < E)
+    at = np.where(ok, idx, 0)
+    dg = np.where(ok, _any64(dgate), 0.0)
+    s = scores(z, score)
+    out = np.zeros((T, E))
+    rows = np.arange(T)
+    if renorm:
+        zc = np.where(ok, np.take_along_axis(z, at, axis=1), -np.inf)
+        pad = np.concatenate((zc, np.full((T, 1), -np.inf)), axis=1)       # (of a row without choices too)
+        share = gates_of(pad, np.broadcast_to(np.arange(idx.shape[1]), idx.shape), score, True, 1.0)
+        val = scale * share * (dg - (share * dg).sum(axis=1, keepdims=True))
+        if score == "sigmoid":
+            with np.errstate(over="ignore"):
+                val = val / (1.0 + np.exp(zc))
+    else:
+        val = scale * np.take_along_axis(s, at, axis=1) * dg
+        if score == "sigmoid":
+            with np.errstate(over="ignore"):
+                val = val / (1.0 + np.exp(np.take_along_axis(z, at, axis=1)))
+        else:
+            out -= s * val.sum(axis=1, keepdims=True)
+    for j in range(idx.shape[1]):
+        out[rows[ok[:, j]], at[ok[:, j], j]] += val[ok[:, j], j]
+    return out
+
+
+def bias_update(counts, sel_bias, rate) -> np.ndarray:
+    n = np.asarray(counts, dtype=np.int64)
+    return _any64(sel_bias) + rate * np.sign(n.sum() - n * len(n))
+
+
+# -------------------------------------------------------- 8-bit float rows ----
+
+FP8_TOP = 448.0
+
+
+def fp8_nearest(q) -> np.ndarray:
+    """The e4m3 value nearest to q (|q| <= 448), ties to even."""
+    q = _any64(q)
+    step = np.exp2(np.maximum(np.frexp(q)[1] - 1, -6) - 3)
+    return np.rint(q / step) * step
+
+
+def fp8_rows(W, block_rows: int = 1):
+    """(e4m3 values of 448 W / top, fp32 scales top / 448 by blocks of block_rows x 128)."""
+    W = _any64(W)
+    rows, cols = W.shape
+    R, C = -(-rows // block_rows), -(-cols // 128)
+    scale = np.zeros((R, C))
+    val = np.zeros((rows, cols))
+    for r in range(R):
+        for c in range(C):
+            b = W[r * block_rows:(r + 1) * block_rows, c * 128:(c + 1) * 128]
+            if not np.isfinite(b).all():
+                scale[r, c] = np.nan
+                continue
+            top = np.abs(b).max()
+            if top == 0:
+                continue
+            top = max(top, FP8_TOP * 2.0 ** -126)
+            scale[r, c] = np.float32(top / FP8_TOP)
+            val[r * block_rows:(r + 1) * block_rows, c * 128:(c + 1) * 128] = fp8_nearest(b * FP8_TOP / top)
+    return val, scale
+
+
+def fp8_spread(scale, rows: int, cols: int, block_rows: int) -> np.ndarray:
+    """Every element's scale."""
+    return np.repeat(np.repeat(scale, block_rows, axis=0)[:rows], 128, axis=1)[:, :cols]
+
+
+def fp8_round(W, block_rows: int = 1) -> np.ndarray:
+    """What W stands for after quantisation."""
+    val, scale = fp8_rows(W, block_rows)
+    return val * fp8_spread(scale, *val.shape, block_rows)
+
+
+def swiglu_fp8_fwd(x, Wg, Wu, Wd):
+    """(H, O) of one expert of the 8-bit float model: activations are quantised in front
+    of each product, Wg, Wu, Wd are values of quantised weights."""
+    xq = fp8_round(x)
+    a = xq @ _any64(Wg).T
+    H = a * sigmoid(a) * (xq @ _any64(Wu).T)
+    return H, fp8_round(H) @ _any64(Wd).T
+
+
+# ---------------------------------------------------------------- gradients ----
+
+def grad_sumsq(tensors) -> float:
+    import math
+    return math.fsum(float(np.dot(v, v)) for v in (_any64(t).ravel() for t in tensors if t is not None))
+
+
+def clip_coefficient(sumsq: float, max_norm: float, eps: float = 1e-6) -> float:
+    den = np.sqrt(sumsq) + eps
+    return 1.0 if den == 0 else float(np.minimum(1.0, max_norm / den))

@@ -46,6 +46,21 @@ class moe_layer_mx4(ctypes.Structure):
                 ("s_down", _vp)]
 
 
+class moe_layer_fp8(ctypes.Structure):
+    _fields_ = [("d", _c_int), ("I", _c_int), ("S_routed", _c_int), ("S_shared", _c_int),
+                ("q_gate", _vp), ("q_up", _vp), ("q_down", _vp), ("s_gate", _vp), ("s_up", _vp),
+                ("s_down", _vp)]
+
+
+class moe_gating(ctypes.Structure):
+    _fields_ = [("E", _c_int), ("k", _c_int), ("score", _c_int), ("n_group", _c_int), ("topk_group", _c_int),
+                ("group_top", _c_int), ("renorm", _c_int), ("scale", _f)]
+
+
+class moe_tensor_set(ctypes.Structure):
+    _fields_ = [("n", _c_int), ("dtype", _c_int), ("data", _vp), ("start", _vp), ("total", ctypes.c_longlong)]
+
+
 # name -> (restype, argtypes)
 _SIGS = {
     "moe_last_error": (ctypes.c_char_p, []),
@@ -100,6 +115,17 @@ _SIGS = {
     "moe_dequant_mxfp4": (_c_int, [_vp, _vp, ctypes.c_long, _c_int, _c_int, _vp, _vp]),
     "moe_grouped_swiglu_fwd_mx4": (_c_int, [_vp, _vp, _vp, _vp, _c_int, _c_int, _vp, _vp, _c_size, _vp]),
     "moe_grouped_swiglu_fwd_mx4_workspace_size": (_c_size, [_vp, _c_int, _c_int]),
+    "moe_router_logits": (_c_int, [_vp, _vp, _c_int, _vp, _c_int, _c_int, _c_int, _vp, _vp]),
+    "moe_route_scored": (_c_int, [_vp, _vp, _vp, _vp, _c_int, _vp, _vp, _vp, _vp]),
+    "moe_route_scored_bwd": (_c_int, [_vp, _vp, _vp, _vp, _c_int, _vp, _c_int, _vp]),
+    "moe_route_bias_update": (_c_int, [_vp, _c_int, _f, _vp, _vp]),
+    "moe_quantize_fp8": (_c_int, [_vp, _c_int, ctypes.c_long, _c_int, _c_int, _vp, _vp, _vp]),
+    "moe_dequant_fp8": (_c_int, [_vp, _vp, ctypes.c_long, _c_int, _c_int, _c_int, _vp, _vp]),
+    "moe_grouped_swiglu_fwd_fp8": (_c_int, [_vp, _vp, _vp, _vp, _c_int, _c_int, _vp, _vp, _c_size, _vp]),
+    "moe_grouped_swiglu_fwd_fp8_workspace_size": (_c_size, [_vp, _c_int, _c_int]),
+    "moe_grad_norm": (_c_int, [_vp, _c_int, _vp, _vp, _vp, _c_size, _vp]),
+    "moe_grad_norm_workspace_size": (_c_size, []),
+    "moe_grad_clip": (_c_int, [_vp, _vp, _f, _f, _vp, _vp]),
     "moe_merge_budget": (_c_int, [_vp, _vp, _c_int, _c_int, _f, _c_int, ctypes.c_double, _vp, _vp]),
     "moe_cluster_workspace_size": (_c_size, [_c_int, _c_int, _c_int, _c_int]),
     "moe_cluster_experts": (_c_int, [_vp, _c_int, _c_int, _c_int, _c_int, _c_int, _vp, _vp, _c_int, _c_int,
@@ -291,6 +317,46 @@ def moe_router_bwd(dlogits, X, Wr, ws, dX=None, dWr=None, dbias=None, accumulate
                  *_ws(v, ws), stream_ptr(stream))
 
 
+def moe_router_logits(X, Wr, bias, logits, stream=None):
+    (T, d), E, v = X.shape, Wr.shape[0], _device()
+    code = dtype_code(X.dtype)
+    return _call("moe_router_logits", _arg(v, "X", X, X.dtype, (T, d)), _arg(v, "Wr", Wr, X.dtype, (E, d)), code,
+                 _arg(v, "bias", bias, F32, (E,)), T, d, E, _arg(v, "logits", logits, F32, (T, E)), stream_ptr(stream))
+
+
+SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def gating(E, k, score="softmax", n_group=1, topk_group=1, group_top=1, renorm=True, scale=1.0) -> moe_gating:
+    """How moe_route_scored turns logits into a routing; checked by the calls that take it."""
+    if score not in SCORES:
+        raise ValueError(f"score={score!r}: expected one of {sorted(SCORES)}")
+    return moe_gating(E, k, SCORES[score], n_group, topk_group, group_top, int(bool(renorm)), float(scale))
+
+
+def moe_route_scored(g, logits, idx, gate, sel_bias=None, counts=None, keep=None, stream=None):
+    """g: a gating().  counts [E] int32 is added to (choices of the tokens whose keep
+    [T] uint8 is not 0; all without keep); sel_bias [E] fp32 steers the selection alone."""
+    T, v, E = logits.shape[0], _device(), g.E
+    return _call("moe_route_scored", ctypes.addressof(g), _arg(v, "logits", logits, F32, (T, E)),
+                 _arg(v, "sel_bias", sel_bias, F32, (E,)), _arg(v, "keep", keep, U8, (T,)), T,
+                 _arg(v, "idx", idx, I32, (T, g.k)), _arg(v, "gate", gate, F32, (T, g.k)), _arg(v, "counts", counts, I32, (E,)),
+                 stream_ptr(stream))
+
+
+def moe_route_scored_bwd(g, logits, idx, dgate, dlogits, accumulate=False, stream=None):
+    T, v, E = logits.shape[0], _device(), g.E
+    return _call("moe_route_scored_bwd", ctypes.addressof(g), _arg(v, "logits", logits, F32, (T, E)),
+                 _arg(v, "idx", idx, I32, (T, g.k)), _arg(v, "dgate", dgate, F32, (T, g.k)), T,
+                 _arg(v, "dlogits", dlogits, F32, (T, E)), int(bool(accumulate)), stream_ptr(stream))
+
+
+def moe_route_bias_update(counts, sel_bias, rate, stream=None):
+    E, v = sel_bias.shape[0], _device()
+    return _call("moe_route_bias_update", _arg(v, "counts", counts, I32, (E,)), E, float(rate),
+                 _arg(v, "sel_bias", sel_bias, F32, (E,)), stream_ptr(stream))
+
+
 def moe_quantize_int8(W, Wq, scale, stream=None):
     E, d = W.shape
     return _call("moe_quantize_int8", ptr(W, FLOAT), dtype_code(W.dtype), E, d, ptr(Wq, I8), ptr(scale, F32),
@@ -388,6 +454,37 @@ def moe_dequant_mxfp4(codes, scale, out, stream=None):
     cs, ss = mxfp4_shapes(rows, cols)
     v, code = _device(), dtype_code(out.dtype)
     return _call("moe_dequant_mxfp4", _arg(v, "codes", codes, U8, cs), _arg(v, "scale", scale, U8, ss), rows, cols, code,
+                 _arg(v, "out", out, out.dtype, (rows, cols)), stream_ptr(stream))
+
+
+def fp8_scale_shape(rows, cols, block_rows=128):
+    """Shape of the scales of a [rows, cols] matrix of 8-bit floats."""
+    return (-(-rows // block_rows), -(-cols // 128))
+
+
+def _f8(codes):
+    """Codes as bytes: uint8, or torch's e4m3 type of the same bits."""
+    return codes.view(U8) if codes is not None and codes.dtype is torch.float8_e4m3fn else codes
+
+
+def moe_quantize_fp8(W, codes, scale, block_rows=128, stream=None):
+    """codes [rows, cols] uint8 or float8_e4m3fn; scale: fp8_scale_shape."""
+    rows, cols = W.shape
+    v, code = _device(), dtype_code(W.dtype)
+    return _call("moe_quantize_fp8", _arg(v, "W", W, W.dtype, (rows, cols)), code, rows, cols, block_rows,
+                 _arg(v, "codes", _f8(codes), U8, (rows, cols)), _arg(v, "scale", scale, F32, _f8_scales(rows, cols, block_rows)),
+                 stream_ptr(stream))
+
+
+def _f8_scales(rows, cols, block_rows):
+    return fp8_scale_shape(rows, cols, block_rows if block_rows > 0 else 1)   # the library refuses others
+
+
+def moe_dequant_fp8(codes, scale, out, block_rows=128, stream=None):
+    rows, cols = out.shape
+    v, code = _device(), dtype_code(out.dtype)
+    return _call("moe_dequant_fp8", _arg(v, "codes", _f8(codes), U8, (rows, cols)),
+                 _arg(v, "scale", scale, F32, _f8_scales(rows, cols, block_rows)), rows, cols, block_rows, code,
                  _arg(v, "out", out, out.dtype, (rows, cols)), stream_ptr(stream))
 
 
@@ -548,6 +645,19 @@ def moe_grouped_swiglu_fwd_mx4(layer, X, perm_token, offsets, T, k, O, ws, strea
                  T, k, _arg(v, "O", O, bf, (T * (k + st.S_shared), st.d)), *_ws(v, ws), stream_ptr(stream))
 
 
+def moe_grouped_swiglu_fwd_fp8_workspace_size(layer, T, k) -> int:
+    return lib().moe_grouped_swiglu_fwd_fp8_workspace_size(ptr(layer), T, k)
+
+
+def moe_grouped_swiglu_fwd_fp8(layer, X, perm_token, offsets, T, k, O, ws, stream=None):
+    st, v, bf = layer.struct if hasattr(layer, "struct") else layer, _device(), torch.bfloat16
+    if hasattr(layer, "tabs") and layer.tabs[0].get_device() != v:
+        raise ValueError(f"the layer's tables are on {layer.tabs[0].device}, the current device is cuda:{v}")
+    return _call("moe_grouped_swiglu_fwd_fp8", ptr(layer), _arg(v, "X", X, bf, (T, st.d)),
+                 _arg(v, "perm_token", perm_token, I32, (T * k,)), _arg(v, "offsets", offsets, I32, (st.S_routed + 1,)),
+                 T, k, _arg(v, "O", O, bf, (T * (k + st.S_shared), st.d)), *_ws(v, ws), stream_ptr(stream))
+
+
 def moe_unpermute(layer, O, inv, perm_gate, T, k, Y, stream=None):
     return _call("moe_unpermute", ptr(layer), ptr(O, FLOAT), ptr(inv, I32), ptr(perm_gate, F32), T, k,
                  ptr(Y, FLOAT), stream_ptr(stream))
@@ -577,6 +687,68 @@ def moe_expert_utility(layer, x_sq, dy_sq, perm_token, perm_gate, offsets, T, k,
     return _call("moe_expert_utility", ptr(layer), ptr(x_sq, F32), ptr(dy_sq, F32), ptr(perm_token, I32),
                  ptr(perm_gate, F32), ptr(offsets, I32), T, k, ptr(ws), ws.numel() * ws.element_size(),
                  ptr(utility, F32), stream_ptr(stream))
+
+
+# ------------------------------------------------------------- gradients ----
+
+def moe_grad_norm_workspace_size() -> int:
+    return lib().moe_grad_norm_workspace_size()
+
+
+def _set_on(dev, name, s):
+    """Address of a TensorSet's struct, whose tables must be on the current GPU `dev`."""
+    if s.tables.get_device() != dev:
+        raise ValueError(f"{name} is on {s.tables.device}, the current device is cuda:{dev}")
+    return ctypes.addressof(s.struct)
+
+
+def moe_grad_norm(grads, sumsq, norm, ws, accumulate=False, stream=None):
+    """grads: a TensorSet; sumsq [1] fp64, norm [1] fp32 (or None) are written."""
+    v = _device()
+    return _call("moe_grad_norm", _set_on(v, "grads", grads), int(bool(accumulate)),
+                 _arg(v, "sumsq", sumsq, torch.float64, (1,)), _arg(v, "norm", norm, F32, (1,)), *_ws(v, ws), stream_ptr(stream))
+
+
+def moe_grad_clip(grads, sumsq, max_norm, out=None, eps=1e-6, stream=None):
+    """Scales grads (a TensorSet) by min(1, max_norm / (sqrt(sumsq) + eps)), in place or into
+    the TensorSet out, whose tensors have the same sizes."""
+    v = _device()
+    if out is not None and out.sizes != grads.sizes:
+        raise ValueError("out has other sizes than grads")
+    return _call("moe_grad_clip", _set_on(v, "grads", grads), _arg(v, "sumsq", sumsq, torch.float64, (1,)), float(max_norm),
+                 float(eps), None if out is None else _set_on(v, "out", out), stream_ptr(stream))
+
+
+class TensorSet:
+    """Device tables of a list of tensors (None: frozen, left out) and the moe_tensor_set
+    struct.  The tensors are dense, of one dtype, on one GPU; they are kept, as the
+    library reads their addresses on the device.  dtype: needed where all are None."""
+
+    def __init__(self, tensors: Sequence[Optional[torch.Tensor]], dtype: Optional[torch.dtype] = None, device=None):
+        self.tensors = list(tensors)
+        if not self.tensors:
+            raise ValueError("no tensors")
+        like = next((t for t in self.tensors if t is not None), None)
+        dtype = dtype if dtype is not None else like.dtype if like is not None else F32
+        code = dtype_code(dtype)
+        dev = like.device if like is not None else torch.device(device if device is not None else "cuda")
+        for i, t in enumerate(self.tensors):
+            if t is None:
+                continue
+            ptr(t, dtype)
+            if t.device != dev:
+                raise ValueError(f"tensors[{i}] is on {t.device}, the set is on {dev}")
+        self.sizes = [0 if t is None else t.numel() for t in self.tensors]
+        start = [0]
+        for n in self.sizes:
+            start.append(start[-1] + n)
+        n = len(self.tensors)
+        # one allocation: the starts, then the addresses from a multiple of 16 bytes on
+        at = (n + 2) // 2 * 2
+        self.tables = torch.tensor(start + [0] * (at - n - 1) + [0 if t is None or not t.numel() else t.data_ptr()
+                                                                 for t in self.tensors], dtype=I64, device=dev)
+        base = self.tables.data_ptr()
+        self.struct = moe_tensor_set(n, code, base + 8 * at, base, start[-1])
 
 
 # ----------------------------------------------------- layer descriptor ----
@@ -632,6 +804,45 @@ class LayerTablesQ8:
         self.struct = moe_layer_q8(d, I, S_routed, S_shared, *[ptr(t) for t in self.tabs])
 
 
+def _addresses(name, x, slots, shape, dt, align, dev):
+    """Device table of the matrices x, one per slot; the library reads their addresses
+    on the device, so alignment and device are checked here."""
+    if len(x) != slots:
+        raise ValueError(f"{name} has {len(x)} matrices for {slots} slots")
+    out = [ptr(_shaped(name, t, shape), dt) for t in x]
+    for i, (p, t) in enumerate(zip(out, x)):
+        if p % align:
+            raise ValueError(f"{name}[{i}] is not {align}-byte aligned")
+        if t.device != dev:
+            raise ValueError(f"{name}[{i}] is on {t.device}, the tables are on {dev}")
+    return torch.tensor(out, dtype=torch.int64, device=dev)
+
+
+def _table_device(device):
+    dev = torch.device(device)
+    if dev.type == "cuda" and dev.index is None and torch.cuda.is_initialized():
+        dev = torch.device("cuda", _device())
+    return dev
+
+
+class LayerTablesFP8:
+    """Device pointer tables of a layer's 8-bit float experts and the moe_layer_fp8
+    struct.  q_*: per-slot codes (uint8 or float8_e4m3fn; routed slots, then shared)
+    and s_* their scales, as moe_quantize_fp8 writes them with block_rows 128 for
+    W_gate, W_up [I,d] and W_down [d,I].  The tensors are kept."""
+
+    def __init__(self, d: int, I: int, S_routed: int, S_shared: int, q_gate, q_up, q_down, s_gate, s_up, s_down,
+                 device="cuda"):
+        S, dev = S_routed + S_shared, _table_device(device)
+        su, sd = fp8_scale_shape(I, d), fp8_scale_shape(d, I)
+        self.keep = [[_f8(t) for t in x] for x in (q_gate, q_up, q_down)] + [list(x) for x in (s_gate, s_up, s_down)]
+        names = ("q_gate", "q_up", "q_down", "s_gate", "s_up", "s_down")
+        shapes = ((I, d), (I, d), (d, I), su, su, sd)
+        self.tabs = [_addresses(n, x, S, sh, U8 if n[0] == "q" else F32, 16 if n[0] == "q" else 4, dev)
+                     for n, x, sh in zip(names, self.keep, shapes)]
+        self.struct = moe_layer_fp8(d, I, S_routed, S_shared, *[ptr(t) for t in self.tabs])
+
+
 class LayerTablesMX4:
     """Device pointer tables of a layer's 4-bit experts and the moe_layer_mx4
     struct.  q_*: per-slot code tensors (routed slots, then shared) and s_*
@@ -641,24 +852,10 @@ class LayerTablesMX4:
 
     def __init__(self, d: int, I: int, S_routed: int, S_shared: int, q_gate, q_up, q_down, s_gate, s_up, s_down,
                  device="cuda"):
-        S = S_routed + S_shared
-
-        def addresses(name, x, shape, align):
-            if len(x) != S:
-                raise ValueError(f"{name} has {len(x)} matrices for {S} slots")
-            out = [ptr(_shaped(name, t, shape), U8) for t in x]
-            for i, (p, t) in enumerate(zip(out, x)):
-                if p % align:
-                    raise ValueError(f"{name}[{i}] is not {align}-byte aligned")
-                if t.device != dev:
-                    raise ValueError(f"{name}[{i}] is on {t.device}, the tables are on {dev}")
-            return torch.tensor(out, dtype=torch.int64, device=dev)
-
-        dev = torch.device(device)
-        if dev.type == "cuda" and dev.index is None and torch.cuda.is_initialized():
-            dev = torch.device("cuda", _device())
+        S, dev = S_routed + S_shared, _table_device(device)
         (cg, sg), (cd, sd) = mxfp4_shapes(I, d), mxfp4_shapes(d, I)
         self.keep = [list(x) for x in (q_gate, q_up, q_down, s_gate, s_up, s_down)]
-        self.tabs = [addresses(*a) for a in (("q_gate", q_gate, cg, 16), ("q_up", q_up, cg, 16), ("q_down", q_down, cd, 16),
-                                             ("s_gate", s_gate, sg, 4), ("s_up", s_up, sg, 4), ("s_down", s_down, sd, 4))]
+        self.tabs = [_addresses(n, x, S, sh, U8, align, dev) for n, x, sh, align in (
+            ("q_gate", q_gate, cg, 16), ("q_up", q_up, cg, 16), ("q_down", q_down, cd, 16),
+            ("s_gate", s_gate, sg, 4), ("s_up", s_up, sg, 4), ("s_down", s_down, sd, 4))]
         self.struct = moe_layer_mx4(d, I, S_routed, S_shared, *[ptr(t) for t in self.tabs])

@@ -1,0 +1,660 @@
+// 8-bit float rows (e4m3 with an fp32 scale per block of 128) and the grouped SwiGLU
+// forward on them (the formulas stand in the header at moe_quantize_fp8 and
+// moe_grouped_swiglu_fwd_fp8).
+//
+// The products run on v_mfma_f32_32x32x64_f8f6f4: a lane holds 32 bytes of one row, lane l
+// row l % 32 and the half l / 32 of the step's k.  A slab is 128 k, a whole scale block, so
+// a slab's sum starts at zero and goes into the tile's sums with one multiplication by the
+// scales: a row's (a lane's) times the weight block's (uniform in a wave).  The instruction
+// aligns the products of 8 consecutive k to the largest sum of their operands' exponents
+// and drops what lies below 2^-13 of that, towards zero (measured; its older 16 k form does
+// the same); the eight's sum joins the others and the accumulator with fp32's bits.  H
+// comes out some 1e-4 off for it.  That is the price of the 8-bit rate: the codes widened
+// to bf16, whose products keep all bits, run at half of it, and the codes themselves are
+// 2^-4 off what they stand for.
+//
+// * A slab row is one 128-byte line; slabs go global -> LDS with global_load_lds_dwordx4, 8
+//   rows per instruction, into two buffers; the scales of 4 slabs of a row (16 bytes)
+//   follow through registers.
+// * Weights are the first operand, so a lane's 16 sums of a 32 x 32 tile belong to one
+//   activation row; weight rows are dealt to the operand's rows so that they are 16
+//   consecutive columns (tile_column).  A tile of gate and up has 128 columns of H, a
+//   scale block: its maximum is 15 comparisons, one exchange and an exchange of four
+//   waves through LDS, and H is quantised in registers.
+// * X and H in the workspace have rows of whole 128-blocks, zero behind the row's end, so
+//   weight chunks past K (clamped reads) meet zero codes.
+#include <type_traits>
+
+#include "debug.hpp"
+#include "ffn_common.hpp"
+#include "ffn_tile.hpp"
+#include "gemm_bf16.hpp"
+#include "grouped_tiles.hpp"
+
+namespace fm {
+namespace {
+
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+
+constexpr float F8_TOP = 448.f;             // the largest e4m3 value
+constexpr float F8_FLOOR = 0x1.cp-118f;     // 448 * 2^-126: no scale below 2^-126
+
+__host__ __device__ constexpr int blocks128(int n) { return (n + 127) / 128; }
+// Scales of an activation row in the workspace: whole groups of 4.
+__host__ __device__ constexpr int scale_row(int nb) { return (nb + 3) / 4 * 4; }
+
+// The scale of a block and what its elements are coded with, from the bits of its
+// largest magnitude.
+struct F8Block {
+  float scale, inv, fix, top;   // top / 448; 448 / top; 512 / top; top / 512
+};
+__device__ __forceinline__ F8Block f8_block(uint32_t bits) {
+  F8Block b;
+  if (bits >= 0x7F800000u) {   // an infinity or a NaN: codes 0
+    b.scale = __uint_as_float(0x7FC00000u);
+    b.inv = b.fix = b.top = 0.f;
+    return b;
+  }
+  const float top = fmaxf(__uint_as_float(bits), F8_FLOOR);
+  b.scale = bits ? top / F8_TOP : 0.f;
+  b.inv = F8_TOP / top;
+  b.fix = b.inv * (512.f / F8_TOP);
+  b.top = top;
+  return b;
+}
+// 448 x / top to within half a step, and exact where it is a number of few bits (a tie):
+// the product with the rounded 448 / top, corrected by its remainder (scaled by 2^-9
+// against overflow; 0.875 x is exact for bf16).  0 for blocks without numbers.
+__device__ __forceinline__ float f8_quotient(float x, const F8Block& b) {
+  if (b.inv == 0.f) return 0.f;
+  const float y = x * b.inv;
+  const float r = fmaf(-(y * 0x1p-9f), b.top, x * 0.875f);
+  return fmaf(r, b.fix, y);
+}
+// Four values as codes, the first in the lowest byte.
+__device__ __forceinline__ uint32_t f8_codes4(const float* v, const F8Block& b) {
+  int c = __builtin_amdgcn_cvt_pk_fp8_f32(f8_quotient(v[0], b), f8_quotient(v[1], b), 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f8_quotient(v[2], b), f8_quotient(v[3], b), c, true);
+}
+
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+template <int N> __device__ __forceinline__ uint32_t top_bits(const float* v) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) top = max(top, abs_bits(v[i]));
+  return top;
+}
+
+// 8 columns from c of a row (0 past cols).
+template <typename T> __device__ __forceinline__ void load8(const T* row, int c, int cols, float (&v)[8]) {
+  if (c < cols) {
+    unpack16(ld16(row + c), v, (T*)nullptr);
+    if constexpr (sizeof(T) == 4) unpack16(ld16(row + c + 4), v + 4, (T*)nullptr);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+  }
+}
+
+// 128 columns of a row in 16 lanes, 8 each: this lane's codes and the block's scale.
+__device__ __forceinline__ u32x2_t quantize128(const float (&v)[8], float& scale) {
+  uint32_t top = top_bits<8>(v);
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+  const F8Block b = f8_block(top);
+  scale = b.scale;
+  return u32x2_t{f8_codes4(v, b), f8_codes4(v + 4, b)};
+}
+
+// Columns [128 blk, 128 blk + 128) of a row to memory; codes up to column code_cols.
+template <typename T>
+__device__ __forceinline__ void quantize_row(const T* row, int cols, int blk, int q, int code_cols, uint8_t* codes,
+                                             float* scale) {
+  const int c = blk * 128 + q * 8;
+  float v[8], s;
+  load8(row, c, cols, v);
+  const u32x2_t code = quantize128(v, s);
+  if (c < code_cols) *(FM_GLOBAL u32x2_t*)(codes + c) = code;
+  if (q == 0) gptr(scale)[blk] = s;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_quantize_f8_rows(const T* __restrict__ W, uint32_t items, int cols, int nb,
+                                                          uint8_t* __restrict__ codes, float* __restrict__ scale) {
+  const uint32_t item = blockIdx.x * 16 + threadIdx.x / 16;
+  if (item >= items) return;
+  const uint32_t r = item / nb;
+  quantize_row(W + (size_t)r * cols, cols, (int)(item - r * nb), threadIdx.x % 16, cols, codes + (size_t)r * cols,
+               scale + (size_t)r * nb);
+}
+
+// A block of 128 x 128: 16 threads to a row, 8 rows each.
+template <typename T>
+__global__ __launch_bounds__(256) void k_quantize_f8(const T* __restrict__ W, int rows, int cols, int nb,
+                                                     uint8_t* __restrict__ codes, float* __restrict__ scale) {
+  __shared__ uint32_t tops[4];
+  const int br = blockIdx.x / nb, bc = blockIdx.x - br * nb, c = bc * 128 + (threadIdx.x % 16) * 8;
+  float v[8][8];
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = br * 128 + 16 * i + threadIdx.x / 16;
+    load8(W + (size_t)min(r, rows - 1) * cols, c, cols, v[i]);   // rows behind the last repeat it
+    top = max(top, top_bits<8>(v[i]));
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+  if (lane_id() == 0) tops[threadIdx.x >> 6] = top;
+  __syncthreads();
+  const F8Block b = f8_block(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = br * 128 + 16 * i + threadIdx.x / 16;
+    if (r < rows && c < cols)
+      *(FM_GLOBAL u32x2_t*)(codes + (size_t)r * cols + c) = u32x2_t{f8_codes4(v[i], b), f8_codes4(v[i] + 4, b)};
+  }
+  if (threadIdx.x == 0) gptr(scale)[(size_t)br * nb + bc] = b.scale;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_dequant_f8(const uint8_t* __restrict__ codes, const float* __restrict__ scale,
+                                                    uint32_t items, int cols, int n8, int row_shift, T* __restrict__ out) {
+  const uint32_t item = blockIdx.x * 256 + threadIdx.x;
+  if (item >= items) return;
+  const uint32_t r = item / n8, c = (item - r * n8) * 8;
+  const u32x2_t code = *(const FM_GLOBAL u32x2_t*)(codes + (size_t)r * cols + c);
+  const float s = gptr(scale)[(size_t)(r >> row_shift) * blocks128(cols) + c / 128];
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)code[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)code[i], true);
+    v[4 * i] = lo[0] * s;
+    v[4 * i + 1] = lo[1] * s;
+    v[4 * i + 2] = hi[0] * s;
+    v[4 * i + 3] = hi[1] * s;
+  }
+  T* o = out + (size_t)r * cols + c;
+  st16(o, pack16(v, (T*)nullptr));
+  if constexpr (sizeof(T) == 4) st16(o + 4, pack16(v + 4, (T*)nullptr));
+}
+
+// ------------------------------------------------------- grouped products ----
+
+struct F8Ptrs {
+  const uint8_t* const* qg;
+  const uint8_t* const* qu;
+  const uint8_t* const* qd;
+  const float* const* sg;
+  const float* const* su;
+  const float* const* sd;
+};
+
+// Workspace: row-tile prefix, X and H as rows of whole 128-blocks with their scales.
+struct F8Ws {
+  int32_t* mbase;
+  uint8_t *xq, *hq;
+  float *xs, *hs;
+};
+inline F8Ws f8_ws_at(void* ws, const moe_layer_fp8* L, int T, int k, size_t* bytes) {
+  const size_t S = L->S_routed + L->S_shared, R = (size_t)T * (k + L->S_shared);
+  const size_t nd = blocks128(L->d), nI = blocks128(L->I);
+  F8Ws w;
+  char* p = (char*)ws;
+  auto take = [&](size_t b) {
+    char* at = p;
+    p += (b + 255) / 256 * 256;
+    return at;
+  };
+  w.mbase = (int32_t*)take((S + 1) * 4);
+  w.xq = (uint8_t*)take((size_t)T * nd * 128);
+  w.xs = (float*)take((size_t)T * scale_row(nd) * 4);
+  w.hq = (uint8_t*)take(R * nI * 128);
+  w.hs = (float*)take(R * scale_row(nI) * 4);
+  *bytes = (size_t)(p - (char*)ws);
+  return w;
+}
+
+// X's tokens as packed rows; the last block builds the row-tile prefix instead.
+__global__ __launch_bounds__(256) void k_f8_prep(const bf16* __restrict__ X, RowArgs ra, int tile_rows, int nb,
+                                                 uint8_t* __restrict__ xq, float* __restrict__ xs,
+                                                 int32_t* __restrict__ mbase) {
+  if (blockIdx.x == gridDim.x - 1) {
+    count_tiles(ra, tile_rows, mbase);
+    return;
+  }
+  const uint32_t item = blockIdx.x * 16 + threadIdx.x / 16;   // below 2^26: T d <= 2^32
+  if (item >= (uint32_t)ra.Tn * nb) return;
+  const uint32_t r = item / nb;
+  quantize_row(X + (size_t)r * ra.d, ra.d, (int)(item - r * nb), threadIdx.x % 16, nb * 128, xq + (size_t)r * nb * 128,
+               xs + (size_t)r * scale_row(nb));
+}
+
+// RA activation rows x RB weight rows by 2 x 4 waves, one block per compute unit.
+template <int RA_> struct F8Cfg {
+  static constexpr int RA = RA_, RB = 256, NW = 8, BPC = 1;
+  static constexpr int TM = RA / 2, TN = RB / 4, MI = TM / 32, NJ = TN / 32;
+  static constexpr int A_BYTES = RA * 128, SLAB = A_BYTES + RB * 128;   // 128 k
+  static constexpr int A_INS = RA / 8 / NW, B_INS = RB / 8 / NW;        // 8 rows each, per wave
+  static constexpr int SCALES = RA * 16;                                // of 4 slabs
+  static constexpr int LDS = 2 * (SLAB + SCALES);
+  static_assert(RA % 64 == 0 && NJ == 2 && RA <= 64 * NW, "tile");
+  static_assert(LDS <= 160 * 1024, "LDS");
+};
+
+// Chunk swizzles of a 128-byte slab row: 16 consecutive lanes' rows at one logical
+// chunk on distinct 4-bank groups; lanes read activation rows in order, weight rows in
+// the order of tile_column.
+__device__ __forceinline__ int f8_swz_a(int r) { return (r >> 1) & 7; }
+__device__ __forceinline__ int f8_swz_b(int r) { return ((r >> 1) & 3) | ((r >> 2) & 4); }
+
+// One operand pair of a tile, rows relative to it.  w2: the second of two matrices
+// whose 32-row blocks alternate (gate, up).
+struct F8Tile {
+  const uint8_t* x;             // activations' codes
+  const float* xs;              // and scales
+  const int32_t* tok;           // row -> activation row (gathered), or NULL
+  int rows, Tn;                 // activation rows of the tile's slot from the tile on
+  const uint8_t *w, *w2;
+  const float* s[2];            // this wave's weight scales by slab, of its two 32-column blocks
+  int wrows;                    // weight rows (per matrix) from the tile on
+  int nk, kw;                   // slabs; 16-byte chunks of a weight row
+};
+
+// acc += X W^T.  LDS: two slabs, then two groups of scales [RA rows][16 bytes].  The
+// barrier at the top of slab kt says that it has landed and that every wave has read slab
+// kt - 1, whose buffer then takes slab kt + 1.  Scales of group g (slabs 4 g to 4 g + 3)
+// are requested at slab 4 g - 2 and put into LDS at slab 4 g - 1.
+template <class C, bool PAIR>
+__device__ __forceinline__ void f8_gemm(const F8Tile& t, FM_LDS char* lds, f32x16_t (&acc)[C::MI][C::NJ]) {
+  const int lane = lane_id(), wave = wave_id();
+  const int nk = t.nk;
+  const uint32_t ldx = nk * 128, ldw = t.kw * 16;
+  FM_LDS char* const sc = lds + 2 * C::SLAB;
+  uint32_t oa[C::A_INS], ob[C::B_INS];
+  auto xrow = [&](int r) {
+    r = min(r, t.rows - 1);
+    return (uint32_t)(t.tok ? min(max(gptr(t.tok)[r], 0), t.Tn - 1) : r);
+  };
+#pragma unroll
+  for (int u = 0; u < C::A_INS; ++u) {
+    const int r = 8 * (wave * C::A_INS + u) + (lane >> 3);
+    oa[u] = xrow(r) * ldx + 16 * ((lane & 7) ^ f8_swz_a(r));
+  }
+#pragma unroll
+  for (int u = 0; u < C::B_INS; ++u) {
+    const int r = 8 * (wave * C::B_INS + u) + (lane >> 3);
+    ob[u] = (uint32_t)min(PAIR ? 32 * (r >> 6) + (r & 31) : r, t.wrows - 1) * ldw + 16 * ((lane & 7) ^ f8_swz_b(r));
+  }
+  // behind a row's end, weights repeat their row's last chunk (it meets zeros)
+  auto issue = [&](int slab) {
+    FM_LDS char* const l = lds + (slab & 1) * C::SLAB;
+#pragma unroll
+    for (int u = 0; u < C::A_INS; ++u)
+      dma16s(t.x + (size_t)slab * 128, oa[u], l + (wave * C::A_INS + u) * 1024);
+#pragma unroll
+    for (int u = 0; u < C::B_INS; ++u) {
+      const int ins = wave * C::B_INS + u;
+      const uint8_t* const w = (PAIR && ((ins >> 2) & 1) ? t.w2 : t.w) + (size_t)slab * 128;
+      uint32_t o = ob[u];
+      if (8 * slab + 8 > t.kw) {
+        const int k = (lane & 7) ^ f8_swz_b(8 * ins + (lane >> 3));
+        o += 16 * (min(k, t.kw - 1 - 8 * slab) - k);
+      }
+      dma16s(w, o, l + C::A_BYTES + ins * 1024);
+    }
+  };
+  // waves below RA / 64 keep a row's scales per lane
+  const int sr = 64 * wave + lane;
+  const bool keeper = 64 * wave < C::RA;
+  const float* sp = t.xs;
+  if (keeper) sp += (size_t)xrow(sr) * scale_row(nk);
+  auto put_scales = [&](int g, const u32x4_t& v) {
+    if (keeper) *(FM_LDS u32x4_t*)(sc + (g & 1) * C::SCALES + sr * 16) = v;
+  };
+  const int row0 = (wave & 1) * C::TM, col0 = (wave >> 1) * C::TN;
+  const int m = lane & 31, h = lane >> 5;
+  uint32_t fa[C::MI], fb[C::NJ];
+#pragma unroll
+  for (int i = 0; i < C::MI; ++i) {
+    const int r = row0 + 32 * i + m;
+    fa[i] = r * 128 + ((h ^ f8_swz_a(r)) << 4);
+  }
+#pragma unroll
+  for (int j = 0; j < C::NJ; ++j) {
+    const int r = col0 + 32 * j + tile_column(m);
+    fb[j] = C::A_BYTES + r * 128 + ((h ^ f8_swz_b(r)) << 4);
+  }
+  const uint32_t ga = (row0 + m) * 16;
+#pragma unroll
+  for (int i = 0; i < C::MI; ++i)
+#pragma unroll
+    for (int j = 0; j < C::NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  issue(0);
+  if (keeper) put_scales(0, ld16(sp));
+  u32x4_t next = {0, 0, 0, 0};
+  float w0 = ld_scalar(t.s[0]), w1 = ld_scalar(t.s[1]);
+#pragma nounroll
+  for (int kt = 0; kt < nk; ++kt) {
+    wait_vmcnt<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (kt + 1 < nk) issue(kt + 1);
+    if ((kt & 3) == 2 && kt + 2 < nk && keeper) next = ld16(sp + kt + 2);
+    if ((kt & 3) == 3 && kt + 1 < nk) put_scales((kt >> 2) + 1, next);
+    const float sw[2] = {w0, w1};
+    const int kn = min(kt + 1, nk - 1);
+    w0 = ld_scalar(t.s[0] + kn);
+    w1 = ld_scalar(t.s[1] + kn);
+    const FM_LDS char* const l = lds + (kt & 1) * C::SLAB;
+    const FM_LDS char* const s = sc + ((kt >> 2) & 1) * C::SCALES + ga + 4 * (kt & 3);
+    auto frag = [&](uint32_t at, int step) {   // 64 k: chunks 4 step + h and 4 step + 2 + h
+      int flip = step << 6;
+      asm volatile("" : "+s"(flip));   // not hoisted: the addresses would take the registers of the sums
+      const u32x4_t a = *(const FM_LDS u32x4_t*)(l + (at ^ flip));
+      const u32x4_t b = *(const FM_LDS u32x4_t*)(l + (at ^ (flip + 32)));
+      return i32x8_t{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+    };
+    i32x8_t xb[2][C::NJ];
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int j = 0; j < C::NJ; ++j) xb[st][j] = frag(fb[j], st);
+    const f32x16_t zero = {};
+#pragma unroll
+    for (int i = 0; i < C::MI; ++i) {
+      const i32x8_t x0 = frag(fa[i], 0), x1 = frag(fa[i], 1);
+      const float sx = *(const FM_LDS float*)(s + 512 * i);
+#pragma unroll
+      for (int j = 0; j < C::NJ; ++j) {
+        f32x16_t p = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xb[0][j], x0, zero, 0, 0, 0, 0, 0, 0);
+        p = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xb[1][j], x1, p, 0, 0, 0, 0, 0, 0);
+        const float f = sx * sw[j];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = fmaf(p[e], f, acc[i][j][e]);
+      }
+    }
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+struct F8Args {
+  F8Ptrs W;
+  F8Ws w;
+  const int32_t* perm_token;
+  RowArgs ra;
+  bf16* O;
+};
+
+// H = F8(silu(F8(X) Qg^T) (F8(X) Qu^T)) of one tile, 128 columns.  tops: [RA][4] dwords
+// that the next tile's first slab and scales leave alone.
+template <class C>
+__device__ __forceinline__ void f8_gate_up_tile(const F8Args& a, FM_LDS char* lds, FM_LDS uint32_t* tops, const TileRows& r) {
+  const RowArgs& ra = a.ra;
+  const int I = ra.I, nI = blocks128(I), nd = blocks128(ra.d), n0 = r.n * 128;
+  F8Tile t;
+  t.x = a.w.xq + (r.sr.shared ? (size_t)r.m0 * nd * 128 : 0);
+  t.xs = a.w.xs + (r.sr.shared ? (size_t)r.m0 * scale_row(nd) : 0);
+  t.tok = r.sr.shared ? nullptr : a.perm_token + r.sr.xrow0 + r.m0;
+  t.rows = r.rows;
+  t.Tn = ra.Tn;
+  t.w = ld_scalar(a.W.qg + r.s) + (size_t)n0 * ra.d;
+  t.w2 = ld_scalar(a.W.qu + r.s) + (size_t)n0 * ra.d;
+  t.s[0] = ld_scalar(a.W.sg + r.s) + (size_t)r.n * nd;
+  t.s[1] = ld_scalar(a.W.su + r.s) + (size_t)r.n * nd;
+  t.wrows = I - n0;
+  t.nk = nd;
+  t.kw = ra.d / 16;
+  f32x16_t acc[C::MI][C::NJ];
+  f8_gemm<C, true>(t, lds, acc);
+  const int lane = lane_id_here(), wave = wave_id(), h = lane >> 5, part = wave >> 1;
+  const int row0 = (wave & 1) * C::TM + (lane & 31), col = n0 + part * 32 + 16 * h;
+#pragma unroll
+  for (int i = 0; i < C::MI; ++i) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float g = acc[i][0][e];
+      acc[i][0][e] = col + e < I ? g * sigm_fast(g) * acc[i][1][e] : 0.f;
+      top = max(top, abs_bits(acc[i][0][e]));
+    }
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+    if (h == 0) tops[(row0 + 32 * i) * 4 + part] = top;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < C::MI; ++i) {
+    const int row = row0 + 32 * i;
+    const u32x4_t tp = *(const FM_LDS u32x4_t*)(tops + row * 4);
+    const F8Block b = f8_block(max(max(tp[0], tp[1]), max(tp[2], tp[3])));
+    float v[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = acc[i][0][e];
+    if (row < r.rows) {
+      st16(a.w.hq + (r.ob + row) * (nI * 128) + col,
+           u32x4_t{f8_codes4(v, b), f8_codes4(v + 4, b), f8_codes4(v + 8, b), f8_codes4(v + 12, b)});
+      if (part == 0 && h == 0) gptr(a.w.hs)[(r.ob + row) * scale_row(nI) + r.n] = b.scale;
+    }
+  }
+}
+
+// O = F8(H) Qd^T of one tile, 256 columns.  A wave's 32 rows x 64 columns go out through
+// LDS, so that a store covers whole lines of 8 rows.  stage: 4 KB per wave that the next
+// tile's first slab and scales leave alone.
+template <class C>
+__device__ __forceinline__ void f8_down_tile(const F8Args& a, FM_LDS char* lds, FM_LDS char* stage, const TileRows& r) {
+  const RowArgs& ra = a.ra;
+  const int d = ra.d, nI = blocks128(ra.I), n0 = r.n * C::RB;
+  F8Tile t;
+  t.x = a.w.hq + r.ob * (nI * 128);
+  t.xs = a.w.hs + r.ob * scale_row(nI);
+  t.tok = nullptr;
+  t.rows = r.rows;
+  t.Tn = ra.Tn;
+  t.w = ld_scalar(a.W.qd + r.s) + (size_t)n0 * ra.I;
+  t.w2 = nullptr;
+  // (columns behind d repeat its last block's scale; they are not stored)
+  const int blk = min((n0 + (wave_id() >> 1) * C::TN) / 128, blocks128(d) - 1);
+  t.s[0] = t.s[1] = ld_scalar(a.W.sd + r.s) + (size_t)blk * nI;
+  t.wrows = d - n0;
+  t.nk = nI;
+  t.kw = ra.I / 16;
+  f32x16_t acc[C::MI][C::NJ];
+  f8_gemm<C, false>(t, lds, acc);
+  const int lane = lane_id_here(), wave = wave_id(), h = lane >> 5;
+  FM_LDS char* const mine = stage + wave * 4096;   // [32 rows][8 chunks of 16 bytes], chunks swizzled by the row
+  const int m = lane & 31, col = n0 + (wave >> 1) * C::TN + 8 * (lane & 7);
+#pragma unroll
+  for (int i = 0; i < C::MI; ++i) {
+#pragma unroll
+    for (int j = 0; j < C::NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; e += 8) {
+        float v[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] = acc[i][j][e + x];
+        *(FM_LDS u32x4_t*)(mine + m * 128 + (((4 * j + 2 * h + e / 8) ^ (m & 7)) << 4)) = pack16(v, (bf16*)nullptr);
+      }
+    wave_lds_fence();
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int q = 8 * u + (lane >> 3), row = (wave & 1) * C::TM + 32 * i + q;
+      const u32x4_t v = *(const FM_LDS u32x4_t*)(mine + q * 128 + (((lane & 7) ^ (q & 7)) << 4));
+      if (row < r.rows && col < d) st16(a.O + (r.ob + row) * d + col, v);
+    }
+    wave_lds_fence();
+  }
+}
+
+template <class C, class BIG, bool DOWN>
+__device__ __forceinline__ void f8_tile(const F8Args& a, FM_LDS char* lds, const TileRows& r) {
+  // what an epilogue keeps in LDS lies behind the larger tile's first slab, inside the
+  // second slab of either height: the next tile requests that one only behind its first
+  // barrier
+  static_assert(BIG::SLAB + BIG::NW * 4096 <= 2 * C::SLAB, "stage");
+  if constexpr (DOWN) f8_down_tile<C>(a, lds, lds + BIG::SLAB, r);
+  else f8_gate_up_tile<C>(a, lds, (FM_LDS uint32_t*)(lds + BIG::SLAB), r);
+}
+
+// C: the tile; HALF: its half-height form for tiles with at most half the rows left.
+template <class C, class HALF, bool DOWN> __global__ __launch_bounds__(64 * C::NW, C::NW / 4) void k_f8_tiles(F8Args a) {
+  __shared__ __align__(16) char lds_[C::LDS];
+  FM_LDS char* const lds = (FM_LDS char*)lds_;
+  constexpr int COLS = DOWN ? C::RB : C::RB / 2;
+  const int NT = ((DOWN ? a.ra.d : a.ra.I) + COLS - 1) / COLS;
+  const TileWalk walk = tile_walk(a.ra, NT);
+  for (int tt = walk.at; tt < walk.end; tt += walk.step) {
+    const TileRows r = tile_rows_at(a.ra, tt, NT, C::RA);
+    if (r.rows <= HALF::RA) f8_tile<HALF, C, DOWN>(a, lds, r);
+    else f8_tile<C, C, DOWN>(a, lds, r);
+  }
+}
+
+typedef F8Cfg<256> E256;
+typedef F8Cfg<128> E128;
+typedef F8Cfg<64> E64;
+
+template <class C, class HALF> void f8_tiles(const F8Args& a, const bf16* X, hipStream_t st) {
+  const RowArgs& ra = a.ra;
+  const int nb = blocks128(ra.d);
+  hipLaunchKernelGGL(k_f8_prep, dim3(cdiv((long)ra.Tn * nb, 16) + 1), dim3(256), 0, st, X, ra, C::RA, nb, a.w.xq, a.w.xs,
+                     a.w.mbase);
+  hipLaunchKernelGGL((k_f8_tiles<C, HALF, false>), tile_grid<C>(ra, cdiv(ra.I, C::RB / 2)), dim3(64 * C::NW), 0, st, a);
+  hipLaunchKernelGGL((k_f8_tiles<C, HALF, true>), tile_grid<C>(ra, cdiv(ra.d, C::RB)), dim3(64 * C::NW), 0, st, a);
+}
+
+int check_rows(const void* a, const char* an, const void* b, const char* bn, const void* c, const char* cn, long rows,
+               int cols, int block_rows) {
+  if (rows <= 0 || cols <= 0) return fail(MOE_ERR_ARG, "rows=%ld cols=%d", rows, cols);
+  if (cols % 8 || cols > 1 << 30) return fail(MOE_ERR_UNSUPPORTED, "cols=%d not a multiple of 8 up to 2^30", cols);
+  if (block_rows != 1 && block_rows != 128) return fail(MOE_ERR_UNSUPPORTED, "block_rows=%d: expected 1 or 128", block_rows);
+  FM_TRY(need(a, an)); FM_TRY(need(b, bn)); FM_TRY(need(c, cn));
+  FM_TRY(need_aligned(a, an)); FM_TRY(need_aligned(b, bn)); FM_TRY(need_aligned(c, cn));
+  return MOE_OK;
+}
+
+// Slots that may hold rows.
+long f8_active(const moe_layer_fp8* L, int T, int k) {
+  const long R = (long)T * k;
+  return (R < L->S_routed ? R : L->S_routed) + L->S_shared;
+}
+
+}  // namespace
+
+int fp8_tile(const moe_layer_fp8* L, int T, int k) {
+  const double r = (double)T * (k + L->S_shared) / f8_active(L, T, k);
+  return r >= 192 ? 256 : 128;
+}
+
+}  // namespace fm
+
+using namespace fm;
+
+extern "C" int moe_quantize_fp8(const void* W, int dtype, long rows, int cols, int block_rows, uint8_t* codes, float* scale,
+                                void* stream) {
+  clear_error();
+  FM_TRY(need_dtype_float(dtype, "dtype"));
+  FM_TRY(check_rows(W, "W", codes, "codes", scale, "scale", rows, cols, block_rows));
+  hipStream_t st = as_stream(stream);
+  const int nb = blocks128(cols), es = esize(dtype);
+  // launches of less than 2^32 threads: 2^27 row blocks of 16 threads, or 2^23 blocks of 256
+  const long step = block_rows == 1 ? (1L << 27) / nb : (1L << 23) / nb * 128;   // nb <= 2^23
+  for (long r = 0; r < rows; r += step) {
+    const long n = rows - r < step ? rows - r : step;
+    const char* w = (const char*)W + (size_t)r * cols * es;
+    uint8_t* q = codes + (size_t)r * cols;
+    float* s = scale + (size_t)(r / block_rows) * nb;
+    if (block_rows == 1) {
+      const uint32_t items = (uint32_t)(n * nb);
+      if (dtype == MOE_BF16)
+        hipLaunchKernelGGL(k_quantize_f8_rows<bf16>, dim3(cdiv(items, 16)), dim3(256), 0, st, (const bf16*)w, items, cols, nb,
+                           q, s);
+      else
+        hipLaunchKernelGGL(k_quantize_f8_rows<float>, dim3(cdiv(items, 16)), dim3(256), 0, st, (const float*)w, items, cols,
+                           nb, q, s);
+    } else {
+      const dim3 grid((unsigned)(cdiv(n, 128) * (long)nb));
+      if (dtype == MOE_BF16)
+        hipLaunchKernelGGL(k_quantize_f8<bf16>, grid, dim3(256), 0, st, (const bf16*)w, (int)n, cols, nb, q, s);
+      else
+        hipLaunchKernelGGL(k_quantize_f8<float>, grid, dim3(256), 0, st, (const float*)w, (int)n, cols, nb, q, s);
+    }
+  }
+  return check_launch("moe_quantize_fp8");
+}
+
+extern "C" int moe_dequant_fp8(const uint8_t* codes, const float* scale, long rows, int cols, int block_rows, int out_dtype,
+                               void* out, void* stream) {
+  clear_error();
+  FM_TRY(need_dtype_float(out_dtype, "out_dtype"));
+  FM_TRY(check_rows(codes, "codes", scale, "scale", out, "out", rows, cols, block_rows));
+  const int n8 = cols / 8, es = esize(out_dtype), shift = block_rows == 1 ? 0 : 7;
+  // launches of less than 2^31 items, a thread each, so that the kernel divides 32-bit
+  // numbers; of whole row blocks (a row has up to 2^27 items: then row by row within a block)
+  const long fit = 0x7FFFFFF0L / n8, step = fit >= block_rows ? fit / block_rows * block_rows : fit;
+  for (long r = 0; r < rows;) {
+    long n = rows - r < step ? rows - r : step;
+    const long in_block = block_rows - r % block_rows;   // a launch's first row begins a block, or the launch stays in one
+    if (r % block_rows && n > in_block) n = in_block;
+    const uint32_t items = (uint32_t)(n * n8);
+    const uint8_t* q = codes + (size_t)r * cols;
+    const float* s = scale + (size_t)(r / block_rows) * blocks128(cols);
+    char* o = (char*)out + (size_t)r * cols * es;
+    if (out_dtype == MOE_BF16)
+      hipLaunchKernelGGL(k_dequant_f8<bf16>, dim3(cdiv(items, 256)), dim3(256), 0, as_stream(stream), q, s, items, cols, n8,
+                         shift, (bf16*)o);
+    else
+      hipLaunchKernelGGL(k_dequant_f8<float>, dim3(cdiv(items, 256)), dim3(256), 0, as_stream(stream), q, s, items, cols, n8,
+                         shift, (float*)o);
+    r += n;
+  }
+  return check_launch("moe_dequant_fp8");
+}
+
+extern "C" size_t moe_grouped_swiglu_fwd_fp8_workspace_size(const moe_layer_fp8* L, int T, int k) {
+  if (!L || T < 0 || k <= 0 || L->d <= 0 || L->I <= 0 || L->S_routed < 0 || L->S_shared < 0) return 0;
+  size_t bytes;
+  f8_ws_at(nullptr, L, T, k, &bytes);
+  return bytes;
+}
+
+extern "C" int moe_grouped_swiglu_fwd_fp8(const moe_layer_fp8* L, const void* X, const int32_t* perm_token,
+                                          const int32_t* offsets, int T, int k, void* O, void* ws, size_t ws_bytes,
+                                          void* stream) {
+  clear_error();
+  if (!L) return fail(MOE_ERR_ARG, "layer must not be NULL");
+  if (L->d <= 0 || L->I <= 0) return fail(MOE_ERR_ARG, "layer d=%d I=%d", L->d, L->I);
+  if (L->d % 16 || L->I % 16 || L->d > 1 << 30 || L->I > 1 << 30)
+    return fail(MOE_ERR_UNSUPPORTED, "8-bit float layer d=%d I=%d must be multiples of 16 up to 2^30", L->d, L->I);
+  if (L->S_routed < 0 || L->S_shared < 0 || L->S_routed + L->S_shared < 1 || L->S_routed > 512 || L->S_shared > 511)
+    return fail(MOE_ERR_ARG, "layer S_routed=%d S_shared=%d", L->S_routed, L->S_shared);
+  // byte offsets within a matrix, and of a token's row, are 32 bits wide
+  if (128LL * blocks128(L->d) * 128 * blocks128(L->I) > (1LL << 32))
+    return fail(MOE_ERR_UNSUPPORTED, "8-bit float layer d=%d I=%d: more than 2^32 weights in a matrix", L->d, L->I);
+  FM_TRY(need(L->q_gate, "layer q_gate")); FM_TRY(need(L->q_up, "layer q_up")); FM_TRY(need(L->q_down, "layer q_down"));
+  FM_TRY(need(L->s_gate, "layer s_gate")); FM_TRY(need(L->s_up, "layer s_up")); FM_TRY(need(L->s_down, "layer s_down"));
+  if (T < 0 || k <= 0 || k > 16) return fail(MOE_ERR_ARG, "T=%d k=%d", T, k);
+  if (128LL * T * blocks128(L->d) > (1LL << 32))
+    return fail(MOE_ERR_UNSUPPORTED, "T=%d tokens of d=%d: more than 2^32 values", T, L->d);
+  if (T == 0) return MOE_OK;
+  FM_TRY(need(X, "X")); FM_TRY(need(offsets, "offsets")); FM_TRY(need(O, "O")); FM_TRY(need(ws, "ws"));
+  if (L->S_routed > 0) FM_TRY(need(perm_token, "perm_token"));
+  FM_TRY(need_aligned(X, "X")); FM_TRY(need_aligned(perm_token, "perm_token")); FM_TRY(need_aligned(offsets, "offsets"));
+  FM_TRY(need_aligned(O, "O")); FM_TRY(need_aligned(ws, "ws"));
+  size_t bytes;
+  const F8Ws w = f8_ws_at(ws, L, T, k, &bytes);
+  if (ws_bytes < bytes) return fail(MOE_ERR_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, bytes);
+  hipStream_t st = as_stream(stream);
+  if (debug_checks() && L->S_routed > 0) {
+    int rows = 0;
+    FM_TRY(debug_check_offsets(offsets, L->S_routed, T, k, st));
+    FM_TRY(debug_rows(offsets, L->S_routed, st, &rows));
+    FM_TRY(debug_check_tokens(perm_token, rows, T, st));
+  }
+  const RowArgs ra{offsets, w.mbase, L->S_routed, L->S_routed + L->S_shared, T, k, L->d, L->I, L->I};
+  const F8Args a{{L->q_gate, L->q_up, L->q_down, L->s_gate, L->s_up, L->s_down}, w, perm_token, ra, (bf16*)O};
+  if (fp8_tile(L, T, k) == 256) f8_tiles<E256, E128>(a, (const bf16*)X, st);
+  else f8_tiles<E128, E64>(a, (const bf16*)X, st);
+  return check_launch("moe_grouped_swiglu_fwd_fp8");
+}

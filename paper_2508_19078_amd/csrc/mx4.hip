@@ -31,6 +31,7 @@
 #include "ffn_common.hpp"
 #include "ffn_tile.hpp"
 #include "gemm_bf16.hpp"
+#include "grouped_tiles.hpp"
 
 namespace fm {
 namespace {
@@ -239,80 +240,12 @@ inline MxWs mx_ws_at(void* ws, const moe_layer_mx4* L, int T, int k, size_t* byt
   return w;
 }
 
-// Row tiles before each slot, tiles[s] for s in [0, S]: one block of 256 threads,
-// thread i the slots 4 i to 4 i + 3 (S <= 1023).
-__device__ __forceinline__ void mx_count_tiles(const RowArgs& ra, int tile_rows, int32_t* tiles) {
-  __shared__ int wave_sum[4];
-  const int s0 = threadIdx.x * 4, lane = lane_id(), wave = threadIdx.x >> 6;
-  int n[4], own = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int s = s0 + i;
-    const int rows = s < ra.S_r ? ra.offsets[s + 1] - ra.offsets[s] : s < ra.S ? ra.Tn : 0;
-    n[i] = (rows + tile_rows - 1) / tile_rows;
-    own += n[i];
-  }
-  int before = own;   // inclusive over the wave's lanes
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(before, o);
-    if (lane >= o) before += v;
-  }
-  if (lane == 63) wave_sum[wave] = before;
-  __syncthreads();
-  before -= own;
-  for (int w = 0; w < wave; ++w) before += wave_sum[w];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (s0 + i <= ra.S) tiles[s0 + i] = before;
-    before += n[i];
-  }
-}
-
-// A block's tiles of a grouped product with NT column tiles: XCD x (blocks go to
-// the XCDs in turn) walks its eighth of them, slot by slot, so that the row tiles
-// of a slot, which share its weights, meet in one L2.
-struct MxWalk {
-  int at, end, step;
-};
-__device__ __forceinline__ MxWalk mx_walk(const RowArgs& ra, int NT) {
-  const long long all = (long long)ld_scalar(ra.mbase + ra.S) * NT;
-  const int x = blockIdx.x % N_XCD;
-  return MxWalk{(int)(all * x / N_XCD) + (int)(blockIdx.x / N_XCD), (int)(all * (x + 1) / N_XCD),
-                (int)(gridDim.x / N_XCD)};
-}
-
-struct MxRows {
-  SlotRows sr;
-  int s, m0, n;   // slot, first row in it, column tile
-  int rows;       // rows of the slot from m0 on
-  size_t ob;      // m0's row in the per-row buffers
-};
-__device__ __forceinline__ MxRows mx_rows(const RowArgs& ra, int t, int NT, int tile_rows) {
-  const int m = t / NT;
-  int s = 0;   // the slots that end at or before row tile m
-  for (int b = 0; b < ra.S; b += 64) {
-    const int i = b + lane_id();
-    s += __builtin_popcountll(__ballot(i < ra.S && gptr(ra.mbase)[min(i, ra.S - 1) + 1] <= m));
-  }
-  MxRows r;
-  r.s = __builtin_amdgcn_readfirstlane(s);
-  const int first = ld_scalar(ra.mbase + r.s), count = ld_scalar(ra.mbase + r.s + 1) - first;
-  int mt;
-  band_order(t - first * NT, count, NT, 8, mt, r.n);
-  r.sr = slot_rows(r.s, ra.offsets, ra.S_r, ra.Tn, ra.k);
-  r.m0 = mt * tile_rows;
-  r.rows = r.sr.nrows - r.m0;
-  r.ob = (size_t)(r.sr.orow0 + r.m0);
-  return r;
-}
-
 // X's tokens as packed rows; the last block builds the row-tile prefix instead.
 __global__ __launch_bounds__(256) void k_mx_prep(const bf16* __restrict__ X, RowArgs ra, int tile_rows, int nb,
                                                  uint8_t* __restrict__ xq, uint8_t* __restrict__ xs,
                                                  int32_t* __restrict__ mbase) {
   if (blockIdx.x == gridDim.x - 1) {
-    mx_count_tiles(ra, tile_rows, mbase);
+    count_tiles(ra, tile_rows, mbase);
     return;
   }
   const uint32_t item = blockIdx.x * 16 + threadIdx.x / 16;   // below 2^26: T up128(d) <= 2^32
@@ -512,7 +445,7 @@ struct MxArgs {
 };
 
 // H = MX(silu(MX(X) Qg^T) (MX(X) Qu^T)) of one tile, RB / 2 columns.
-template <class C> __device__ __forceinline__ void mx_gate_up_tile(const MxArgs& a, FM_LDS char* lds, const MxRows& r) {
+template <class C> __device__ __forceinline__ void mx_gate_up_tile(const MxArgs& a, FM_LDS char* lds, const TileRows& r) {
   const RowArgs& ra = a.ra;
   const int I = ra.I, nI = act_blocks(I), kd = act_blocks(ra.d), n0 = r.n * (C::RB / 2);
   const size_t lw = up32(ra.d) / 2, ls = up128(ra.d) / 32;
@@ -567,7 +500,7 @@ template <class C> __device__ __forceinline__ void mx_gate_up_tile(const MxArgs&
 // rows, 16 bytes of each).  stage: 4 KB per wave that the next tile's first slab and
 // scales leave alone, whichever its height.
 template <class C>
-__device__ __forceinline__ void mx_down_tile(const MxArgs& a, FM_LDS char* lds, FM_LDS char* stage, const MxRows& r) {
+__device__ __forceinline__ void mx_down_tile(const MxArgs& a, FM_LDS char* lds, FM_LDS char* stage, const TileRows& r) {
   const RowArgs& ra = a.ra;
   const int d = ra.d, nI = act_blocks(ra.I), n0 = r.n * C::RB;
   MxTile t;
@@ -610,7 +543,7 @@ __device__ __forceinline__ void mx_down_tile(const MxArgs& a, FM_LDS char* lds, 
 }
 
 template <class C, class BIG, bool DOWN>
-__device__ __forceinline__ void mx_tile(const MxArgs& a, FM_LDS char* lds, const MxRows& r) {
+__device__ __forceinline__ void mx_tile(const MxArgs& a, FM_LDS char* lds, const TileRows& r) {
   // the first 4 KB per wave behind the larger tile's first slab: inside the second slab
   // of either height, which the next tile requests only behind its first barrier
   static_assert(BIG::SLAB + BIG::NW * 4096 <= 2 * C::SLAB, "stage");
@@ -624,9 +557,9 @@ template <class C, class HALF, bool DOWN> __global__ __launch_bounds__(64 * C::N
   FM_LDS char* const lds = (FM_LDS char*)lds_;
   constexpr int COLS = DOWN ? C::RB : C::RB / 2;
   const int NT = ((DOWN ? a.ra.d : a.ra.I) + COLS - 1) / COLS;
-  const MxWalk walk = mx_walk(a.ra, NT);
+  const TileWalk walk = tile_walk(a.ra, NT);
   for (int tt = walk.at; tt < walk.end; tt += walk.step) {
-    const MxRows r = mx_rows(a.ra, tt, NT, C::RA);
+    const TileRows r = tile_rows_at(a.ra, tt, NT, C::RA);
     if (r.rows <= HALF::RA) mx_tile<HALF, C, DOWN>(a, lds, r);
     else mx_tile<C, C, DOWN>(a, lds, r);
   }
@@ -649,30 +582,6 @@ typedef MxCfg<64, 128, 2, 2> Q64;
 // was bound by vector instructions).  H goes through the workspace in fp32 and is
 // quantised the same way.  Rows come 16 at a time.  Blocks exist for the slots that may
 // hold rows only: the i-th of them is found by a ballot over the offsets.
-
-// The i-th slot with rows (s = -1: there is none), and its rows.
-__device__ __forceinline__ int mx_active_slot(const RowArgs& ra, int i, SlotRows& sr) {
-  int before = 0;
-  for (int b = 0; b < ra.S; b += 64) {
-    const int s = b + lane_id(), sc = max(min(s, ra.S_r - 1), 0);
-    int lo = 0, hi = 0;
-    if (ra.S_r > 0) lo = gptr(ra.offsets)[sc], hi = gptr(ra.offsets)[sc + 1];
-    unsigned long long m = __ballot(s < ra.S && (s >= ra.S_r || hi > lo));
-    const int n = __builtin_popcountll(m);
-    if (i < before + n) {
-      for (int drop = i - before; drop > 0; --drop) m &= m - 1;
-      const int at = __builtin_amdgcn_readfirstlane(__builtin_ctzll(m)), sl = b + at;
-      sr.shared = sl >= ra.S_r;
-      const int first = __builtin_amdgcn_readlane(lo, at);
-      sr.nrows = sr.shared ? ra.Tn : __builtin_amdgcn_readlane(hi, at) - first;
-      sr.xrow0 = sr.shared ? 0 : first;
-      sr.orow0 = sr.shared ? (long)ra.Tn * ra.k + (long)(sl - ra.S_r) * ra.Tn : first;
-      return sl;
-    }
-    before += n;
-  }
-  return -1;
-}
 
 // Rows of nb 128-blocks in LDS: codes, then scales; padded so that 16 rows' chunks at
 // one place lie on different banks.
@@ -769,7 +678,7 @@ __global__ __launch_bounds__(64 * NW) void k_mx_few_gate_up(MxArgs a, const bf16
   FM_LDS f32x4_t* const red = (FM_LDS f32x4_t*)mx_few_lds;
   const RowArgs& ra = a.ra;
   SlotRows sr;
-  const int sl = mx_active_slot(ra, blockIdx.x / NT, sr);
+  const int sl = active_slot(ra, blockIdx.x / NT, sr);
   if (sl < 0) return;
   const int n0 = (blockIdx.x % NT) * 8, I = ra.I, kd = up128(ra.d) / 128;
   const int lane = lane_id(), r16 = lane & 15;
@@ -805,7 +714,7 @@ __global__ __launch_bounds__(64 * NW) void k_mx_few_down(MxArgs a, int NT, int m
   FM_LDS f32x4_t* const red = (FM_LDS f32x4_t*)mx_few_lds;
   const RowArgs& ra = a.ra;
   SlotRows sr;
-  const int sl = mx_active_slot(ra, blockIdx.x / NT, sr);
+  const int sl = active_slot(ra, blockIdx.x / NT, sr);
   if (sl < 0) return;
   const int n0 = (blockIdx.x % NT) * 32, d = ra.d, nI = up128(ra.I) / 128;
   const int lane = lane_id(), r16 = lane & 15;
@@ -861,23 +770,13 @@ bool mx_large_tiles(const moe_layer_mx4* L, int T, int k, long active) {
   return r >= 1000 && active * (r / 256 + 0.5) * ((L->I + 127) / 128) >= 1024;
 }
 
-// BPC blocks per compute unit, a multiple of the XCDs, at most one per tile.
-template <class C> dim3 mx_grid(const RowArgs& ra, int NT) {
-  const long long R = (long long)ra.Tn * ra.k;
-  const long long tiles = (R / C::RA + (R < ra.S_r ? R : ra.S_r) +
-                           (long long)(ra.S - ra.S_r) * ((ra.Tn + C::RA - 1) / C::RA)) * NT;
-  const long long most = (long long)(device_cus() + N_XCD - 1) / N_XCD * N_XCD * C::BPC;
-  const long long g = (tiles + N_XCD - 1) / N_XCD * N_XCD;
-  return dim3((unsigned)(g < most ? g : most));
-}
-
 template <class C, class HALF> void mx_tiles(const MxArgs& a, const bf16* X, hipStream_t st) {
   const RowArgs& ra = a.ra;
   const int nb = act_blocks(ra.d);
   hipLaunchKernelGGL(k_mx_prep, dim3(cdiv((long)ra.Tn * nb, 16) + 1), dim3(256), 0, st, X, ra, C::RA, nb, a.w.xq, a.w.xs,
                      a.w.mbase);
-  hipLaunchKernelGGL((k_mx_tiles<C, HALF, false>), mx_grid<C>(ra, cdiv(ra.I, C::RB / 2)), dim3(64 * C::NW), 0, st, a);
-  hipLaunchKernelGGL((k_mx_tiles<C, HALF, true>), mx_grid<C>(ra, cdiv(ra.d, C::RB)), dim3(64 * C::NW), 0, st, a);
+  hipLaunchKernelGGL((k_mx_tiles<C, HALF, false>), tile_grid<C>(ra, cdiv(ra.I, C::RB / 2)), dim3(64 * C::NW), 0, st, a);
+  hipLaunchKernelGGL((k_mx_tiles<C, HALF, true>), tile_grid<C>(ra, cdiv(ra.d, C::RB)), dim3(64 * C::NW), 0, st, a);
 }
 
 int check_rows(const void* a, const char* an, const void* b, const char* bn, const void* c, const char* cn, long rows,

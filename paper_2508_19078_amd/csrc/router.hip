@@ -210,7 +210,7 @@ __device__ __forceinline__ void route_select(const float* part, int PSTRIDE, int
       sum += row_ror<4>(sum);
       sum += row_ror<2>(sum);
       sum += row_ror<1>(sum);
-      if (mine) {
+      if (mine && idx) {
         idx[(size_t)t * k + gl] = mye[u];
         gate[(size_t)t * k + gl] = g / sum;
       }
@@ -349,7 +349,7 @@ __device__ __forceinline__ void route_select_q(const float* stage, int PSTRIDE, 
 #pragma unroll
       for (int r = 0; r < RPL; ++r) {
         const int j = LPT * r + q;
-        if (j < k && on && t < T) {
+        if (j < k && on && t < T && idx) {
           idx[(size_t)t * k + j] = re[r];
           gate[(size_t)t * k + j] = g[r] / sum;
         }
@@ -1130,6 +1130,24 @@ extern "C" int moe_route_topk(const void* X, const void* Wr, int dtype, const fl
                                        idx, gate, logits, nullptr, st);
   return launch_route<float, float, 0>((const float*)X, (const float*)Wr, nullptr, bias, T, d, E, k,
                                        idx, gate, logits, nullptr, st);
+}
+
+extern "C" int moe_router_logits(const void* X, const void* Wr, int dtype, const float* bias, int T, int d, int E,
+                                 float* logits, void* stream) {
+  clear_error();
+  FM_TRY(check_route_shape(T, d, E, 1));
+  FM_TRY(need_dtype_float(dtype, "dtype"));
+  if (T == 0) return MOE_OK;
+  FM_TRY(need(X, "X")); FM_TRY(need(Wr, "Wr")); FM_TRY(need(logits, "logits"));
+  FM_TRY(need_aligned(X, "X")); FM_TRY(need_aligned(Wr, "Wr")); FM_TRY(need_aligned(bias, "bias"));
+  FM_TRY(need_aligned(logits, "logits"));
+  hipStream_t st = as_stream(stream);
+  // the routing kernels with one choice that is not written
+  if (dtype == MOE_BF16)
+    return launch_route<bf16, bf16, 0>((const bf16*)X, (const bf16*)Wr, nullptr, bias, T, d, E, 1, nullptr, nullptr, logits,
+                                       nullptr, st);
+  return launch_route<float, float, 0>((const float*)X, (const float*)Wr, nullptr, bias, T, d, E, 1, nullptr, nullptr,
+                                       logits, nullptr, st);
 }
 
 extern "C" int moe_quantize_int8(const void* W, int dtype, int E, int d, int8_t* Wq, float* scale,

@@ -6,10 +6,16 @@ stream.  It is plumbing: every value is computed by libfluxmoe.
 
   profile()  int8 router quantisation + activation histogram (once per round)
   merge()    merge plan, Eq. 2 merge and the slot tables (once per round)
-  route()    softmax top-k gate
+  route()    softmax top-k gate, or the routing from scores of a given gating
   forward()  permute -> grouped SwiGLU forward -> combine
   backward() combine backward -> grouped SwiGLU backward -> permute backward
   step()     all of the above in that order: one pass of the whole hot path
+
+With a gating (api.gating), also:
+
+  router_backward()  the router's gradients from the gates' (after backward(dgate=True))
+  balance()          the selection bias moved against the step's load
+  clip()             the global norm of the step's gradients, and their clipping (any routing)
 
 HBM layout.  Expert weights are stacked per matrix ([E, I, d], [E, I, d],
 [E, d, I]); merged groups get their own stacks and shared experts theirs.
@@ -54,8 +60,11 @@ def tuning_flags(w: LayerWorkload, K: int, G: int):
 
 class MoELayerRunner:
     def __init__(self, w: LayerWorkload, inputs: Optional[LayerInputs] = None, layer: int = 0,
-                 device: str = "cuda"):
+                 device: str = "cuda", gating: Optional[api.moe_gating] = None):
         self.w, self.layer, self.dev = w, layer, device
+        if gating is not None and (gating.E, gating.k) != (w.E, w.k):
+            raise ValueError(f"gating for {gating.E} experts, top-{gating.k}; the layer has {w.E}, top-{w.k}")
+        self.gating = gating
         inp = inputs if inputs is not None else LayerInputs(w, layer)
         dt = TORCH_DT[w.dtype]
         self.dt = dt
@@ -141,6 +150,12 @@ class MoELayerRunner:
         self.idx = zi(T, k)
         self.gate = z(T, k, dtype=torch.float32)
         self.logits = z(T, E, dtype=torch.float32)
+        if gating is not None:
+            self.sel_bias = torch.zeros(E, dtype=torch.float32, device=device)
+            self.load = zi(E)               # choices of the steps since the last balance()
+            self.dlogits = z(T, E, dtype=torch.float32)
+            self.dWr, self.dbias = z(E, d, dtype=torch.float32), z(E, dtype=torch.float32)
+            self.ws_router = torch.empty(api.moe_router_bwd_workspace_size(T, d, E), dtype=torch.uint8, device=device)
         R, Rt = T * k, T * (k + w.n_shared)
         self.offsets = zi(self.S_r + 1)
         self.perm_token = zi(R)
@@ -191,7 +206,11 @@ class MoELayerRunner:
                               merged, self.t_wg, self.t_wu, self.t_wd)
 
     def route(self):
-        api.moe_route_topk(self.X, self.Wr, self.bias, self.w.k, self.idx, self.gate, None)
+        if self.gating is None:
+            api.moe_route_topk(self.X, self.Wr, self.bias, self.w.k, self.idx, self.gate, None)
+            return
+        api.moe_router_logits(self.X, self.Wr, self.bias, self.logits)
+        api.moe_route_scored(self.gating, self.logits, self.idx, self.gate, sel_bias=self.sel_bias, counts=self.load)
 
     def forward(self, idx=None, gate=None):
         w = self.w
@@ -210,6 +229,29 @@ class MoELayerRunner:
         api.moe_grouped_swiglu_bwd(self.layer_tables, self.X, self.X_perm, self.offsets, w.T, w.k, self.A_g,
                                    self.A_u, self.H, self.dO, self.dX_perm, accumulate_dw, self.ws_bwd)
         api.moe_permute_bwd(self.layer_tables, self.dX_perm, self.inv, w.T, w.k, self.dX)
+
+    def router_backward(self):
+        """dWr, dbias, and the router's share added to dX; after backward(dgate=True)."""
+        api.moe_route_scored_bwd(self.gating, self.logits, self.idx, self.dgate, self.dlogits)
+        api.moe_router_bwd(self.dlogits, self.X, self.Wr, self.ws_router, dX=self.dX, dWr=self.dWr, dbias=self.dbias,
+                           accumulate_dx=True)
+
+    def balance(self, rate: float):
+        api.moe_route_bias_update(self.load, self.sel_bias, rate)
+        self.load.zero_()
+
+    def clip(self, max_norm: float, eps: float = 1e-6):
+        """Clips the weight gradients (the router's too, with a gating) in place by their
+        global norm, which is returned (a device tensor)."""
+        if not hasattr(self, "grads"):
+            router = () if self.gating is None else (self.dWr, self.dbias)
+            self.grads = api.TensorSet([*self.dWg, *self.dWu, *self.dWd, *router], torch.float32, self.dev)
+            self.sumsq = torch.empty(1, dtype=torch.float64, device=self.dev)
+            self.norm = torch.empty(1, dtype=torch.float32, device=self.dev)
+            self.ws_norm = torch.empty(api.moe_grad_norm_workspace_size(), dtype=torch.uint8, device=self.dev)
+        api.moe_grad_norm(self.grads, self.sumsq, self.norm, self.ws_norm)
+        api.moe_grad_clip(self.grads, self.sumsq, max_norm, eps=eps)
+        return self.norm
 
     def step(self):
         self.profile()
