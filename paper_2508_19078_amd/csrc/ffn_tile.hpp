@@ -41,7 +41,8 @@ void tile_fwd_q8(const moe_layer_q8* L, const void* X, const void* Xp, const int
 // the kernels for a few tokens.
 int mx4_tile(const moe_layer_mx4* L, int T, int k);
 
-// Rows of the 8-bit float forward's row tile: 128 (64 where few are left) or 256 (128).
+// Rows of the 8-bit float forward's row tile: 128 (64 where few are left) or 256 (128), or
+// 0: the kernels for a few tokens.
 int fp8_tile(const moe_layer_fp8* L, int T, int k);
 
 // One block per compute unit, rounded to the XCD count.

@@ -24,6 +24,7 @@
 // * X and H in the workspace have rows of whole 128-blocks, zero behind the row's end, so
 //   weight chunks past K (clamped reads) meet zero codes.
 #include <type_traits>
+#include <utility>
 
 #include "debug.hpp"
 #include "ffn_common.hpp"
@@ -189,11 +190,14 @@ struct F8Ptrs {
   const float* const* sd;
 };
 
+constexpr int F8_FEW = 8;   // most tokens of a call that takes the kernels for few
+
 // Workspace: row-tile prefix, X and H as rows of whole 128-blocks with their scales.
 struct F8Ws {
   int32_t* mbase;
   uint8_t *xq, *hq;
   float *xs, *hs;
+  float* hf;   // H of a call of few tokens, [rows][I]
 };
 inline F8Ws f8_ws_at(void* ws, const moe_layer_fp8* L, int T, int k, size_t* bytes) {
   const size_t S = L->S_routed + L->S_shared, R = (size_t)T * (k + L->S_shared);
@@ -210,6 +214,7 @@ inline F8Ws f8_ws_at(void* ws, const moe_layer_fp8* L, int T, int k, size_t* byt
   w.xs = (float*)take((size_t)T * scale_row(nd) * 4);
   w.hq = (uint8_t*)take(R * nI * 128);
   w.hs = (float*)take(R * scale_row(nI) * 4);
+  w.hf = (float*)take((size_t)(T < F8_FEW ? T : F8_FEW) * (k + L->S_shared) * L->I * 4);
   *bytes = (size_t)(p - (char*)ws);
   return w;
 }
@@ -259,6 +264,10 @@ struct F8Tile {
   int wrows;                    // weight rows (per matrix) from the tile on
   int nk, kw;                   // slabs; 16-byte chunks of a weight row
 };
+
+template <typename F, int... N> __device__ __forceinline__ void f8_steps(F f, std::integer_sequence<int, N...>) {
+  (f(std::integral_constant<int, N>{}), ...);
+}
 
 // acc += X W^T.  LDS: two slabs, then two groups of scales [RA rows][16 bytes].  The
 // barrier at the top of slab kt says that it has landed and that every wave has read slab
@@ -313,17 +322,10 @@ __device__ __forceinline__ void f8_gemm(const F8Tile& t, FM_LDS char* lds, f32x1
   };
   const int row0 = (wave & 1) * C::TM, col0 = (wave >> 1) * C::TN;
   const int m = lane & 31, h = lane >> 5;
-  uint32_t fa[C::MI], fb[C::NJ];
-#pragma unroll
-  for (int i = 0; i < C::MI; ++i) {
-    const int r = row0 + 32 * i + m;
-    fa[i] = r * 128 + ((h ^ f8_swz_a(r)) << 4);
-  }
-#pragma unroll
-  for (int j = 0; j < C::NJ; ++j) {
-    const int r = col0 + 32 * j + tile_column(m);
-    fb[j] = C::A_BYTES + r * 128 + ((h ^ f8_swz_b(r)) << 4);
-  }
+  // this lane's first chunk in a slab; its rows of the other 32-row blocks lie 4096 bytes
+  // on (32 rows leave the swizzles as they are), its other chunks at an exclusive or
+  const int ra = row0 + m, rb = col0 + tile_column(m);
+  const uint32_t fa = ra * 128 + ((h ^ f8_swz_a(ra)) << 4), fb = C::A_BYTES + rb * 128 + ((h ^ f8_swz_b(rb)) << 4);
   const uint32_t ga = (row0 + m) * 16;
 #pragma unroll
   for (int i = 0; i < C::MI; ++i)
@@ -347,34 +349,60 @@ __device__ __forceinline__ void f8_gemm(const F8Tile& t, FM_LDS char* lds, f32x1
     const int kn = min(kt + 1, nk - 1);
     w0 = ld_scalar(t.s[0] + kn);
     w1 = ld_scalar(t.s[1] + kn);
-    const FM_LDS char* const l = lds + (kt & 1) * C::SLAB;
+    const uint32_t slab = (uint32_t)(uintptr_t)lds + (kt & 1) * C::SLAB;
     const FM_LDS char* const s = sc + ((kt >> 2) & 1) * C::SCALES + ga + 4 * (kt & 3);
-    auto frag = [&](uint32_t at, int step) {   // 64 k: chunks 4 step + h and 4 step + 2 + h
-      int flip = step << 6;
-      asm volatile("" : "+s"(flip));   // not hoisted: the addresses would take the registers of the sums
-      const u32x4_t a = *(const FM_LDS u32x4_t*)(l + (at ^ flip));
-      const u32x4_t b = *(const FM_LDS u32x4_t*)(l + (at ^ (flip + 32)));
+    // 64 k of a row: chunks 4 step + h and 4 step + 2 + h
+    const uint32_t aa = slab + fa, ab = slab + fb;
+    auto chunk = [](uint32_t at, int c, int blk) { return *(const FM_LDS u32x4_t*)(uintptr_t)((at ^ (c << 5)) + 4096 * blk); };
+    auto frag = [&](uint32_t at, int step, int blk) {
+      const u32x4_t a = chunk(at, 2 * step, blk), b = chunk(at, 2 * step + 1, blk);
       return i32x8_t{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
     };
-    i32x8_t xb[2][C::NJ];
+    i32x8_t xb[2][C::NJ], xa[2][2];   // [step][block], [block's parity][step]
+    float sx[2];
+    auto read_a = [&](int i) {
+      xa[i & 1][0] = frag(aa, 0, i);
+      xa[i & 1][1] = frag(aa, 1, i);
+      sx[i & 1] = *(const FM_LDS float*)(s + 512 * i);
+    };
+    // LDS answers in order: what the first products take is asked for first
+    xb[0][0] = frag(ab, 0, 0);
+    xa[0][0] = frag(aa, 0, 0);
+    sched_fence();
+    xb[1][0] = frag(ab, 1, 0);
+    xa[0][1] = frag(aa, 1, 0);
+    sx[0] = *(const FM_LDS float*)s;
+    sched_fence();
+    // a tile's two products, and between them the sums of the tile before it, which the
+    // matrix unit has finished by then
+    constexpr int N = C::MI * C::NJ;
+    f32x16_t p[2];
+    float f[2];
+    auto add = [&](auto n_, auto half_) {
+      constexpr int n = decltype(n_)::value, half = decltype(half_)::value;
+      if constexpr (n >= 0) {
 #pragma unroll
-    for (int st = 0; st < 2; ++st)
-#pragma unroll
-      for (int j = 0; j < C::NJ; ++j) xb[st][j] = frag(fb[j], st);
-    const f32x16_t zero = {};
-#pragma unroll
-    for (int i = 0; i < C::MI; ++i) {
-      const i32x8_t x0 = frag(fa[i], 0), x1 = frag(fa[i], 1);
-      const float sx = *(const FM_LDS float*)(s + 512 * i);
-#pragma unroll
-      for (int j = 0; j < C::NJ; ++j) {
-        f32x16_t p = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xb[0][j], x0, zero, 0, 0, 0, 0, 0, 0);
-        p = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xb[1][j], x1, p, 0, 0, 0, 0, 0, 0);
-        const float f = sx * sw[j];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][j][e] = fmaf(p[e], f, acc[i][j][e]);
+        for (int e = 8 * half; e < 8 * half + 8; ++e)
+          acc[n / C::NJ][n % C::NJ][e] = fmaf(p[n & 1][e], f[n & 1], acc[n / C::NJ][n % C::NJ][e]);
       }
-    }
+    };
+    auto step = [&](auto n_) {
+      constexpr int n = decltype(n_)::value, i = n / C::NJ, j = n % C::NJ;
+      const f32x16_t zero = {};
+      if constexpr (n < N) p[n & 1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xb[0][j], xa[i & 1][0], zero, 0, 0, 0, 0, 0, 0);
+      sched_fence();
+      if constexpr (n == 0) xb[0][1] = frag(ab, 0, 1);
+      if constexpr (n == 0) xb[1][1] = frag(ab, 1, 1);
+      if constexpr (j == 0 && i + 1 < C::MI) read_a(i + 1);
+      add(std::integral_constant<int, n - 1>{}, std::integral_constant<int, 0>{});
+      sched_fence();
+      if constexpr (n < N) p[n & 1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xb[1][j], xa[i & 1][1], p[n & 1], 0, 0, 0, 0, 0, 0);
+      sched_fence();
+      add(std::integral_constant<int, n - 1>{}, std::integral_constant<int, 1>{});
+      if constexpr (n < N) f[n & 1] = sx[i & 1] * sw[j];
+      sched_fence();
+    };
+    f8_steps(step, std::make_integer_sequence<int, N + 1>{});
   }
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
@@ -515,6 +543,185 @@ typedef F8Cfg<256> E256;
 typedef F8Cfg<128> E128;
 typedef F8Cfg<64> E64;
 
+// --------------------------------------------------------- a few tokens ----
+// Calls of a few tokens are bound by latency and by the weights' bytes, which have to be
+// spread over all compute units: a block takes 8 columns of H (8 gate and 8 up rows, one
+// fragment of v_mfma_f32_16x16x128_f8f6f4: lane l row l % 16, 32 k from l / 16 on), or 32 of
+// O, of one slot, and its NW waves split the slabs of 128 k into consecutive parts whose
+// sums meet in LDS.  A wave requests BS slabs of weights straight into registers, and the
+// block quantises its activation rows into LDS while they are on their way.  H goes
+// through the workspace in fp32 and is quantised the same way.  Rows come 16 at a time.
+// Blocks exist for the slots that may hold rows only.
+
+// Rows of nb 128-blocks in LDS: codes, then scales; padded so that 16 rows' chunks at one
+// place lie on different banks.
+struct F8FewRows {
+  FM_LDS char* codes;
+  FM_LDS float* scale;
+  int ld, lds;
+};
+__host__ __device__ constexpr int f8_few_row_bytes(int nb) { return nb * 128 + 16 + (nb | 1) * 4; }
+__device__ __forceinline__ F8FewRows f8_few_rows(FM_LDS char* at, int nb, int rows) {
+  return F8FewRows{at, (FM_LDS float*)(at + rows * (nb * 128 + 16)), nb * 128 + 16, nb | 1};
+}
+
+// The block's n rows (row(r): pointer) of cols columns, quantised into LDS.
+template <int THREADS, typename Row>
+__device__ __forceinline__ void f8_few_stage(const F8FewRows& l, int n, int nb, int cols, Row row) {
+  for (int item = threadIdx.x / 16; item < n * nb; item += THREADS / 16) {
+    const int r = item / nb, blk = item - r * nb, q = threadIdx.x % 16;
+    float v[8], s;
+    load8(row(r), blk * 128 + q * 8, cols, v);
+    *(FM_LDS u32x2_t*)(l.codes + r * l.ld + blk * 128 + q * 8) = quantize128(v, s);
+    if (q == 0) l.scale[r * l.lds + blk] = s;
+  }
+}
+
+// Sums over this wave's slabs [k0, k1): NF fragments of 16 weight rows (codes at w[f], of
+// this lane's row; scale(f, k): the scale of the rows this lane has sums of) by the 16
+// activation rows that stage() puts into LDS (n of them are there).
+template <int NF, int BS, typename Scale, typename Stage>
+__device__ __forceinline__ void f8_few_sums(const uint8_t* const (&w)[NF], int kw, Scale scale, const F8FewRows& l, int n, int k0,
+                                            int k1, Stage stage, f32x4_t (&acc)[NF]) {
+  const int kb = lane_id() >> 4, r = min(lane_id() & 15, n - 1);
+  u32x4_t wc[BS][NF][2];
+  float ws[BS][NF];
+  auto load = [&](int k) {
+#pragma unroll
+    for (int u = 0; u < BS; ++u) {
+      if (k + u >= k1) break;
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
+        // (chunks behind the row's end meet activations that are 0)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) wc[u][f][c] = ld16(w[f] + 16 * min(8 * (k + u) + 2 * kb + c, kw - 1));
+        ws[u][f] = scale(f, k + u);
+      }
+    }
+  };
+  load(k0);
+  stage();
+  __syncthreads();
+  for (int k = k0; k < k1; k += BS) {
+    if (k > k0) load(k);
+#pragma unroll
+    for (int u = 0; u < BS; ++u) {
+      if (k + u >= k1) break;
+      const FM_LDS char* const at = l.codes + r * l.ld + (k + u) * 128 + kb * 32;
+      const u32x4_t x0 = *(const FM_LDS u32x4_t*)at, x1 = *(const FM_LDS u32x4_t*)(at + 16);
+      const float sx = l.scale[r * l.lds + k + u];
+      auto both = [](const u32x4_t& a, const u32x4_t& b) {
+        return i32x8_t{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+      };
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
+        const f32x4_t p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(both(wc[u][f][0], wc[u][f][1]), both(x0, x1),
+                                                                           f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+        const float s = sx * ws[u][f];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[f][e] = fmaf(p[e], s, acc[f][e]);
+      }
+    }
+  }
+}
+
+// The waves' sums through LDS: [wave][f][lane] quads; element (row, weight row n) of
+// fragment f is in quad lane 16 (n / 4) + row, component n % 4.
+template <int NF, int NW> __device__ __forceinline__ float f8_few_sum(const FM_LDS f32x4_t* red, int f, int row, int n) {
+  const FM_LDS float* const p = (const FM_LDS float*)(red + f * 64 + 16 * (n >> 2) + row) + (n & 3);
+  float v = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) v += p[w * NF * 256];
+  return v;
+}
+
+// This wave's part of n slabs.
+template <int NW> __device__ __forceinline__ void f8_few_part(int n, int& k0, int& k1) {
+  const int per = (n + NW - 1) / NW, w = wave_id();
+  k0 = min(w * per, n);
+  k1 = min(k0 + per, n);
+}
+
+extern __shared__ __align__(16) char f8_few_lds[];
+
+template <int NW, int BS>
+__global__ __launch_bounds__(64 * NW) void k_f8_few_gate_up(F8Args a, const bf16* __restrict__ X, int NT, int max_rows) {
+  FM_LDS f32x4_t* const red = (FM_LDS f32x4_t*)f8_few_lds;
+  const RowArgs& ra = a.ra;
+  SlotRows sr;
+  const int sl = active_slot(ra, blockIdx.x / NT, sr);
+  if (sl < 0) return;
+  const int n0 = (blockIdx.x % NT) * 8, I = ra.I, nd = blocks128(ra.d);
+  const int lane = lane_id(), r16 = lane & 15;
+  const F8FewRows l = f8_few_rows((FM_LDS char*)f8_few_lds + NW * 1024, nd, max_rows);
+  // weight rows: 8 of gate, 8 of up (I % 8 == 0); lanes 0 to 31 have sums of the gate's
+  const uint8_t* const w[1] = {(r16 < 8 ? ld_scalar(a.W.qg + sl) : ld_scalar(a.W.qu + sl)) + (size_t)(n0 + (r16 & 7)) * ra.d};
+  const float* const s = (lane < 32 ? ld_scalar(a.W.sg + sl) : ld_scalar(a.W.su + sl)) + (size_t)(n0 / 128) * nd;
+  int k0, k1;
+  f8_few_part<NW>(nd, k0, k1);
+  for (int m0 = 0; m0 < sr.nrows; m0 += max_rows) {
+    const int n = min(max_rows, sr.nrows - m0);
+    f32x4_t acc[1] = {{0.f, 0.f, 0.f, 0.f}};
+    f8_few_sums<1, BS>(w, ra.d / 16, [&](int, int k) { return gptr(s)[k]; }, l, n, k0, k1, [&] {
+      f8_few_stage<64 * NW>(l, n, nd, ra.d, [&](int r) {
+        const size_t tok = sr.shared ? m0 + r : min(max(gptr(a.perm_token)[sr.xrow0 + m0 + r], 0), ra.Tn - 1);
+        return X + tok * ra.d;
+      });
+    }, acc);
+    red[wave_id() * 64 + lane] = acc[0];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 8 * n; i += 64 * NW) {
+      const int row = i >> 3, c = i & 7;
+      const float g = f8_few_sum<1, NW>(red, 0, row, c), u = f8_few_sum<1, NW>(red, 0, row, 8 + c);
+      gptr(a.w.hf)[(size_t)(sr.orow0 + m0 + row) * I + n0 + c] = g * sigm_fast(g) * u;
+    }
+    __syncthreads();   // red and the rows are read
+  }
+}
+
+template <int NW, int BS>
+__global__ __launch_bounds__(64 * NW) void k_f8_few_down(F8Args a, int NT, int max_rows) {
+  FM_LDS f32x4_t* const red = (FM_LDS f32x4_t*)f8_few_lds;
+  const RowArgs& ra = a.ra;
+  SlotRows sr;
+  const int sl = active_slot(ra, blockIdx.x / NT, sr);
+  if (sl < 0) return;
+  const int n0 = (blockIdx.x % NT) * 32, d = ra.d, nI = blocks128(ra.I);
+  const int lane = lane_id(), r16 = lane & 15;
+  const F8FewRows l = f8_few_rows((FM_LDS char*)f8_few_lds + NW * 2048, nI, max_rows);
+  const uint8_t* w[2];
+#pragma unroll
+  for (int f = 0; f < 2; ++f) w[f] = ld_scalar(a.W.qd + sl) + (size_t)min(n0 + 16 * f + r16, d - 1) * ra.I;
+  const float* const s = ld_scalar(a.W.sd + sl) + (size_t)(n0 / 128) * nI;   // 32 columns lie in one block
+  int k0, k1;
+  f8_few_part<NW>(nI, k0, k1);
+  for (int m0 = 0; m0 < sr.nrows; m0 += max_rows) {
+    const int n = min(max_rows, sr.nrows - m0);
+    const size_t row0 = (size_t)(sr.orow0 + m0);
+    f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    f8_few_sums<2, BS>(w, ra.I / 16, [&](int, int k) { return gptr(s)[k]; }, l, n, k0, k1, [&] {
+      f8_few_stage<64 * NW>(l, n, nI, ra.I, [&](int r) { return (const float*)a.w.hf + (row0 + r) * ra.I; });
+    }, acc);
+#pragma unroll
+    for (int f = 0; f < 2; ++f) red[(wave_id() * 2 + f) * 64 + lane] = acc[f];
+    __syncthreads();
+    // 16 lanes per row, two columns each
+    for (int r = threadIdx.x >> 4; r < n; r += 4 * NW) {
+      const int c = (threadIdx.x & 15) * 2;
+      if (n0 + c >= d) break;
+      const float v0 = f8_few_sum<2, NW>(red, c >> 4, r, c & 15), v1 = f8_few_sum<2, NW>(red, c >> 4, r, (c & 15) + 1);
+      *(FM_GLOBAL uint32_t*)((uint16_t*)a.O + (row0 + r) * d + n0 + c) = pk_bf16(v0, v1);
+    }
+    __syncthreads();   // red and the rows are read
+  }
+}
+
+// Whether a call takes the kernels for a few tokens: a block's rows have to fit the LDS.
+bool f8_few_tokens(const moe_layer_fp8* L, int T, long active) {
+  return T <= F8_FEW && active * (L->I / 8) <= 2048 && T * f8_few_row_bytes(blocks128(L->d)) <= 56 * 1024 &&
+         T * f8_few_row_bytes(blocks128(L->I)) <= 52 * 1024;
+}
+
 template <class C, class HALF> void f8_tiles(const F8Args& a, const bf16* X, hipStream_t st) {
   const RowArgs& ra = a.ra;
   const int nb = blocks128(ra.d);
@@ -543,7 +750,9 @@ long f8_active(const moe_layer_fp8* L, int T, int k) {
 }  // namespace
 
 int fp8_tile(const moe_layer_fp8* L, int T, int k) {
-  const double r = (double)T * (k + L->S_shared) / f8_active(L, T, k);
+  const long active = f8_active(L, T, k);
+  if (f8_few_tokens(L, T, active)) return 0;
+  const double r = (double)T * (k + L->S_shared) / active;
   return r >= 192 ? 256 : 128;
 }
 
@@ -654,7 +863,17 @@ extern "C" int moe_grouped_swiglu_fwd_fp8(const moe_layer_fp8* L, const void* X,
   }
   const RowArgs ra{offsets, w.mbase, L->S_routed, L->S_routed + L->S_shared, T, k, L->d, L->I, L->I};
   const F8Args a{{L->q_gate, L->q_up, L->q_down, L->s_gate, L->s_up, L->s_down}, w, perm_token, ra, (bf16*)O};
-  if (fp8_tile(L, T, k) == 256) f8_tiles<E256, E128>(a, (const bf16*)X, st);
+  const int tile = fp8_tile(L, T, k);
+  if (tile == 0) {
+    const long active = f8_active(L, T, k);
+    const int ng = L->I / 8, nd = cdiv(L->d, 32);
+    hipLaunchKernelGGL((k_f8_few_gate_up<4, 8>), dim3(active * ng), dim3(256), T * f8_few_row_bytes(blocks128(L->d)) + 4 * 1024,
+                       st, a, (const bf16*)X, ng, T);
+    hipLaunchKernelGGL((k_f8_few_down<4, 3>), dim3(active * nd), dim3(256), T * f8_few_row_bytes(blocks128(L->I)) + 4 * 2048, st,
+                       a, nd, T);
+    return check_launch("moe_grouped_swiglu_fwd_fp8");
+  }
+  if (tile == 256) f8_tiles<E256, E128>(a, (const bf16*)X, st);
   else f8_tiles<E128, E64>(a, (const bf16*)X, st);
   return check_launch("moe_grouped_swiglu_fwd_fp8");
 }
