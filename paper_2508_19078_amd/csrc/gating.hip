@@ -3,14 +3,19 @@
 // top-k, and the gradient of the logits.
 //
 // 16 lanes per token, four tokens per wave: lane q holds experts 64 c + 4 q to + 3 for
-// chunks c, as they lie in memory.  A selection round is a maximum over the lane's keys
-// and four row rotations over the lanes; rank j ends in lane j.
+// chunks c, as they lie in memory.
 //
-// The selection is that of keys in fp64, but fp64 is seldom needed.  Without sel_bias
-// the logits themselves order the experts, exactly.  With it, keys in fp32 decide where
-// neighbours in rank order (the first one left out among them), and the worst group kept
-// and the best one not, lie further apart than twice the keys' error; a wave with a token
-// where they do not selects again from keys in fp64.
+// The selection is that of keys in fp64 (or of the logits, exactly), but it is made on 32
+// bits: a key's distance from the bottom of a window below the largest, in 24 bits, then
+// 255 - expert, so that one unsigned maximum finds a round's winner and its index, and the
+// next round's is the largest of the differences to it that wrap.  The map to 24 bits does
+// not decrease, so where neighbours in rank order (the first one left out among them)
+// differ by more than the fp32 keys' error, and the worst group kept and the best one not
+// do, the selection is the exact one.  Elsewhere fp64 decides, on as few keys as it takes (a
+// kernel of 32768 tokens always meets some such, and waits for its slowest wave): the
+// largest keys of groups that are near the border; the 16 first in rank order, a lane each,
+// if the last of them is clearly behind the k-th; all keys where that does not hold or the
+// largest is no number.
 #include "common.hpp"
 #include "ffn_common.hpp"
 
@@ -22,7 +27,9 @@ constexpr int GT_MAXK = 16, GT_MAXG = 32;
 constexpr int NOBODY = 0x7FFFFFFF;
 
 struct Gating {
-  int E, k, n_group, topk_group, group_top, size;   // size: experts of a group
+  int E, k, n_group, topk_group, group_top;
+  int size;    // experts of a group
+  int lanes;   // lanes of a chunk that hold a group of 4, 8, .. 64 experts, or 0
   bool sigmoid, renorm;
   float scale;
 };
@@ -65,215 +72,460 @@ template <typename K> __device__ __forceinline__ K softmax_part(K z, K m) {
   return m == inf ? (K)(z == inf) : z == -inf ? (K)0 : e_to(z - m);
 }
 
-// Scores of this lane's experts (0 for places behind E, whose z is -inf).
-template <typename K, int N> __device__ __forceinline__ void scores(const Gating& g, const float (&z)[N], K (&s)[N]) {
+__device__ __forceinline__ uint32_t larger3(uint32_t a, uint32_t b, uint32_t c) { return max(max(a, b), c); }
+__device__ __forceinline__ uint32_t row_max_u(uint32_t x) {
+  x = max(x, (uint32_t)ror<8>((int)x));
+  x = max(x, (uint32_t)ror<4>((int)x));
+  x = max(x, (uint32_t)ror<2>((int)x));
+  return max(x, (uint32_t)ror<1>((int)x));
+}
+
+// Expert of place i of lane q.
+__device__ __forceinline__ int expert_at(int i, int q) { return 64 * (i / 4) + 4 * q + i % 4; }
+
+// The rows' logits, NaN as -inf, -inf behind E.
+template <int N> __device__ __forceinline__ void load_logits(const float* zr, int E, int q, float (&z)[N]) {
+  const float none = minus_inf<float>();
+  if ((E & 3) == 0) {   // rows of whole 16-byte chunks
+#pragma unroll
+    for (int c = 0; c < N / 4; ++c) {
+      u32x4_t v = {0, 0, 0, 0};
+      const int e = expert_at(4 * c, q);
+      if (e < E) v = ld16(zr + e);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) z[4 * c + b] = e < E ? __builtin_fmaxf(__uint_as_float(v[b]), none) : none;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int e = expert_at(i, q);
+      z[i] = e < E ? __builtin_fmaxf(gptr(zr)[e], none) : none;
+    }
+  }
+}
+
+// Scores with the hardware's exponential and reciprocal, for deciding a selection and a
+// softmax's denominator.  Steps of 2^-24 of a score (below 1): sigmoid 4 (the exponent's
+// rounding weighs |z| s (1 - s) < 1/4, exponential and reciprocal 2 each), softmax 3 and
+// its sum's 20, common to a row.  total: a softmax's sum; m its largest logit.
+template <int N> __device__ __forceinline__ void fast_scores(const Gating& g, const float (&z)[N], float (&s)[N], float& m, float& total) {
+  constexpr float L2E = 1.4426950408889634f;
   if (g.sigmoid) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) s[i] = logistic<K>((K)z[i]);
+    for (int i = 0; i < N; ++i) s[i] = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-L2E * z[i]));
     return;
   }
-  float m = z[0];
+  m = z[0];
 #pragma unroll
   for (int i = 1; i < N; ++i) m = larger(m, z[i]);
   m = row_max(m);
-  K sum = 0;
+  float sum = 0.f;
+  if (__any(!(fabsf(m) < __builtin_inff()))) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) sum += s[i] = softmax_part<K>((K)z[i], (K)m);
-  sum = row_sum(sum);
+    for (int i = 0; i < N; ++i) sum += s[i] = softmax_part(z[i], m);
+  } else {
 #pragma unroll
-  for (int i = 0; i < N; ++i) s[i] = sum > 0 ? s[i] / sum : (K)0;
+    for (int i = 0; i < N; ++i) sum += s[i] = __builtin_amdgcn_exp2f((z[i] - m) * L2E);
+  }
+  total = row_sum(sum);
+  const float inv = total > 0.f ? 1.f / total : 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) s[i] *= inv;
 }
 
-// What a selection leaves in lane j of a row: the choice of rank j.
-struct Choice {
-  int e;
-  bool sure;   // false: fp32 keys did not decide
-};
+// The two largest of two lanes' (h, l), h >= l, by a DPP control.
+template <int CTRL> __device__ __forceinline__ void merge_two(float& h, float& l) {
+  const float h2 = dpp_f<CTRL>(h), l2 = dpp_f<CTRL>(l);
+  l = larger(larger(fminf(h, h2), l), l2);
+  h = larger(h, h2);
+}
 
-// Selection for a row's token.  key: the experts' keys; of: what the groups rank by;
-// gap: neighbours in rank order must differ by more to be sure (0: keys are exact).
-template <typename K, int N>
-__device__ __forceinline__ Choice select(const Gating& g, const K (&key)[N], const K (&of)[N], K gap, K group_gap, K* row) {
-  const int lane = lane_id(), q = lane & 15;
-  bool sure = true;
-  uint32_t left = 0;   // this lane's experts that may still be chosen
-  uint32_t kept = ~0u;
-  if (g.n_group > 1) {
+// Which of this lane's chunks lie in a group that stays (bits), from the groups' keys.
+// Groups of 4, 8, .. 64 experts are lanes of one chunk; of others the ranks are read from
+// LDS key by key and bits has one per expert.  near: where the worst group kept and the
+// best one not are not further apart than gap (0: keys are exact, ties as defined), the
+// experts that decide between them, which are those not key_gap below what their group
+// ranks by.
+template <int N>
+__device__ __forceinline__ uint32_t groups_kept(const Gating& g, const float (&of)[N], float gap, float key_gap, float* row,
+                                                uint32_t& near) {
+  const int q = lane_id() & 15;
+  const float none = minus_inf<float>();
+  float worst = -none, best = none;   // of the groups kept, of the others
+  uint32_t left = 0;
+  if (g.lanes > 0) {
+    float r[N / 4], last[N / 4];   // ranks, and the least key in them
+    const int mine = q / g.lanes, per = 16 / g.lanes;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int e = 64 * (i / 4) + 4 * q + i % 4;
-      if (e < g.E) row[e] = of[i];
+    for (int c = 0; c < N / 4; ++c) {
+      const float a = of[4 * c], b = of[4 * c + 1], x = of[4 * c + 2], y = of[4 * c + 3];
+      const float h1 = larger(a, b), l1 = fminf(a, b), h2 = larger(x, y), l2 = fminf(x, y);
+      float h = larger(h1, h2), l = larger(larger(fminf(h1, h2), l1), l2);
+      if (g.lanes > 1) merge_two<0xB1>(h, l);     // quad_perm [1, 0, 3, 2]
+      if (g.lanes > 2) merge_two<0x4E>(h, l);     // quad_perm [2, 3, 0, 1]
+      if (g.lanes > 4) merge_two<0x141>(h, l);    // row_half_mirror
+      if (g.lanes > 8) merge_two<0x140>(h, l);    // row_mirror
+      r[c] = g.group_top == 2 ? __builtin_fmaxf(h + l, none) : h;
+      last[c] = g.group_top == 2 ? l : h;
+      const int grp = c * per + mine;
+      if (q % g.lanes == 0 && grp < g.n_group) row[grp] = r[c];
     }
     wave_lds_fence();
-    // lane q ranks groups q and q + 16, reading their experts from different places
-    K r[2];
+    int ahead[N / 4];
+#pragma unroll
+    for (int c = 0; c < N / 4; ++c) ahead[c] = 0;
+    for (int o = 0; o < g.n_group; ++o) {
+      const float v = row[o];
+#pragma unroll
+      for (int c = 0; c < N / 4; ++c) ahead[c] += v > r[c] || (v == r[c] && o < c * per + mine);
+    }
+#pragma unroll
+    for (int c = 0; c < N / 4; ++c) {
+      if (c * per + mine >= g.n_group) continue;
+      if (ahead[c] < g.topk_group) {
+        left |= 15u << (4 * c);
+        worst = fminf(worst, r[c]);
+      } else {
+        best = larger(best, r[c]);
+      }
+    }
+    worst = -row_max(-worst);
+    best = row_max(best);
+    if (gap > 0.f && !(worst - best > gap))
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (r[i / 4] >= worst - gap && r[i / 4] <= best + gap && !(of[i] < last[i / 4] - key_gap)) near |= 1u << i;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (expert_at(i, q) < g.E) row[expert_at(i, q)] = of[i];
+    wave_lds_fence();
+    // lane q ranks groups q and q + 16
+    float r[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int grp = q + 16 * h;
-      K a = minus_inf<K>(), b = minus_inf<K>();
-      if (grp < g.n_group) {
-        int at = q % g.size;
+      float a = none, b = none;
+      if (q + 16 * h < g.n_group)
         for (int i = 0; i < g.size; ++i) {
-          const K v = row[grp * g.size + at];
-          b = larger(b, v < a ? v : a);
+          const float v = row[(q + 16 * h) * g.size + i];
+          b = larger(b, fminf(v, a));
           a = larger(a, v);
-          if (++at == g.size) at = 0;
         }
-      }
-      r[h] = g.group_top == 2 ? number(a + b) : a;
+      r[h] = g.group_top == 2 ? __builtin_fmaxf(a + b, none) : a;
     }
     wave_lds_fence();
 #pragma unroll
     for (int h = 0; h < 2; ++h)
       if (q + 16 * h < g.n_group) row[q + 16 * h] = r[h];
     wave_lds_fence();
-    K worst = -minus_inf<K>(), best = minus_inf<K>();   // of the groups kept, of the others
-    uint32_t bits = 0;
+    uint32_t in = 0;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int grp = q + 16 * h;
       int ahead = 0;
       for (int o = 0; o < g.n_group; ++o) ahead += before(row[o], o, r[h], grp);
-      const bool in = grp < g.n_group && ahead < g.topk_group;
-      if (in) {
-        bits |= 1u << grp;
-        worst = r[h] < worst ? r[h] : worst;
-      } else if (grp < g.n_group) {
+      if (grp >= g.n_group) continue;
+      if (ahead < g.topk_group) {
+        in |= 1u << grp;
+        worst = fminf(worst, r[h]);
+      } else {
         best = larger(best, r[h]);
       }
     }
-    kept = (uint32_t)row_fold((int)bits, [](int a, int b) { return a | b; });
+    in = (uint32_t)row_fold((int)in, [](int a, int b) { return a | b; });
+#pragma unroll
+    for (int i = 0; i < N; ++i) left |= (in >> (min(expert_at(i, q), g.E - 1) / g.size) & 1u) << i;
     worst = -row_max(-worst);
     best = row_max(best);
-    if (group_gap > 0 && g.topk_group < g.n_group && !(worst - best > group_gap)) sure = false;
-    wave_lds_fence();
+    if (gap > 0.f && !(worst - best > gap)) near = ~0u;
   }
+  wave_lds_fence();
+  return left;
+}
+
+// A row of keys in LDS: 16 N of experts, then 32 for the groups' ranks.
+template <int N> constexpr int key_row = 16 * N + GT_MAXG;
+
+// Scores of a row in fp64 (loops that are not unrolled: this code is there in case).
+struct ExactScores {
+  const float* zr;
+  bool sigmoid;
+  double m, sum;
+  __device__ __forceinline__ ExactScores(const Gating& g, const float* zr_, int places) : zr(zr_), sigmoid(g.sigmoid) {
+    m = minus_inf<double>(), sum = 0;
+    if (sigmoid) return;
+    const int q = lane_id() & 15;
+#pragma nounroll
+    for (int i = 0; i < places; ++i)
+      if (expert_at(i, q) < g.E) m = larger(m, logit(expert_at(i, q)));
+    m = row_max(m);
+#pragma nounroll
+    for (int i = 0; i < places; ++i)
+      if (expert_at(i, q) < g.E) sum += softmax_part(logit(expert_at(i, q)), m);
+    sum = row_sum(sum);
+  }
+  __device__ __forceinline__ double logit(int e) const { return number(gptr(zr)[e]); }
+  __device__ __forceinline__ double of(int e) const {
+    return sigmoid ? logistic<double>(logit(e)) : sum > 0 ? softmax_part(logit(e), m) / sum : 0.0;
+  }
+};
+
+// The groups that stay (bits), by ranks of the keys in a row of LDS.
+__device__ __forceinline__ uint32_t groups_exact(const Gating& g, const double* row, double* ranks) {
+  const int q = lane_id() & 15;
+  double r[2];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int e = 64 * (i / 4) + 4 * q + i % 4;
+  for (int h = 0; h < 2; ++h) {
+    double a = minus_inf<double>(), b = a;
+    if (q + 16 * h < g.n_group)
+#pragma unroll 4
+      for (int i = 0; i < g.size; ++i) {
+        const double v = row[(q + 16 * h) * g.size + i];
+        b = larger(b, v < a ? v : a);
+        a = larger(a, v);
+      }
+    r[h] = g.group_top == 2 ? number(a + b) : a;
+    if (q + 16 * h < g.n_group) ranks[q + 16 * h] = r[h];
+  }
+  wave_lds_fence();
+  uint32_t kept = 0;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    int ahead = 0;
+#pragma unroll 4
+    for (int o = 0; o < g.n_group; ++o) ahead += before(ranks[o], o, r[h], q + 16 * h);
+    if (q + 16 * h < g.n_group && ahead < g.topk_group) kept |= 1u << (q + 16 * h);
+  }
+  wave_lds_fence();
+  return (uint32_t)row_fold((int)kept, [](int a, int b) { return a | b; });
+}
+
+// This lane's experts in the groups of `kept`.
+__device__ __forceinline__ uint32_t in_groups(const Gating& g, uint32_t kept, int places) {
+  const int q = lane_id() & 15;
+  uint32_t left = 0;
+#pragma nounroll
+  for (int i = 0; i < places; ++i) {
+    const int e = expert_at(i, q);
     if (e < g.E && (g.n_group == 1 || (kept >> (e / g.size) & 1))) left |= 1u << i;
   }
-  int mine = 0;
-  K last = 0;
-  const int rounds = gap > 0 ? g.k + 1 : g.k;   // one more shows how far the first left out is
-  for (int j = 0; j < rounds; ++j) {
-    K v = minus_inf<K>();
-    int e = NOBODY;
+  return left;
+}
+
+// groups_kept's bits, one per expert, with fp64 keys of the experts in near.
+template <bool BIAS, int N>
+__device__ __forceinline__ uint32_t near_groups(const Gating& g, const float (&of)[N], const float* zr, const float* sel_bias,
+                                                uint32_t near, double* row) {
+  const int q = lane_id() & 15;
 #pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (expert_at(i, q) < g.E) row[expert_at(i, q)] = of[i];
+  const ExactScores s(g, zr, N);
+#pragma nounroll
+  for (int i = 0; i < N; ++i) {
+    const int e = expert_at(i, q);
+    const bool mine = (near >> i & 1) && e < g.E;
+    if (!__any(mine)) continue;
+    if (mine) row[e] = BIAS ? number(s.of(e) + (double)gptr(sel_bias)[e]) : s.of(e);
+  }
+  wave_lds_fence();
+  return in_groups(g, groups_exact(g, row, row + 16 * N), N);
+}
+
+// The selection from keys in fp64 (BIAS) or the logits, group ranks in fp64, of a wave's
+// four tokens.  Returns the choice of rank q.
+template <bool BIAS, int N>
+__device__ __forceinline__ int select_exact(const Gating& g, const float* zr, const float* sel_bias, double* row) {
+  const int q = lane_id() & 15;
+  const bool ranks = g.n_group > 1 && g.group_top == 2;
+  auto put = [&](auto key) {
+#pragma nounroll
+    for (int i = 0; i < N; ++i)
+      if (expert_at(i, q) < g.E) row[expert_at(i, q)] = key(expert_at(i, q));
+    wave_lds_fence();
+  };
+  const ExactScores s(g, zr, BIAS || ranks ? N : 0);
+  uint32_t kept = ~0u;
+  if (BIAS) put([&](int e) { return number(s.of(e) + (double)gptr(sel_bias)[e]); });
+  else if (ranks) put([&](int e) { return s.of(e); });
+  else put([&](int e) { return s.logit(e); });
+  if (g.n_group > 1) kept = groups_exact(g, row, row + 16 * N);
+  if (!BIAS && ranks) put([&](int e) { return s.logit(e); });
+  uint32_t left = in_groups(g, kept, N);
+  int mine = 0;
+#pragma nounroll
+  for (int j = 0; j < g.k; ++j) {
+    double v = minus_inf<double>();
+    int e = NOBODY;
+#pragma unroll 2
     for (int i = 0; i < N; ++i) {
-      const int ei = 64 * (i / 4) + 4 * q + i % 4;
-      if ((left >> i & 1) && before(key[i], ei, v, e)) v = key[i], e = ei;
+      const int ei = expert_at(i, q);
+      const double vi = row[min(ei, g.E - 1)];
+      if ((left >> i & 1) && before(vi, ei, v, e)) v = vi, e = ei;
     }
-    auto step = [&](K v2, int e2) {
+    auto step = [&](double v2, int e2) {
       if (before(v2, e2, v, e)) v = v2, e = e2;
     };
     step(ror<8>(v), ror<8>(e));
     step(ror<4>(v), ror<4>(e));
     step(ror<2>(v), ror<2>(e));
     step(ror<1>(v), ror<1>(e));
-    if (e != NOBODY) {
-      if (j > 0 && gap > 0 && !(last - v > gap)) sure = false;
-      if (q == (e >> 2 & 15)) left &= ~(1u << (4 * (e >> 6) + (e & 3)));
-    }
-    last = v;
+    if (q == (e >> 2 & 15)) left &= ~(1u << (4 * (e >> 6) + (e & 3)));
     if (q == j) mine = e;
   }
-  return Choice{mine, sure};
+  wave_lds_fence();
+  return mine;
 }
 
-// N / 4 chunks of 64 experts.  32768 tokens of 256 experts in 8 groups: see DESIGN.
-template <int N>
-__global__ __launch_bounds__(256) void k_route_scored(Gating g, const float* __restrict__ logits,
+// The first n <= 16 experts in rank order, lane q's the q-th, put in order by keys in fp64
+// (BIAS) or the logits.  Returns the choice of rank q.
+template <bool BIAS, int N>
+__device__ __forceinline__ int order_exact(const Gating& g, const float* zr, const float* sel_bias, int e, int n, double* row) {
+  const int q = lane_id() & 15;
+  const bool on = q < n;
+  e = on ? e : 0;
+  const ExactScores s(g, zr, BIAS ? N : 0);
+  const double key = BIAS ? number(s.of(e) + (double)gptr(sel_bias)[e]) : s.logit(e);
+  int* const who = (int*)(row + 16);
+  row[q] = key;
+  who[q] = e;
+  wave_lds_fence();
+  int ahead = 0;
+  for (int o = 0; o < n; ++o) ahead += before(row[o], who[o], key, e);
+  wave_lds_fence();
+  if (on) who[ahead] = e;
+  wave_lds_fence();
+  e = who[q];
+  wave_lds_fence();
+  return e;
+}
+
+// N / 4 chunks of 64 experts.  WAVES: 4, or with counts, which each block adds to memory from
+// a histogram of its own, as many as the registers allow (additions to one address come
+// some 17 ns apart, whatever block they are of: 512 blocks cost 8.6 us).
+template <int N, bool BIAS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_route_scored(Gating g, const float* __restrict__ logits,
                                                       const float* __restrict__ sel_bias, const uint8_t* __restrict__ keep,
                                                       int T, int32_t* __restrict__ idx, float* __restrict__ gate,
                                                       int32_t* __restrict__ counts) {
-  __shared__ double rows[GT_TOK][16 * N];
+  constexpr int TOK = 4 * WAVES;
+  __shared__ double rows[TOK][key_row<N>];
   __shared__ int hist[16 * N];
   const int lane = lane_id(), q = lane & 15, tok = threadIdx.x >> 4;
   if (counts) {
-    for (int e = threadIdx.x; e < g.E; e += 256) hist[e] = 0;
+    for (int e = threadIdx.x; e < g.E; e += 64 * WAVES) hist[e] = 0;
     __syncthreads();
   }
-  for (int t0 = blockIdx.x * GT_TOK; t0 < T; t0 += gridDim.x * GT_TOK) {
+  float bias[N];
+  if (BIAS) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) bias[i] = gptr(sel_bias)[min(expert_at(i, q), g.E - 1)];
+  }
+  for (int t0 = blockIdx.x * TOK; t0 < T; t0 += gridDim.x * TOK) {
     const int t = t0 + tok, tc = min(t, T - 1);   // rows behind the last token repeat it
     const float* const zr = logits + (size_t)tc * g.E;
-    float z[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int e = 64 * (i / 4) + 4 * q + i % 4;
-      z[i] = e < g.E ? number(gptr(zr)[e]) + 0.f : minus_inf<float>();
-    }
-    Choice c;
-    if (sel_bias) {
-      float s[N], key[N];
-      scores<float>(g, z, s);
-      float top = 0.f;   // the largest finite key's magnitude
+    float z[N], s[N], m = 0.f, total = 0.f;
+    load_logits<N>(zr, g.E, q, z);
+    bool sure = true;
+    const bool two = g.n_group > 1 && g.group_top == 2;
+    if (BIAS || two || (!g.sigmoid && !g.renorm)) fast_scores<N>(g, z, s, m, total);
+    // a key's error in fp32, twice, and half a step of each of two keys
+    float gap = g.sigmoid ? 0x1p-21f : 0x1p-18f;
+    float top = minus_inf<float>();
+    uint32_t left = ~0u;
+    // keys, into s with a bias
+    if (BIAS) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int e = 64 * (i / 4) + 4 * q + i % 4;
-        key[i] = e < g.E ? number(s[i] + gptr(sel_bias)[e]) : minus_inf<float>();
-        const float a = fabsf(key[i]);
-        if (a < __builtin_inff()) top = larger(top, a);
-      }
-      // steps of 2^-24 of a score (below 1): exponential and quotient 5, the softmax's sum 20
-      // more, so keys differ by 2^-21 or 2^-18.4 from the exact ones' difference at most, and
-      // by half a step of the larger each
-      const float gap = (g.sigmoid ? 0x1p-20f : 0x1p-18f) + 0x1p-22f * row_max(top);
-      c = select(g, key, key, gap, g.group_top == 2 ? 4 * gap : gap, (float*)rows[tok]);
-      if (__any(!c.sure)) {
-        double sd[N], kd[N];
-        scores<double>(g, z, sd);
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int e = 64 * (i / 4) + 4 * q + i % 4;
-          kd[i] = e < g.E ? number(sd[i] + (double)gptr(sel_bias)[e]) : minus_inf<double>();
-        }
-        c = select(g, kd, kd, 0.0, 0.0, rows[tok]);
-      }
-    } else if (g.n_group > 1 && g.group_top == 2) {
-      float s[N];
-      scores<float>(g, z, s);
-      c = select(g, z, s, 0.f, g.sigmoid ? 0x1p-18f : 0x1p-16f, (float*)rows[tok]);   // sums of two
-      if (__any(!c.sure)) {
-        double sd[N], zd[N];
-        scores<double>(g, z, sd);
-#pragma unroll
-        for (int i = 0; i < N; ++i) zd[i] = z[i];
-        c = select(g, zd, sd, 0.0, 0.0, rows[tok]);
+        s[i] = __builtin_fmaxf(s[i] + bias[i], minus_inf<float>());
+        if (expert_at(i, q) >= g.E) s[i] = minus_inf<float>();
+        top = larger(top, s[i]);
       }
     } else {
-      c = select(g, z, z, 0.f, 0.f, (float*)rows[tok]);
+#pragma unroll
+      for (int i = 0; i < N; ++i) top = larger(top, z[i]);
+    }
+    top = row_max(top);
+    constexpr float WINDOW = BIAS ? 2.f : 32.f;
+    if (BIAS) gap += 0x1p-23f * (fabsf(top) + WINDOW);
+    if (g.n_group > 1) {
+      // (a rank of two keys: twice the error, and the sum's rounding)
+      const float rank_gap = two ? 2 * gap + 0x1p-22f * (BIAS ? fabsf(top) + WINDOW : 2.f) : BIAS ? gap : 0.f;
+      uint32_t near = 0;
+      if (BIAS || two) left = groups_kept<N>(g, s, rank_gap, gap, (float*)rows[tok], near);
+      else left = groups_kept<N>(g, z, 0.f, 0.f, (float*)rows[tok], near);
+      if (__any(near != 0)) left = near_groups<BIAS, N>(g, s, zr, sel_bias, near, rows[tok]);
+    }
+    if (!(fabsf(top) < __builtin_inff())) sure = false;
+    // packed keys: 1 + the distance from the window's bottom, then 255 - expert; 0: cannot be chosen
+    constexpr float UNITS = 0xFFFFFE.0p0f / WINDOW;
+    const float bottom = top - WINDOW;
+    uint32_t pk[N];
+    const uint32_t base = 256 + 255 - 4 * q;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float d = __builtin_fmaxf(((BIAS ? s[i] : z[i]) - bottom) * UNITS, 0.f);
+      const uint32_t v = ((uint32_t)d << 8) + (base - expert_at(i, 0));
+      pk[i] = expert_at(i, q) < g.E && (left >> i & 1) ? v : 0u;
+    }
+    uint32_t win = 0;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) win = larger3(win, pk[i], pk[i + 1]);
+    win = row_max_u(win);
+    const uint32_t need = BIAS ? (uint32_t)fminf(gap * UNITS, 1e6f) + 4u : 1u;   // (two keys, two units of rounding and one of the cut)
+    const int places = g.topk_group * g.size, rounds = min(g.k + 1, places);
+    int mine = 0;
+    uint32_t kth = 0;
+    bool apart = true;   // neighbours in rank order
+    auto following = [&] {
+      uint32_t next = 0;
+#pragma unroll
+      for (int i = 0; i < N; i += 2) next = larger3(next, pk[i] - win, pk[i + 1] - win);   // those below win wrap
+      return row_max_u(next) + win;
+    };
+    for (int j = 0;; ++j) {
+      if (q == j) mine = 255 - (int)(win & 255u);
+      if (j == g.k - 1) kth = win >> 8;
+      if (j + 1 >= rounds) break;
+      const uint32_t next = following();
+      if ((win >> 8) - (next >> 8) < need) apart = false;
+      win = next;
+    }
+    if (__any(!sure)) {
+      mine = select_exact<BIAS, N>(g, zr, sel_bias, rows[tok]);
+    } else if (__any(!apart)) {
+      const int more = min(16, places);
+      for (int j = rounds; j < more; ++j) {
+        win = following();
+        if (q == j) mine = 255 - (int)(win & 255u);
+      }
+      if (__any(places > 16 && kth - (win >> 8) < need)) mine = select_exact<BIAS, N>(g, zr, sel_bias, rows[tok]);
+      else mine = order_exact<BIAS, N>(g, zr, sel_bias, mine, more, rows[tok]);
     }
     // gates: lane j the choice of rank j
-    const bool mine = q < g.k;
-    const float zj = mine ? number(gptr(zr)[c.e]) : minus_inf<float>();
+    const bool on = q < g.k;
+    const float zj = on ? number(gptr(zr)[mine]) : minus_inf<float>();
     float w, S = 1.f;
     if (g.renorm) {
-      const float m = row_max(zj);
-      w = g.sigmoid ? logistic(zj, fminf(m, 0.f)) : softmax_part(zj, m);
-      if (!mine) w = 0.f;
+      const float mj = row_max(zj);
+      w = g.sigmoid ? logistic(zj, fminf(mj, 0.f)) : softmax_part(zj, mj);
+      if (!on) w = 0.f;
       S = row_sum(w);
     } else if (g.sigmoid) {
       w = logistic(zj);
     } else {
-      float m = z[0], sum = 0.f;
-#pragma unroll
-      for (int i = 1; i < N; ++i) m = larger(m, z[i]);
-      m = row_max(m);
-#pragma unroll
-      for (int i = 0; i < N; ++i) sum += softmax_part(z[i], m);
       w = softmax_part(zj, m);
-      S = row_sum(sum);
+      S = total;
     }
-    if (mine && t < T) {
-      idx[(size_t)t * g.k + q] = c.e;
+    if (on && t < T) {
+      idx[(size_t)t * g.k + q] = mine;
       gate[(size_t)t * g.k + q] = S > 0.f ? g.scale * (w / S) : 0.f;
-      if (counts && (!keep || keep[t])) atomicAdd(&hist[c.e], 1);
+      if (counts && (!keep || keep[t])) atomicAdd(&hist[mine], 1);
     }
   }
   if (counts) {
     __syncthreads();
-    for (int e = threadIdx.x; e < g.E; e += 256)
+    for (int e = threadIdx.x; e < g.E; e += 64 * WAVES)
       if (hist[e]) atomicAdd(&counts[e], hist[e]);
   }
 }
@@ -295,12 +547,9 @@ __global__ __launch_bounds__(256) void k_route_scored_bwd(Gating g, const float*
   const float dg = mine ? g.scale * gptr(dgate)[(size_t)tc * g.k + q] : 0.f;
   float z[N], m = minus_inf<float>(), sum = 0.f;
   if (dense) {
+    load_logits<N>(zr, g.E, q, z);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int ei = 64 * (i / 4) + 4 * q + i % 4;
-      z[i] = ei < g.E ? number(gptr(zr)[ei]) : minus_inf<float>();
-      m = larger(m, z[i]);
-    }
+    for (int i = 0; i < N; ++i) m = larger(m, z[i]);
     m = row_max(m);
 #pragma unroll
     for (int i = 0; i < N; ++i) sum += z[i] = softmax_part(z[i], m);
@@ -349,12 +598,25 @@ __global__ __launch_bounds__(256) void k_route_scored_bwd(Gating g, const float*
   wave_lds_fence();
   if (t >= T) return;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int ei = 64 * (i / 4) + 4 * q + i % 4;
-    if (ei >= g.E) continue;
-    float v = row[ei];
-    if (dense) v = z[i] * (v - inner);
-    gptr(out)[ei] = accumulate ? gptr(out)[ei] + v : v;
+  for (int c = 0; c < N / 4; ++c) {
+    const int e0 = expert_at(4 * c, q);
+    if (e0 >= g.E) continue;
+    u32x4_t v = *(const u32x4_t*)(row + e0);
+    if (dense)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) v[b] = __float_as_uint(z[4 * c + b] * (__uint_as_float(v[b]) - inner));
+    if ((g.E & 3) == 0) {
+      if (accumulate) {
+        const u32x4_t old = ld16(out + e0);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) v[b] = __float_as_uint(__uint_as_float(old[b]) + __uint_as_float(v[b]));
+      }
+      st16(out + e0, v);
+    } else {
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        if (e0 + b < g.E) gptr(out)[e0 + b] = accumulate ? gptr(out)[e0 + b] + __uint_as_float(v[b]) : __uint_as_float(v[b]);
+    }
   }
 }
 
@@ -396,7 +658,8 @@ int check_gating(const moe_gating* g, int T) {
 Gating device_gating(const moe_gating* g) {
   // groups that all stay change nothing
   const int n = g->topk_group == g->n_group ? 1 : g->n_group;
-  return Gating{g->E, g->k, n, n == 1 ? 1 : g->topk_group, g->group_top, g->E / n, g->score == MOE_SCORE_SIGMOID,
+  const int size = g->E / n, lanes = size >= 4 && size <= 64 && (size & (size - 1)) == 0 ? size / 4 : 0;
+  return Gating{g->E, g->k, n, n == 1 ? 1 : g->topk_group, g->group_top, size, lanes, g->score == MOE_SCORE_SIGMOID,
                 g->renorm != 0, g->scale};
 }
 
@@ -414,15 +677,21 @@ extern "C" int moe_route_scored(const moe_gating* g, const float* logits, const 
   FM_TRY(need_aligned(logits, "logits")); FM_TRY(need_aligned(sel_bias, "sel_bias")); FM_TRY(need_aligned(keep, "keep"));
   FM_TRY(need_aligned(idx, "idx")); FM_TRY(need_aligned(gate, "gate")); FM_TRY(need_aligned(counts, "counts"));
   const Gating dg = device_gating(g);
-  // with counts every block adds its own histogram: fewer blocks, each several times
-  const int blocks = cdiv(T, GT_TOK), most = counts ? 4 * device_cus() : 1 << 20;
+  // (16 waves of 128 registers hold up to 128 experts, 8 waves 256)
+  const bool wide = counts && T > 2048;
+  const int waves = !wide ? 4 : g->E <= 128 ? 16 : 8;
+  const int blocks = cdiv(T, 4 * waves), most = wide ? device_cus() : 1 << 20;
   const dim3 grid(blocks < most ? blocks : most);
-#define FM_GT(N)                                                                                              \
-  hipLaunchKernelGGL(k_route_scored<N>, grid, dim3(256), 0, as_stream(stream), dg, logits, sel_bias, keep, T, idx, gate, \
-                     counts)
-  if (g->E <= 64) FM_GT(4);
-  else if (g->E <= 128) FM_GT(8);
-  else FM_GT(16);
+#define FM_GT(N, BIAS, WAVES)                                                                                            \
+  hipLaunchKernelGGL((k_route_scored<N, BIAS, WAVES>), grid, dim3(64 * WAVES), 0, as_stream(stream), dg, logits, sel_bias, \
+                     keep, T, idx, gate, counts)
+#define FM_GT_B(N, WIDE)                                             \
+  if (wide) { if (sel_bias) FM_GT(N, true, WIDE); else FM_GT(N, false, WIDE); } \
+  else { if (sel_bias) FM_GT(N, true, 4); else FM_GT(N, false, 4); }
+  if (g->E <= 64) { FM_GT_B(4, 16) }
+  else if (g->E <= 128) { FM_GT_B(8, 16) }
+  else { FM_GT_B(16, 8) }
+#undef FM_GT_B
 #undef FM_GT
   return check_launch("moe_route_scored");
 }
