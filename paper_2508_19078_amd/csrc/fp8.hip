@@ -234,23 +234,29 @@ __global__ __launch_bounds__(256) void k_f8_prep(const bf16* __restrict__ X, Row
                xs + (size_t)r * scale_row(nb));
 }
 
-// RA activation rows x RB weight rows by 2 x 4 waves, one block per compute unit.
-template <int RA_> struct F8Cfg {
-  static constexpr int RA = RA_, RB = 256, NW = 8, BPC = 1;
-  static constexpr int TM = RA / 2, TN = RB / 4, MI = TM / 32, NJ = TN / 32;
-  static constexpr int A_BYTES = RA * 128, SLAB = A_BYTES + RB * 128;   // 128 k
+// RA activation rows x RB weight rows by 2 x 4 waves, one block per compute unit.  LDS: rings
+// of RING slabs of activations (the place of BIG rows, the larger tile's that shares the
+// kernel) and of weights, then two groups of scales [BIG rows][16 bytes].
+template <int RA_, int RING_, int BIG> struct F8Cfg {
+  static constexpr int RA = RA_, RB = 256, NW = 8, BPC = 1, RING = RING_;
+  static constexpr int TM = RA / 2, TN = RB / 4, MI = TM / 16, NJ = TN / 16;
+  static constexpr int A_BYTES = RA * 128, B_BYTES = RB * 128, B_BASE = RING * BIG * 128;   // 128 k
   static constexpr int A_INS = RA / 8 / NW, B_INS = RB / 8 / NW;        // 8 rows each, per wave
-  static constexpr int SCALES = RA * 16;                                // of 4 slabs
-  static constexpr int LDS = 2 * (SLAB + SCALES);
-  static_assert(RA % 64 == 0 && NJ == 2 && RA <= 64 * NW, "tile");
-  static_assert(LDS <= 160 * 1024, "LDS");
+  static constexpr int AHEAD = RING == 3 ? A_INS + B_INS : 0;           // requests of slab kt + 1 that may be under way at kt
+  static constexpr int LAST = B_BASE + (RING - 1) * B_BYTES;            // the last weight slab's place, free until a tile's first barrier
+  static constexpr int SCALES = B_BASE + RING * B_BYTES, GROUP = BIG * 16;
+  static constexpr int LDS = SCALES + 2 * GROUP;
+  static_assert(RA % 64 == 0 && RA <= BIG && RA <= 64 * NW && NJ == 4 && (RING == 2 || RING == 3), "tile");
+  static_assert(LDS <= 160 * 1024 && NW * 2048 <= B_BYTES, "LDS");
 };
 
-// Chunk swizzles of a 128-byte slab row: 16 consecutive lanes' rows at one logical
-// chunk on distinct 4-bank groups; lanes read activation rows in order, weight rows in
-// the order of tile_column.
+// Chunk swizzles of a 128-byte slab row: the 16 rows that lanes read at one logical chunk
+// lie on distinct 4-bank groups.  Activation rows come in order; a fragment's weight rows are
+// 4 out of every 8 of 32 (gate or up) or of every 16 of 64 columns.
 __device__ __forceinline__ int f8_swz_a(int r) { return (r >> 1) & 7; }
-__device__ __forceinline__ int f8_swz_b(int r) { return ((r >> 1) & 3) | ((r >> 2) & 4); }
+template <bool PAIR> __device__ __forceinline__ int f8_swz_b(int r) {
+  return ((r >> 1) & 1) | ((PAIR ? r >> 3 : r >> 4) & 3) << 1;
+}
 
 // One operand pair of a tile, rows relative to it.  w2: the second of two matrices
 // whose 32-row blocks alternate (gate, up).
@@ -260,7 +266,7 @@ struct F8Tile {
   const int32_t* tok;           // row -> activation row (gathered), or NULL
   int rows, Tn;                 // activation rows of the tile's slot from the tile on
   const uint8_t *w, *w2;
-  const float* s[2];            // this wave's weight scales by slab, of its two 32-column blocks
+  const float* s[2];            // this wave's weight scales by slab, of gate and up (or twice the same)
   int wrows;                    // weight rows (per matrix) from the tile on
   int nk, kw;                   // slabs; 16-byte chunks of a weight row
 };
@@ -269,16 +275,19 @@ template <typename F, int... N> __device__ __forceinline__ void f8_steps(F f, st
   (f(std::integral_constant<int, N>{}), ...);
 }
 
-// acc += X W^T.  LDS: two slabs, then two groups of scales [RA rows][16 bytes].  The
-// barrier at the top of slab kt says that it has landed and that every wave has read slab
-// kt - 1, whose buffer then takes slab kt + 1.  Scales of group g (slabs 4 g to 4 g + 3)
-// are requested at slab 4 g - 2 and put into LDS at slab 4 g - 1.
+// acc = X W^T: acc[i][j][e] of lane l is row 16 i + l % 16 of the wave's and, with g = l / 16,
+// column 8 g + 4 (j % 2) + e of its 32 of gate (j < 2) or up, or column 16 g + 4 j + e of its 64.
+//
+// The barrier at the top of slab kt says that it has landed and that every wave has read
+// slab kt - 1, whose places then take slab kt + RING - 1.  Scales of group g (slabs 4 g to
+// 4 g + 3), 16 bytes of a row, are requested at slab 4 g - 2 by the waves that 64 rows each
+// give work.  Sums of a 16 x 16 tile are taken two products after it was issued, so that
+// neither waits for the other.
 template <class C, bool PAIR>
-__device__ __forceinline__ void f8_gemm(const F8Tile& t, FM_LDS char* lds, f32x16_t (&acc)[C::MI][C::NJ]) {
+__device__ __forceinline__ void f8_gemm(const F8Tile& t, FM_LDS char* lds, f32x4_t (&acc)[C::MI][C::NJ]) {
   const int lane = lane_id(), wave = wave_id();
   const int nk = t.nk;
   const uint32_t ldx = nk * 128, ldw = t.kw * 16;
-  FM_LDS char* const sc = lds + 2 * C::SLAB;
   uint32_t oa[C::A_INS], ob[C::B_INS];
   auto xrow = [&](int r) {
     r = min(r, t.rows - 1);
@@ -292,117 +301,101 @@ __device__ __forceinline__ void f8_gemm(const F8Tile& t, FM_LDS char* lds, f32x1
 #pragma unroll
   for (int u = 0; u < C::B_INS; ++u) {
     const int r = 8 * (wave * C::B_INS + u) + (lane >> 3);
-    ob[u] = (uint32_t)min(PAIR ? 32 * (r >> 6) + (r & 31) : r, t.wrows - 1) * ldw + 16 * ((lane & 7) ^ f8_swz_b(r));
+    ob[u] = (uint32_t)min(PAIR ? 32 * (r >> 6) + (r & 31) : r, t.wrows - 1) * ldw + 16 * ((lane & 7) ^ f8_swz_b<PAIR>(r));
   }
   // behind a row's end, weights repeat their row's last chunk (it meets zeros)
-  auto issue = [&](int slab) {
-    FM_LDS char* const l = lds + (slab & 1) * C::SLAB;
+  auto issue = [&](int slab, int place) {
+    FM_LDS char* const la = lds + place * C::A_BYTES;
+    FM_LDS char* const lb = lds + C::B_BASE + place * C::B_BYTES;
 #pragma unroll
-    for (int u = 0; u < C::A_INS; ++u)
-      dma16s(t.x + (size_t)slab * 128, oa[u], l + (wave * C::A_INS + u) * 1024);
+    for (int u = 0; u < C::A_INS; ++u) dma16s(t.x + (size_t)slab * 128, oa[u], la + (wave * C::A_INS + u) * 1024);
 #pragma unroll
     for (int u = 0; u < C::B_INS; ++u) {
       const int ins = wave * C::B_INS + u;
       const uint8_t* const w = (PAIR && ((ins >> 2) & 1) ? t.w2 : t.w) + (size_t)slab * 128;
-      uint32_t o = ob[u];
+      uint32_t at = ob[u];
       if (8 * slab + 8 > t.kw) {
-        const int k = (lane & 7) ^ f8_swz_b(8 * ins + (lane >> 3));
-        o += 16 * (min(k, t.kw - 1 - 8 * slab) - k);
+        const int k = (lane & 7) ^ f8_swz_b<PAIR>(8 * ins + (lane >> 3));
+        at += 16 * (min(k, t.kw - 1 - 8 * slab) - k);
       }
-      dma16s(w, o, l + C::A_BYTES + ins * 1024);
+      dma16s(w, at, lb + ins * 1024);
     }
   };
-  // waves below RA / 64 keep a row's scales per lane
-  const int sr = 64 * wave + lane;
   const bool keeper = 64 * wave < C::RA;
-  const float* sp = t.xs;
-  if (keeper) sp += (size_t)xrow(sr) * scale_row(nk);
-  auto put_scales = [&](int g, const u32x4_t& v) {
-    if (keeper) *(FM_LDS u32x4_t*)(sc + (g & 1) * C::SCALES + sr * 16) = v;
+  const uint32_t os = xrow(keeper ? 64 * wave + lane : 0) * (scale_row(nk) * 4);
+  auto issue_scales = [&](int group) {
+    if (keeper) dma16s(t.xs + 4 * group, os, lds + C::SCALES + (group & 1) * C::GROUP + wave * 1024);
   };
   const int row0 = (wave & 1) * C::TM, col0 = (wave >> 1) * C::TN;
-  const int m = lane & 31, h = lane >> 5;
-  // this lane's first chunk in a slab; its rows of the other 32-row blocks lie 4096 bytes
-  // on (32 rows leave the swizzles as they are), its other chunks at an exclusive or
-  const int ra = row0 + m, rb = col0 + tile_column(m);
-  const uint32_t fa = ra * 128 + ((h ^ f8_swz_a(ra)) << 4), fb = C::A_BYTES + rb * 128 + ((h ^ f8_swz_b(rb)) << 4);
-  const uint32_t ga = (row0 + m) * 16;
+  const int o = lane & 15, kb = lane >> 4;
+  // this lane's chunk kb of a slab's first rows (kb + 4: at an exclusive or with 64); other
+  // fragments lie a constant on, which leaves the swizzles as they are
+  const int ra = row0 + o, rb = col0 + (PAIR ? 8 : 16) * (o >> 2) + (o & 3);
+  const uint32_t fa = (uint32_t)(uintptr_t)lds + ra * 128 + ((kb ^ f8_swz_a(ra)) << 4);
+  const uint32_t fb = (uint32_t)(uintptr_t)lds + rb * 128 + ((kb ^ f8_swz_b<PAIR>(rb)) << 4);
 #pragma unroll
   for (int i = 0; i < C::MI; ++i)
 #pragma unroll
-    for (int j = 0; j < C::NJ; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    for (int j = 0; j < C::NJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-  issue(0);
-  if (keeper) put_scales(0, ld16(sp));
-  u32x4_t next = {0, 0, 0, 0};
-  float w0 = ld_scalar(t.s[0]), w1 = ld_scalar(t.s[1]);
+  issue_scales(0);
+  issue(0, 0);
+  if (C::RING == 3 && nk > 1) issue(1, 1);
+  float w0 = ld_scalar(t.s[0]), w1 = PAIR ? ld_scalar(t.s[1]) : 0.f;
+  const FM_LDS char* const sc = lds + C::SCALES + (row0 + o) * 16;
+  int place = 0;   // of slab kt
 #pragma nounroll
   for (int kt = 0; kt < nk; ++kt) {
-    wait_vmcnt<0>();
+    if (kt + 1 < nk) wait_vmcnt<C::AHEAD>();
+    else wait_vmcnt<0>();
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (kt + 1 < nk) issue(kt + 1);
-    if ((kt & 3) == 2 && kt + 2 < nk && keeper) next = ld16(sp + kt + 2);
-    if ((kt & 3) == 3 && kt + 1 < nk) put_scales((kt >> 2) + 1, next);
+    if ((kt & 3) == 2 && kt + 2 < nk) issue_scales((kt >> 2) + 1);
+    if (kt + C::RING - 1 < nk) issue(kt + C::RING - 1, place == 0 ? C::RING - 1 : place - 1);   // where slab kt - 1 was
     const float sw[2] = {w0, w1};
     const int kn = min(kt + 1, nk - 1);
     w0 = ld_scalar(t.s[0] + kn);
-    w1 = ld_scalar(t.s[1] + kn);
-    const uint32_t slab = (uint32_t)(uintptr_t)lds + (kt & 1) * C::SLAB;
-    const FM_LDS char* const s = sc + ((kt >> 2) & 1) * C::SCALES + ga + 4 * (kt & 3);
-    // 64 k of a row: chunks 4 step + h and 4 step + 2 + h
-    const uint32_t aa = slab + fa, ab = slab + fb;
-    auto chunk = [](uint32_t at, int c, int blk) { return *(const FM_LDS u32x4_t*)(uintptr_t)((at ^ (c << 5)) + 4096 * blk); };
-    auto frag = [&](uint32_t at, int step, int blk) {
-      const u32x4_t a = chunk(at, 2 * step, blk), b = chunk(at, 2 * step + 1, blk);
+    if (PAIR) w1 = ld_scalar(t.s[1] + kn);
+    const uint32_t aa = fa + place * C::A_BYTES, ab = fb + C::B_BASE + place * C::B_BYTES;
+    const FM_LDS char* const s = sc + ((kt >> 2) & 1) * C::GROUP + 4 * (kt & 3);
+    auto frag = [](uint32_t at, int off) {
+      const u32x4_t a = *(const FM_LDS u32x4_t*)(uintptr_t)(at + off), b = *(const FM_LDS u32x4_t*)(uintptr_t)((at ^ 64) + off);
       return i32x8_t{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
     };
-    i32x8_t xb[2][C::NJ], xa[2][2];   // [step][block], [block's parity][step]
-    float sx[2];
-    auto read_a = [&](int i) {
-      xa[i & 1][0] = frag(aa, 0, i);
-      xa[i & 1][1] = frag(aa, 1, i);
-      sx[i & 1] = *(const FM_LDS float*)(s + 512 * i);
-    };
+    auto b_off = [](int j) { return (PAIR ? 32 * (j >> 1) + 4 * (j & 1) : 4 * j) * 128; };
+    i32x8_t xb[C::NJ], xa[2];
+    float sx[C::MI];
     // LDS answers in order: what the first products take is asked for first
-    xb[0][0] = frag(ab, 0, 0);
-    xa[0][0] = frag(aa, 0, 0);
+    xb[0] = frag(ab, 0);
+    xa[0] = frag(aa, 0);
     sched_fence();
-    xb[1][0] = frag(ab, 1, 0);
-    xa[0][1] = frag(aa, 1, 0);
-    sx[0] = *(const FM_LDS float*)s;
-    sched_fence();
-    // a tile's two products, and between them the sums of the tile before it, which the
-    // matrix unit has finished by then
-    constexpr int N = C::MI * C::NJ;
-    f32x16_t p[2];
-    float f[2];
-    auto add = [&](auto n_, auto half_) {
-      constexpr int n = decltype(n_)::value, half = decltype(half_)::value;
-      if constexpr (n >= 0) {
 #pragma unroll
-        for (int e = 8 * half; e < 8 * half + 8; ++e)
-          acc[n / C::NJ][n % C::NJ][e] = fmaf(p[n & 1][e], f[n & 1], acc[n / C::NJ][n % C::NJ][e]);
-      }
-    };
+    for (int j = 1; j < C::NJ; ++j) xb[j] = frag(ab, b_off(j));
+#pragma unroll
+    for (int i = 0; i < C::MI; ++i) sx[i] = *(const FM_LDS float*)(s + 256 * i);
+    sched_fence();
+    constexpr int N = C::MI * C::NJ, D = 2;   // D: products between one and its sums
+    f32x4_t p[4];
+    float f[2];
     auto step = [&](auto n_) {
       constexpr int n = decltype(n_)::value, i = n / C::NJ, j = n % C::NJ;
-      const f32x16_t zero = {};
-      if constexpr (n < N) p[n & 1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xb[0][j], xa[i & 1][0], zero, 0, 0, 0, 0, 0, 0);
+      if constexpr (n < N) {
+        if constexpr (j == 0 && i + 1 < C::MI) xa[(i + 1) & 1] = frag(aa, 2048 * (i + 1));
+        p[n & 3] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(xb[j], xa[i & 1], f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+      }
       sched_fence();
-      if constexpr (n == 0) xb[0][1] = frag(ab, 0, 1);
-      if constexpr (n == 0) xb[1][1] = frag(ab, 1, 1);
-      if constexpr (j == 0 && i + 1 < C::MI) read_a(i + 1);
-      add(std::integral_constant<int, n - 1>{}, std::integral_constant<int, 0>{});
-      sched_fence();
-      if constexpr (n < N) p[n & 1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xb[1][j], xa[i & 1][1], p[n & 1], 0, 0, 0, 0, 0, 0);
-      sched_fence();
-      add(std::integral_constant<int, n - 1>{}, std::integral_constant<int, 1>{});
-      if constexpr (n < N) f[n & 1] = sx[i & 1] * sw[j];
+      if constexpr (n >= D) {
+        constexpr int m = n - D, mi = m / C::NJ, mj = m % C::NJ;
+        if constexpr (mj == 0) {
+          f[0] = sx[mi] * sw[0];
+          if (PAIR) f[1] = sx[mi] * sw[1];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[mi][mj][e] = fmaf(p[m & 3][e], f[PAIR ? mj >> 1 : 0], acc[mi][mj][e]);
+      }
       sched_fence();
     };
-    f8_steps(step, std::make_integer_sequence<int, N + 1>{});
+    f8_steps(step, std::make_integer_sequence<int, N + D>{});
+    place = place == C::RING - 1 ? 0 : place + 1;
   }
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
@@ -434,42 +427,44 @@ __device__ __forceinline__ void f8_gate_up_tile(const F8Args& a, FM_LDS char* ld
   t.wrows = I - n0;
   t.nk = nd;
   t.kw = ra.d / 16;
-  f32x16_t acc[C::MI][C::NJ];
+  f32x4_t acc[C::MI][C::NJ];
   f8_gemm<C, true>(t, lds, acc);
-  const int lane = lane_id_here(), wave = wave_id(), h = lane >> 5, part = wave >> 1;
-  const int row0 = (wave & 1) * C::TM + (lane & 31), col = n0 + part * 32 + 16 * h;
+  const int lane = lane_id_here(), wave = wave_id(), g = lane >> 4, part = wave >> 1;
+  const int row0 = (wave & 1) * C::TM + (lane & 15), col = n0 + part * 32 + 8 * g;
 #pragma unroll
   for (int i = 0; i < C::MI; ++i) {
     uint32_t top = 0;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float g = acc[i][0][e];
-      acc[i][0][e] = col + e < I ? g * sigm_fast(g) * acc[i][1][e] : 0.f;
-      top = max(top, abs_bits(acc[i][0][e]));
-    }
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float v = acc[i][j][e];
+        acc[i][j][e] = col + 4 * j + e < I ? v * sigm_fast(v) * acc[i][j + 2][e] : 0.f;
+        top = max(top, abs_bits(acc[i][j][e]));
+      }
+    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
     top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-    if (h == 0) tops[(row0 + 32 * i) * 4 + part] = top;
+    if (g == 0) tops[(row0 + 16 * i) * 4 + part] = top;
   }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < C::MI; ++i) {
-    const int row = row0 + 32 * i;
+    const int row = row0 + 16 * i;
     const u32x4_t tp = *(const FM_LDS u32x4_t*)(tops + row * 4);
     const F8Block b = f8_block(max(max(tp[0], tp[1]), max(tp[2], tp[3])));
-    float v[16];
+    float v[8];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) v[e] = acc[i][0][e];
+    for (int e = 0; e < 8; ++e) v[e] = acc[i][e / 4][e % 4];
     if (row < r.rows) {
-      st16(a.w.hq + (r.ob + row) * (nI * 128) + col,
-           u32x4_t{f8_codes4(v, b), f8_codes4(v + 4, b), f8_codes4(v + 8, b), f8_codes4(v + 12, b)});
-      if (part == 0 && h == 0) gptr(a.w.hs)[(r.ob + row) * scale_row(nI) + r.n] = b.scale;
+      *(FM_GLOBAL u32x2_t*)(a.w.hq + (r.ob + row) * (nI * 128) + col) = u32x2_t{f8_codes4(v, b), f8_codes4(v + 4, b)};
+      if (part == 0 && g == 0) gptr(a.w.hs)[(r.ob + row) * scale_row(nI) + r.n] = b.scale;
     }
   }
 }
 
 // O = F8(H) Qd^T of one tile, 256 columns.  A wave's 32 rows x 64 columns go out through
-// LDS, so that a store covers whole lines of 8 rows.  stage: 4 KB per wave that the next
-// tile's first slab and scales leave alone.
+// LDS 16 at a time, so that a store covers whole lines of 8 rows.  stage: 2 KB per wave that
+// the next tile's first slabs leave alone.
 template <class C>
 __device__ __forceinline__ void f8_down_tile(const F8Args& a, FM_LDS char* lds, FM_LDS char* stage, const TileRows& r) {
   const RowArgs& ra = a.ra;
@@ -488,26 +483,24 @@ __device__ __forceinline__ void f8_down_tile(const F8Args& a, FM_LDS char* lds, 
   t.wrows = d - n0;
   t.nk = nI;
   t.kw = ra.I / 16;
-  f32x16_t acc[C::MI][C::NJ];
+  f32x4_t acc[C::MI][C::NJ];
   f8_gemm<C, false>(t, lds, acc);
-  const int lane = lane_id_here(), wave = wave_id(), h = lane >> 5;
-  FM_LDS char* const mine = stage + wave * 4096;   // [32 rows][8 chunks of 16 bytes], chunks swizzled by the row
-  const int m = lane & 31, col = n0 + (wave >> 1) * C::TN + 8 * (lane & 7);
+  const int lane = lane_id_here(), wave = wave_id(), g = lane >> 4, m = lane & 15;
+  FM_LDS char* const mine = stage + wave * 2048;   // [16 rows][8 chunks of 16 bytes], chunks swizzled by the row
+  const int col = n0 + (wave >> 1) * C::TN + 8 * (lane & 7);
 #pragma unroll
   for (int i = 0; i < C::MI; ++i) {
 #pragma unroll
-    for (int j = 0; j < C::NJ; ++j)
+    for (int h = 0; h < 2; ++h) {
+      float v[8];
 #pragma unroll
-      for (int e = 0; e < 16; e += 8) {
-        float v[8];
-#pragma unroll
-        for (int x = 0; x < 8; ++x) v[x] = acc[i][j][e + x];
-        *(FM_LDS u32x4_t*)(mine + m * 128 + (((4 * j + 2 * h + e / 8) ^ (m & 7)) << 4)) = pack16(v, (bf16*)nullptr);
-      }
+      for (int e = 0; e < 8; ++e) v[e] = acc[i][2 * h + e / 4][e % 4];
+      *(FM_LDS u32x4_t*)(mine + m * 128 + (((2 * g + h) ^ (m & 7)) << 4)) = pack16(v, (bf16*)nullptr);
+    }
     wave_lds_fence();
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int q = 8 * u + (lane >> 3), row = (wave & 1) * C::TM + 32 * i + q;
+    for (int u = 0; u < 2; ++u) {
+      const int q = 8 * u + (lane >> 3), row = (wave & 1) * C::TM + 16 * i + q;
       const u32x4_t v = *(const FM_LDS u32x4_t*)(mine + q * 128 + (((lane & 7) ^ (q & 7)) << 4));
       if (row < r.rows && col < d) st16(a.O + (r.ob + row) * d + col, v);
     }
@@ -515,33 +508,32 @@ __device__ __forceinline__ void f8_down_tile(const F8Args& a, FM_LDS char* lds, 
   }
 }
 
-template <class C, class BIG, bool DOWN>
-__device__ __forceinline__ void f8_tile(const F8Args& a, FM_LDS char* lds, const TileRows& r) {
-  // what an epilogue keeps in LDS lies behind the larger tile's first slab, inside the
-  // second slab of either height: the next tile requests that one only behind its first
-  // barrier
-  static_assert(BIG::SLAB + BIG::NW * 4096 <= 2 * C::SLAB, "stage");
-  if constexpr (DOWN) f8_down_tile<C>(a, lds, lds + BIG::SLAB, r);
-  else f8_gate_up_tile<C>(a, lds, (FM_LDS uint32_t*)(lds + BIG::SLAB), r);
+// What an epilogue keeps in LDS lies in the last weight slab's place, which the next tile
+// requests only behind its first barrier, in both heights.
+template <class C, bool DOWN> __device__ __forceinline__ void f8_tile(const F8Args& a, FM_LDS char* lds, const TileRows& r) {
+  if constexpr (DOWN) f8_down_tile<C>(a, lds, lds + C::LAST, r);
+  else f8_gate_up_tile<C>(a, lds, (FM_LDS uint32_t*)(lds + C::LAST), r);
 }
 
 // C: the tile; HALF: its half-height form for tiles with at most half the rows left.
 template <class C, class HALF, bool DOWN> __global__ __launch_bounds__(64 * C::NW, C::NW / 4) void k_f8_tiles(F8Args a) {
   __shared__ __align__(16) char lds_[C::LDS];
   FM_LDS char* const lds = (FM_LDS char*)lds_;
+  static_assert(C::LAST == HALF::LAST && C::LDS == HALF::LDS, "one layout");
   constexpr int COLS = DOWN ? C::RB : C::RB / 2;
   const int NT = ((DOWN ? a.ra.d : a.ra.I) + COLS - 1) / COLS;
   const TileWalk walk = tile_walk(a.ra, NT);
   for (int tt = walk.at; tt < walk.end; tt += walk.step) {
     const TileRows r = tile_rows_at(a.ra, tt, NT, C::RA);
-    if (r.rows <= HALF::RA) f8_tile<HALF, C, DOWN>(a, lds, r);
-    else f8_tile<C, C, DOWN>(a, lds, r);
+    if (r.rows <= HALF::RA) f8_tile<HALF, DOWN>(a, lds, r);
+    else f8_tile<C, DOWN>(a, lds, r);
   }
 }
 
-typedef F8Cfg<256> E256;
-typedef F8Cfg<128> E128;
-typedef F8Cfg<64> E64;
+typedef F8Cfg<256, 2, 256> E256;
+typedef F8Cfg<128, 2, 256> E256h;
+typedef F8Cfg<128, 3, 128> E128;
+typedef F8Cfg<64, 3, 128> E128h;
 
 // --------------------------------------------------------- a few tokens ----
 // Calls of a few tokens are bound by latency and by the weights' bytes, which have to be
@@ -873,7 +865,7 @@ extern "C" int moe_grouped_swiglu_fwd_fp8(const moe_layer_fp8* L, const void* X,
                        a, nd, T);
     return check_launch("moe_grouped_swiglu_fwd_fp8");
   }
-  if (tile == 256) f8_tiles<E256, E128>(a, (const bf16*)X, st);
-  else f8_tiles<E128, E64>(a, (const bf16*)X, st);
+  if (tile == 256) f8_tiles<E256, E256h>(a, (const bf16*)X, st);
+  else f8_tiles<E128, E128h>(a, (const bf16*)X, st);
   return check_launch("moe_grouped_swiglu_fwd_fp8");
 }
