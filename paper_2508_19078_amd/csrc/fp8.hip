@@ -78,6 +78,25 @@ __device__ __forceinline__ uint32_t f8_codes4(const float* v, const F8Block& b) 
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f8_quotient(v[2], b), f8_quotient(v[3], b), c, true);
 }
 
+// The same for H, which comes out of fp32 sums: scale and quotient to an ulp (a code moves
+// only where those sums' own error moves it too).
+__device__ __forceinline__ F8Block f8_block_h(uint32_t bits) {
+  F8Block b;
+  const float top = fmaxf(__uint_as_float(bits), F8_FLOOR);
+  b.scale = bits ? top * (1.f / F8_TOP) : 0.f;
+  b.inv = F8_TOP * __builtin_amdgcn_rcpf(top);
+  if (bits >= 0x7F800000u) {
+    b.scale = __uint_as_float(0x7FC00000u);
+    b.inv = 0.f;
+  }
+  return b;
+}
+__device__ __forceinline__ uint32_t f8_codes4_h(const float* v, const F8Block& b) {
+  const auto q = [&](float x) { return __builtin_amdgcn_fmed3f(x * b.inv, -F8_TOP, F8_TOP); };   // (0 times an infinity is no number)
+  int c = __builtin_amdgcn_cvt_pk_fp8_f32(q(v[0]), q(v[1]), 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q(v[2]), q(v[3]), c, true);
+}
+
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 template <int N> __device__ __forceinline__ uint32_t top_bits(const float* v) {
   uint32_t top = 0;
@@ -190,7 +209,7 @@ struct F8Ptrs {
   const float* const* sd;
 };
 
-constexpr int F8_FEW = 8;   // most tokens of a call that takes the kernels for few
+constexpr int F8_FEW = 16;   // most tokens of a call that takes the kernels for few
 
 // Workspace: row-tile prefix, X and H as rows of whole 128-blocks with their scales.
 struct F8Ws {
@@ -451,12 +470,12 @@ __device__ __forceinline__ void f8_gate_up_tile(const F8Args& a, FM_LDS char* ld
   for (int i = 0; i < C::MI; ++i) {
     const int row = row0 + 16 * i;
     const u32x4_t tp = *(const FM_LDS u32x4_t*)(tops + row * 4);
-    const F8Block b = f8_block(max(max(tp[0], tp[1]), max(tp[2], tp[3])));
+    const F8Block b = f8_block_h(max(max(tp[0], tp[1]), max(tp[2], tp[3])));
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = acc[i][e / 4][e % 4];
     if (row < r.rows) {
-      *(FM_GLOBAL u32x2_t*)(a.w.hq + (r.ob + row) * (nI * 128) + col) = u32x2_t{f8_codes4(v, b), f8_codes4(v + 4, b)};
+      *(FM_GLOBAL u32x2_t*)(a.w.hq + (r.ob + row) * (nI * 128) + col) = u32x2_t{f8_codes4_h(v, b), f8_codes4_h(v + 4, b)};
       if (part == 0 && g == 0) gptr(a.w.hs)[(r.ob + row) * scale_row(nI) + r.n] = b.scale;
     }
   }
@@ -708,9 +727,14 @@ __global__ __launch_bounds__(64 * NW) void k_f8_few_down(F8Args a, int NT, int m
   }
 }
 
-// Whether a call takes the kernels for a few tokens: a block's rows have to fit the LDS.
+// Whether a call takes the kernels for a few tokens.  us there and on 64-row tiles (calls
+// among others): d = 4096, I = 688, 16 slots, top-4 (344 blocks to 1376): 1 token 14, 36;
+// 2 19, 38; 4 24, 38; 8 30, 39; 12 46, 39.  d = 2048, I = 1408, 64 slots, top-6: 1 token (1056
+// blocks) 20, 29; 2 (2112) 24, 31; 3 (3168) 33, 32; 6 54, 36.  d = 512, I = 256, 8 slots, top-2
+// (256 blocks): 12 tokens 10, 15; 16 11, 15.  A block's rows have to fit the LDS.
 bool f8_few_tokens(const moe_layer_fp8* L, int T, long active) {
-  return T <= F8_FEW && active * (L->I / 8) <= 2048 && T * f8_few_row_bytes(blocks128(L->d)) <= 56 * 1024 &&
+  const long blocks = active * (L->I / 8);
+  return ((T <= 8 && blocks <= 2560) || (T <= F8_FEW && blocks <= 512)) && T * f8_few_row_bytes(blocks128(L->d)) <= 56 * 1024 &&
          T * f8_few_row_bytes(blocks128(L->I)) <= 52 * 1024;
 }
 
@@ -744,8 +768,11 @@ long f8_active(const moe_layer_fp8* L, int T, int k) {
 int fp8_tile(const moe_layer_fp8* L, int T, int k) {
   const long active = f8_active(L, T, k);
   if (f8_few_tokens(L, T, active)) return 0;
+  // us on 256- and 128-row tiles by rows per slot: d = 2048, I = 1408, 64 slots: 28 rows 144,
+  // 110; 140 219, 196; 187 246, 219; 281 307, 310; 384 361, 373; 768 615, 664.  d = 4096, I =
+  // 688, 16 slots: 128 rows 91, 63; 256 94, 75; 512 119, 133.
   const double r = (double)T * (k + L->S_shared) / active;
-  return r >= 192 ? 256 : 128;
+  return r >= 272 ? 256 : 128;
 }
 
 }  // namespace fm

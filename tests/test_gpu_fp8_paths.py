@@ -1,0 +1,104 @@
+"""The kernels behind moe_grouped_swiglu_fwd_fp8, each at the sizes where it can go wrong: the
+ones for a few tokens, the 128- and 256-row tiles (with their half-height forms) and both
+sides of the rules between them.  A case names the path it is there for and asks the
+library's own rule (fm::fp8_tile), so that a retuned rule does not leave it on another.
+
+Formulas and tolerances as in test_gpu_fp8."""
+import ctypes
+
+import pytest
+
+from paper_2508_19078_amd import api
+
+import test_gpu_fp8 as M
+
+FEW, SMALL, LARGE = 0, 128, 256
+
+
+def path(T, d, E, k, I, sh):
+    f = getattr(api.lib(), "_ZN2fm8fp8_tileEPK13moe_layer_fp8ii")   # fm::fp8_tile(const moe_layer_fp8*, int, int)
+    f.restype, f.argtypes = ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int]
+    L = api.moe_layer_fp8(d, I, E, sh, *[None] * 6)
+    return f(ctypes.addressof(L), T, k)
+
+
+FEW_CASES = {
+    # name: (T, d, E, k, I, shared, experts drawn from)
+    "one_token": (1, 4096, 6, 2, 688, 0, 6),                  # I ends inside a block, k split over idle waves too
+    "two_tokens_on_one_expert": (2, 4096, 2, 1, 272, 0, 1),
+    "ragged_ends_and_empty_slots": (3, 1040, 5, 2, 1040, 1, 3),
+    "many_empty_slots": (3, 1040, 70, 2, 1024, 0, 70),        # the slots' ballot goes round twice
+    "seven_tokens_shared_alone": (7, 2064, 0, 1, 528, 2, 0),
+    "eight_tokens_on_all": (8, 4096, 8, 8, 272, 0, 8),
+    "many_slabs_per_wave": (2, 6160, 2, 2, 2320, 0, 2),       # a second round of requests in both
+    "one_expert": (8, 1040, 1, 1, 1024, 0, 1),
+    "sixteen_tokens": (16, 528, 4, 2, 272, 0, 4),             # more than eight rows in a slot
+    "narrowest": (16, 16, 3, 1, 16, 1, 2),
+}
+# both sides of a limit of the rule
+LIMITS = [
+    ((8, 1040, 3, 1, 2048, 0, 3), FEW), ((9, 1040, 3, 1, 2048, 0, 3), SMALL),          # tokens
+    ((16, 528, 2, 1, 2048, 0, 2), FEW), ((17, 528, 2, 1, 2048, 0, 2), SMALL),
+    ((4, 272, 5, 4, 4096, 0, 5), FEW), ((4, 272, 6, 4, 4096, 0, 6), SMALL),            # slots times I / 8
+    ((16, 272, 8, 2, 512, 0, 8), FEW), ((16, 272, 8, 2, 528, 0, 8), SMALL),
+    ((8, 6912, 2, 1, 128, 1, 2), FEW), ((8, 7168, 2, 1, 128, 1, 2), SMALL),            # rows in LDS
+    ((271, 144, 2, 1, 144, 1, 2), SMALL), ((272, 144, 1, 1, 144, 0, 1), LARGE),        # rows per slot
+]
+SMALL_CASES = {
+    "empty_slots_between": (150, 528, 40, 2, 272, 0, 9),
+    "three_slabs": (200, 384, 3, 2, 384, 1, 3),               # the ring is as long as the product
+    "one_slab": (100, 128, 3, 2, 128, 0, 3),
+    "two_slabs": (100, 144, 3, 2, 160, 0, 3),
+    "four_slabs_and_a_part": (100, 528, 3, 1, 560, 0, 3),     # a second group of scales
+    "columns_end_inside_tiles": (70, 656, 2, 1, 400, 2, 2),
+    "tiles_of_two_rows": (260, 272, 2, 1, 272, 0, 2),
+}
+LARGE_CASES = {
+    "one_slab": (300, 128, 1, 1, 128, 0, 1),
+    "two_slabs": (600, 144, 2, 2, 160, 0, 2),
+    "five_slabs": (600, 640, 2, 1, 640, 0, 1),
+    "nine_slabs_ragged": (530, 1040, 2, 1, 1072, 1, 2),
+    "a_row_more_than_the_half_tile": (385, 272, 1, 1, 272, 0, 1),
+    "the_half_tile": (384, 272, 1, 1, 272, 0, 1),
+    "more_tiles_than_blocks": (4000, 144, 4, 2, 1168, 0, 4),
+}
+
+
+def test_paths():
+    for cases, want in ((FEW_CASES, FEW), (SMALL_CASES, SMALL), (LARGE_CASES, LARGE)):
+        for name, case in cases.items():
+            assert path(*case[:6]) == want, name
+    for case, want in LIMITS:
+        assert path(*case[:6]) == want, case
+
+
+def forward(case):
+    T, d, E, k, I, sh, _ = case
+    X, w, offsets, tok = M.draw(*case)
+    got = M.run(M.tables(w, d, E, k, I, sh), X, offsets, tok, T, k, sh, d)
+    M.check(got, X, w, offsets, tok, T, d, E, k, I, sh)
+    assert bool((got[int(offsets[-1]):T * k] == 7.0).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", list(FEW_CASES))
+def test_few_tokens(name):
+    forward(FEW_CASES[name])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", [c for c, _ in LIMITS], ids=["-".join(map(str, c)) for c, _ in LIMITS])
+def test_both_sides_of_the_rule(case):
+    forward(case)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", list(SMALL_CASES))
+def test_small_tiles(name):
+    forward(SMALL_CASES[name])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", list(LARGE_CASES))
+def test_large_tiles(name):
+    forward(LARGE_CASES[name])
