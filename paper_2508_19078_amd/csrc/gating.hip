@@ -472,7 +472,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_route_scored(Gating g, const flo
 #pragma unroll
     for (int i = 0; i < N; i += 2) win = larger3(win, pk[i], pk[i + 1]);
     win = row_max_u(win);
-    const uint32_t need = BIAS ? (uint32_t)fminf(gap * UNITS, 1e6f) + 4u : 1u;   // (two keys, two units of rounding and one of the cut)
+    // (two keys, two units of rounding and one of the cut; with more than the window nothing is apart)
+    const uint32_t need = BIAS ? (uint32_t)fminf(gap * UNITS, 0x1p25f) + 4u : 1u;
     const int places = g.topk_group * g.size, rounds = min(g.k + 1, places);
     int mine = 0;
     uint32_t kth = 0;

@@ -6,6 +6,8 @@ oracle; inputs that tie do so exactly.  Gates: an exponential and its argument (
 |z| half steps of it), a quotient and two sums of at most 256 terms, half a step of fp32
 each: (48 + 2 max|z|) 2^-24 relative, the gradient the same relative to the sum of the
 magnitudes it is a difference of."""
+import itertools
+
 import numpy as np
 import pytest
 import torch
@@ -143,6 +145,16 @@ def test_keys_that_fp32_cannot_tell_apart(score, bias, spread):
     # without a bias, groups of saturated scores tie in fp64 as in the oracle
     g, idx = check(z, b, 5, how)
     check_backward(g, z, idx, how)
+
+
+def test_bias_whose_steps_are_as_large_as_scores():
+    """Keys in fp32 are whole eighths here, and scores make up for the differences of the
+    biases: their sums lie on both sides of a tie and round apart, either way."""
+    rng = np.random.default_rng(0)
+    for i, j in itertools.combinations(range(8), 2):
+        at = np.array([i, j]) / 8
+        s = 15 / 16 - at + 2.0 ** -25 * rng.uniform(-3, 3, (8192, 2))
+        check(np.log(s / (1 - s)).astype(np.float32), (15938355 / 8 + at).astype(np.float32), 1, dict(score="sigmoid"))
 
 
 @pytest.mark.parametrize("how", [dict(), dict(renorm=False), dict(score="sigmoid"), dict(score="sigmoid", renorm=False),
