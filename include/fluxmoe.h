@@ -689,7 +689,7 @@ size_t moe_grouped_swiglu_fwd_mx4_workspace_size(const moe_layer_mx4* L, int T, 
  * to moe_quantize_fp8's codes (16-byte aligned) and scales (4-byte aligned) of W_gate,
  * W_up [I,d] and W_down [d,I] with block_rows 128 (read on the device only, not
  * checked).  d and I multiples of 16; d * I and T * d, both rounded up to 128 columns,
- * at most 2^32.
+ * at most 2^32, I at most 2^24.
  */
 typedef struct moe_layer_fp8 {
   int d;

@@ -860,6 +860,8 @@ extern "C" int moe_grouped_swiglu_fwd_fp8(const moe_layer_fp8* L, const void* X,
   // byte offsets within a matrix, and of a token's row, are 32 bits wide
   if (128LL * blocks128(L->d) * 128 * blocks128(L->I) > (1LL << 32))
     return fail(MOE_ERR_UNSUPPORTED, "8-bit float layer d=%d I=%d: more than 2^32 weights in a matrix", L->d, L->I);
+  // (and of the 256 rows of H of a tile)
+  if (L->I > 1 << 24) return fail(MOE_ERR_UNSUPPORTED, "8-bit float layer I=%d > 2^24", L->I);
   FM_TRY(need(L->q_gate, "layer q_gate")); FM_TRY(need(L->q_up, "layer q_up")); FM_TRY(need(L->q_down, "layer q_down"));
   FM_TRY(need(L->s_gate, "layer s_gate")); FM_TRY(need(L->s_up, "layer s_up")); FM_TRY(need(L->s_down, "layer s_down"));
   if (T < 0 || k <= 0 || k > 16) return fail(MOE_ERR_ARG, "T=%d k=%d", T, k);

@@ -157,6 +157,7 @@ def fp8(L, layer=(), **over):
     (dict(d=2147483632, I=16), {}, UNS, "2^30"),
     (dict(I=0), {}, ARG, "I=0"),
     (dict(d=1 << 20, I=1 << 13), {}, UNS, "2^32 weights"),
+    (dict(d=16, I=(1 << 24) + 16), {}, UNS, "2^24"),
     (dict(S_routed=513), {}, ARG, "S_routed=513"),
     (dict(S_routed=0, S_shared=0), {}, ARG, "S_routed=0"),
     (dict(s_up=None), {}, ARG, "s_up"),
