@@ -11,11 +11,12 @@ stream.  It is plumbing: every value is computed by libfluxmoe.
   backward() combine backward -> grouped SwiGLU backward -> permute backward
   step()     all of the above in that order: one pass of the whole hot path
 
-With a gating (api.gating), also:
+Apart from the benchmark's step:
 
-  router_backward()  the router's gradients from the gates' (after backward(dgate=True))
-  balance()          the selection bias moved against the step's load
-  clip()             the global norm of the step's gradients, and their clipping (any routing)
+  clip()             the global norm of the step's gradients, and their clipping
+  router_backward()  with a gating (api.gating): the router's gradients from the gates'
+                     (after backward(dgate=True))
+  balance()          with a gating: the selection bias moved against the steps' load
 
 HBM layout.  Expert weights are stacked per matrix ([E, I, d], [E, I, d],
 [E, d, I]); merged groups get their own stacks and shared experts theirs.
@@ -181,6 +182,12 @@ class MoELayerRunner:
         self.ws_bwd = torch.empty(api.moe_grouped_swiglu_bwd_workspace_size(self.layer_tables, T, k),
                                   dtype=torch.uint8, device=device)
 
+        # the step's weight gradients as one set (a frozen layer without a gating has none)
+        grads = [*self.dWg, *self.dWu, *self.dWd] + ([] if gating is None else [self.dWr, self.dbias])
+        self.grads = api.TensorSet(grads or [None], torch.float32, device)
+        self.sumsq, self.norm = z(1, dtype=torch.float64), z(1, dtype=torch.float32)
+        self.ws_norm = torch.empty(api.moe_grad_norm_workspace_size(), dtype=torch.uint8, device=device)
+
     # ------------------------------------------------------------ stages --
     def profile(self, idx8: Optional[torch.Tensor] = None):
         """idx8 [T,k] int32, if given, receives the int8 router's top-k sets."""
@@ -243,12 +250,6 @@ class MoELayerRunner:
     def clip(self, max_norm: float, eps: float = 1e-6):
         """Clips the weight gradients (the router's too, with a gating) in place by their
         global norm, which is returned (a device tensor)."""
-        if not hasattr(self, "grads"):
-            router = () if self.gating is None else (self.dWr, self.dbias)
-            self.grads = api.TensorSet([*self.dWg, *self.dWu, *self.dWd, *router], torch.float32, self.dev)
-            self.sumsq = torch.empty(1, dtype=torch.float64, device=self.dev)
-            self.norm = torch.empty(1, dtype=torch.float32, device=self.dev)
-            self.ws_norm = torch.empty(api.moe_grad_norm_workspace_size(), dtype=torch.uint8, device=self.dev)
         api.moe_grad_norm(self.grads, self.sumsq, self.norm, self.ws_norm)
         api.moe_grad_clip(self.grads, self.sumsq, max_norm, eps=eps)
         return self.norm
