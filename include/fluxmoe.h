@@ -681,7 +681,9 @@ size_t moe_grouped_swiglu_fwd_mx4_workspace_size(const moe_layer_mx4* L, int T, 
  * by the fp32 product of its two scales, and blocks add up in fp32; one rounding.  The
  * matrix unit aligns the products of 8 consecutive k to the largest of them and drops
  * what of the others lies below 2^-13 of it (the rounding of that largest product's own
- * operands to 8 bits weighs 2^-4).  H is quantised from its fp32 values and not written out.  X [T,d] bf16 is quantised once
+ * operands to 8 bits weighs 2^-4), but for gate and up in calls of a few tokens, where no
+ * average over rows hides an element of H that takes the other code for it.  H is
+ * quantised from its fp32 values and not written out.  X [T,d] bf16 is quantised once
  * per token; routed row p reads token perm_token[p] (moe_permute's; values clamped to
  * [0, T)), so X_perm is not needed.  offsets, the row space and O [R_tot, d] bf16 as
  * in moe_grouped_swiglu_fwd; O's rows behind the last routed one are left as they

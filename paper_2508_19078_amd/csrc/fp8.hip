@@ -2,27 +2,39 @@
 // forward on them (the formulas stand in the header at moe_quantize_fp8 and
 // moe_grouped_swiglu_fwd_fp8).
 //
-// The products run on v_mfma_f32_32x32x64_f8f6f4: a lane holds 32 bytes of one row, lane l
-// row l % 32 and the half l / 32 of the step's k.  A slab is 128 k, a whole scale block, so
-// a slab's sum starts at zero and goes into the tile's sums with one multiplication by the
-// scales: a row's (a lane's) times the weight block's (uniform in a wave).  The instruction
-// aligns the products of 8 consecutive k to the largest sum of their operands' exponents
-// and drops what lies below 2^-13 of that, towards zero (measured; its older 16 k form does
-// the same); the eight's sum joins the others and the accumulator with fp32's bits.  H
-// comes out some 1e-4 off for it.  That is the price of the 8-bit rate: the codes widened
-// to bf16, whose products keep all bits, run at half of it, and the codes themselves are
-// 2^-4 off what they stand for.
+// The products run on v_mfma_f32_16x16x128_f8f6f4: a lane holds 32 bytes of one row, lane l
+// of row l % 16.  A slab is 128 k, a whole scale block and one product, so a slab's sum
+// starts at zero and goes into the tile's sums with one multiplication by the scales: a
+// row's (a lane's) times the weight block's (uniform in a wave).  The instruction aligns the
+// products of 8 consecutive k to the largest sum of their operands' exponents and drops what
+// lies below 2^-13 of that, towards zero (measured; its older 16 k form does the same); the
+// eight's sum joins the others and the accumulator with fp32's bits.  H comes out some 1e-4
+// off for it, and one element in 500 or so takes the other code.  That is the price of the
+// 8-bit rate: the codes widened to bf16, whose products keep all bits, run at half of it
+// (128-row tiles of at most 64 rows so: 333 tokens 130 us to 133, 32 tokens 41 to 55).
+// Only calls of a few tokens, which wait for bytes and not for the matrix unit, take gate
+// and up in bf16 (1 token 13.9 us to 14.7): a large element's step is 0.6 % of one token's
+// output there, and 2e-3 is what many rows leave of it.
 //
 // * A slab row is one 128-byte line; slabs go global -> LDS with global_load_lds_dwordx4, 8
-//   rows per instruction, into two buffers; the scales of 4 slabs of a row (16 bytes)
-//   follow through registers.
-// * Weights are the first operand, so a lane's 16 sums of a 32 x 32 tile belong to one
-//   activation row; weight rows are dealt to the operand's rows so that they are 16
-//   consecutive columns (tile_column).  A tile of gate and up has 128 columns of H, a
-//   scale block: its maximum is 15 comparisons, one exchange and an exchange of four
-//   waves through LDS, and H is quantised in registers.
+//   rows per instruction, into a ring of RING slabs, the scales of 4 slabs of a row (16
+//   bytes) the same way into two groups.
+// * Weights are the first operand, so a lane's 4 sums of a 16 x 16 tile belong to one
+//   activation row; weight rows are dealt to the operand's rows so that two tiles of gate or
+//   up give a lane 8 consecutive columns, and 4 of the down product 16.  A tile of gate and
+//   up has 128 columns of H, a scale block: its maximum is 7 comparisons, two exchanges and
+//   an exchange of four waves through LDS, and H is quantised in registers.
 // * X and H in the workspace have rows of whole 128-blocks, zero behind the row's end, so
 //   weight chunks past K (clamped reads) meet zero codes.
+//
+// 262144 rows, d = 4096, I = 1024 (64 slots): gate and up 2.20 ms (2.0 PFLOP/s), down 1.30 ms
+// (1.7, with 2.1 GB of O).  The matrix unit alone, on registers with random codes, does
+// 3.9 PFLOP/s.  A slab of a 256 x 256 tile takes 1.9 us, of which the products alone are
+// 1.2 and the requests alone 1.4 to 1.55; a tile's lookup, first slab and epilogue 9 us.
+// 32x32x64 products gave 2.16 us a slab, three slabs of activations with two of weights 2.11,
+// padding activation rows to odd lines nothing, bands of 4 to 16 row tiles nothing or 4 %
+// more time.  The next tile's first slab requested before the epilogue: 3 % less there, 12 %
+// more at 333 tokens.
 #include <type_traits>
 #include <utility>
 
@@ -138,6 +150,7 @@ __device__ __forceinline__ void quantize_row(const T* row, int cols, int blk, in
   if (q == 0) gptr(scale)[blk] = s;
 }
 
+// 16 lanes per 1 x 128 block.  2.7 us for 2048 x 128 fp32, a launch.
 template <typename T>
 __global__ __launch_bounds__(256) void k_quantize_f8_rows(const T* __restrict__ W, uint32_t items, int cols, int nb,
                                                           uint8_t* __restrict__ codes, float* __restrict__ scale) {
@@ -148,7 +161,9 @@ __global__ __launch_bounds__(256) void k_quantize_f8_rows(const T* __restrict__ 
                scale + (size_t)r * nb);
 }
 
-// A block of 128 x 128: 16 threads to a row, 8 rows each.
+// A block of 128 x 128: 16 threads to a row, 8 rows each, held in registers between the
+// maximum and the codes, so that W is read once.  Bound by HBM: 90112 x 2048 bf16 in 115 to
+// 133 us (4.8 to 4.2 TB/s of 553 MB).
 template <typename T>
 __global__ __launch_bounds__(256) void k_quantize_f8(const T* __restrict__ W, int rows, int cols, int nb,
                                                      uint8_t* __restrict__ codes, float* __restrict__ scale) {
@@ -176,6 +191,7 @@ __global__ __launch_bounds__(256) void k_quantize_f8(const T* __restrict__ W, in
   if (threadIdx.x == 0) gptr(scale)[(size_t)br * nb + bc] = b.scale;
 }
 
+// 8 columns per thread.  Bound by HBM: the same matrix back in 91 us (6.1 TB/s).
 template <typename T>
 __global__ __launch_bounds__(256) void k_dequant_f8(const uint8_t* __restrict__ codes, const float* __restrict__ scale,
                                                     uint32_t items, int cols, int n8, int row_shift, T* __restrict__ out) {
@@ -238,7 +254,8 @@ inline F8Ws f8_ws_at(void* ws, const moe_layer_fp8* L, int T, int k, size_t* byt
   return w;
 }
 
-// X's tokens as packed rows; the last block builds the row-tile prefix instead.
+// X's tokens as packed rows; the last block builds the row-tile prefix instead.  32768 x 4096:
+// 88 us (4.6 TB/s); 333 x 2048: 4.7, the prefix's chain of loads.
 __global__ __launch_bounds__(256) void k_f8_prep(const bf16* __restrict__ X, RowArgs ra, int tile_rows, int nb,
                                                  uint8_t* __restrict__ xq, float* __restrict__ xs,
                                                  int32_t* __restrict__ mbase) {
@@ -562,7 +579,10 @@ typedef F8Cfg<64, 3, 128> E128h;
 // sums meet in LDS.  A wave requests BS slabs of weights straight into registers, and the
 // block quantises its activation rows into LDS while they are on their way.  H goes
 // through the workspace in fp32 and is quantised the same way.  Rows come 16 at a time.
-// Blocks exist for the slots that may hold rows only.
+// Blocks exist for the slots that may hold rows only.  d = 4096, I = 688, one token on 4
+// slots: 11.8 us gate and up (22.5 MB), 4.6 down (11.3 MB), each a chain of slot, pointers,
+// rows and their sums; 8 waves per block in place of 4: 13 us a call here for 14, 27 for 24 with
+// two tokens of d = 2048, I = 1408.
 
 // Rows of nb 128-blocks in LDS: codes, then scales; padded so that 16 rows' chunks at one
 // place lie on different banks.
@@ -588,10 +608,27 @@ __device__ __forceinline__ void f8_few_stage(const F8FewRows& l, int n, int nb, 
   }
 }
 
+// Codes widened to bf16, which holds every one of them.
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ bf16x8_t f8_widen(int lo, int hi) {
+  const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
+  const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
+  return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+// A slab's sums of 16 x 16, by 8-bit products, or WIDE by bf16 ones, which drop nothing.
+template <bool WIDE> __device__ __forceinline__ f32x4_t f8_slab(const i32x8_t& w, const i32x8_t& x) {
+  f32x4_t p = {0.f, 0.f, 0.f, 0.f};
+  if constexpr (!WIDE) return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, p, 0, 0, 0, 0, 0, 0);
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f8_widen(w[j], w[j + 1]), f8_widen(x[j], x[j + 1]), p, 0, 0, 0);
+  return p;
+}
+
 // Sums over this wave's slabs [k0, k1): NF fragments of 16 weight rows (codes at w[f], of
 // this lane's row; scale(f, k): the scale of the rows this lane has sums of) by the 16
 // activation rows that stage() puts into LDS (n of them are there).
-template <int NF, int BS, typename Scale, typename Stage>
+template <bool WIDE, int NF, int BS, typename Scale, typename Stage>
 __device__ __forceinline__ void f8_few_sums(const uint8_t* const (&w)[NF], int kw, Scale scale, const F8FewRows& l, int n, int k0,
                                             int k1, Stage stage, f32x4_t (&acc)[NF]) {
   const int kb = lane_id() >> 4, r = min(lane_id() & 15, n - 1);
@@ -626,8 +663,7 @@ __device__ __forceinline__ void f8_few_sums(const uint8_t* const (&w)[NF], int k
       };
 #pragma unroll
       for (int f = 0; f < NF; ++f) {
-        const f32x4_t p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(both(wc[u][f][0], wc[u][f][1]), both(x0, x1),
-                                                                           f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+        const f32x4_t p = f8_slab<WIDE>(both(wc[u][f][0], wc[u][f][1]), both(x0, x1));
         const float s = sx * ws[u][f];
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[f][e] = fmaf(p[e], s, acc[f][e]);
@@ -673,7 +709,7 @@ __global__ __launch_bounds__(64 * NW) void k_f8_few_gate_up(F8Args a, const bf16
   for (int m0 = 0; m0 < sr.nrows; m0 += max_rows) {
     const int n = min(max_rows, sr.nrows - m0);
     f32x4_t acc[1] = {{0.f, 0.f, 0.f, 0.f}};
-    f8_few_sums<1, BS>(w, ra.d / 16, [&](int, int k) { return gptr(s)[k]; }, l, n, k0, k1, [&] {
+    f8_few_sums<true, 1, BS>(w, ra.d / 16, [&](int, int k) { return gptr(s)[k]; }, l, n, k0, k1, [&] {
       f8_few_stage<64 * NW>(l, n, nd, ra.d, [&](int r) {
         const size_t tok = sr.shared ? m0 + r : min(max(gptr(a.perm_token)[sr.xrow0 + m0 + r], 0), ra.Tn - 1);
         return X + tok * ra.d;
@@ -710,7 +746,7 @@ __global__ __launch_bounds__(64 * NW) void k_f8_few_down(F8Args a, int NT, int m
     const int n = min(max_rows, sr.nrows - m0);
     const size_t row0 = (size_t)(sr.orow0 + m0);
     f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-    f8_few_sums<2, BS>(w, ra.I / 16, [&](int, int k) { return gptr(s)[k]; }, l, n, k0, k1, [&] {
+    f8_few_sums<false, 2, BS>(w, ra.I / 16, [&](int, int k) { return gptr(s)[k]; }, l, n, k0, k1, [&] {
       f8_few_stage<64 * NW>(l, n, nI, ra.I, [&](int r) { return (const float*)a.w.hf + (row0 + r) * ra.I; });
     }, acc);
 #pragma unroll
@@ -727,11 +763,12 @@ __global__ __launch_bounds__(64 * NW) void k_f8_few_down(F8Args a, int NT, int m
   }
 }
 
-// Whether a call takes the kernels for a few tokens.  us there and on 64-row tiles (calls
-// among others): d = 4096, I = 688, 16 slots, top-4 (344 blocks to 1376): 1 token 14, 36;
-// 2 19, 38; 4 24, 38; 8 30, 39; 12 46, 39.  d = 2048, I = 1408, 64 slots, top-6: 1 token (1056
-// blocks) 20, 29; 2 (2112) 24, 31; 3 (3168) 33, 32; 6 54, 36.  d = 512, I = 256, 8 slots, top-2
-// (256 blocks): 12 tokens 10, 15; 16 11, 15.  A block's rows have to fit the LDS.
+// Whether a call takes the kernels for a few tokens.  us there and on tiles (calls among
+// others): d = 4096, I = 688, 16 slots, top-4 (344 blocks to 1376): 1 token 14.6, 37.0; 2 19.7,
+// 38.0; 4 25.3, 38.5; 8 35.5, 39.2; 10 38.3, 39.4; 12 45.3, 39.6.  d = 2048, I = 1408, 64 slots,
+// top-6: 1 token (1056 blocks) 19.7, 29.9; 2 (2112) 27.5, 30.3; 3 (3168) 33.2, 31.2; 6 48.8, 36.4.
+// d = 512, I = 256, 8 slots, top-2 (256 blocks at most): 1 to 16 tokens 10, 15.  A block's rows
+// have to fit the LDS.
 bool f8_few_tokens(const moe_layer_fp8* L, int T, long active) {
   const long blocks = active * (L->I / 8);
   return ((T <= 8 && blocks <= 2560) || (T <= F8_FEW && blocks <= 512)) && T * f8_few_row_bytes(blocks128(L->d)) <= 56 * 1024 &&

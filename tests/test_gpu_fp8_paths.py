@@ -6,7 +6,10 @@ library's own rule (fm::fp8_tile), so that a retuned rule does not leave it on a
 Formulas and tolerances as in test_gpu_fp8."""
 import ctypes
 
+import numpy as np
+import oracle as O
 import pytest
+import torch
 
 from paper_2508_19078_amd import api
 
@@ -84,6 +87,28 @@ def forward(case):
 @pytest.mark.parametrize("name", list(FEW_CASES))
 def test_few_tokens(name):
     forward(FEW_CASES[name])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 8])
+def test_few_tokens_drop_nothing_of_gate_and_up(T):
+    """Large products that cancel, from different groups of 8, and small ones that 8-bit
+    products would drop beside them: what is left decides H.  All codes are exact; the
+    output is off by its rounding to bf16 and by what tells H's codes in fp32 from those
+    in 64 bits, a step at most."""
+    d, I = 128, 16
+    assert path(T, d, 2, 1, I, 0) == FEW
+    X = torch.zeros(T, d)
+    X[:, :16] = 2.0 ** -6
+    X[:, 0] = X[:, 8] = 448
+    W = torch.ones(2, I, d)
+    W[:, :, 8] = -1
+    w = dict(g=W.to(M.BF), u=W.to(M.BF), d=torch.ones(2, d, I, dtype=M.BF))
+    offsets, tok = np.array([0, 0, T]), np.arange(T)
+    got = M.run(M.tables(w, d, 2, 1, I, 0), X.to(M.BF), offsets, tok, T, 1, 0, d).double().cpu().numpy()
+    H, want = O.swiglu_fp8_fwd(X.double().numpy(), *(w[m][1].double().numpy() for m in "gud"))
+    assert abs(H[0, 0] - 0.21875 ** 2 / (1 + np.exp(-0.21875))) < 1e-12
+    assert np.all(np.abs(got - want) <= 2.0 ** -8 * want)
 
 
 @pytest.mark.gpu
