@@ -89,6 +89,22 @@ def test_fp8_blocks():
     assert s[0, 0] == 2.0 ** -126 and not v.any()
 
 
+def test_fp8_forward():
+    """Activations that are codes times a power of two pass as they are; H is quantised
+    between the products, and where its rows are codes too the output is torch's."""
+    rng = np.random.default_rng(2)
+    x = rng.choice([448.0, 0.5, -3.0, 0.0, 26.0], (5, 160))
+    x[:, 0] = x[:, 128] = 448
+    Wg, Wu, Wd = rng.standard_normal((130, 160)) / 500, rng.standard_normal((130, 160)) / 500, rng.standard_normal((160, 130))
+    H, out = O.swiglu_fp8_fwd(x, Wg, Wu, Wd)
+    t = torch.tensor(x)
+    np.testing.assert_allclose(H, torch.nn.functional.silu(t @ torch.tensor(Wg).T) * (t @ torch.tensor(Wu).T), rtol=1e-10, atol=1e-13)
+    np.testing.assert_array_equal(out, O.fp8_round(H) @ Wd.T)
+    big = np.abs(H).max() * 1e3                          # one gate saturates, and up makes H a code
+    Hs, out = O.swiglu_fp8_fwd(np.array([[448.0] + [0.0] * 127]), np.full((1, 128), big), np.full((1, 128), 2.0), Wd[:, :1])
+    np.testing.assert_allclose(out, Hs * Wd[:, 0], rtol=1e-7)
+
+
 def test_clip_by_hand():
     assert O.grad_sumsq([np.array([3.0]), None, np.array([[4.0]])]) == 25
     assert O.clip_coefficient(25.0, 1.0, 0.0) == 0.2 and O.clip_coefficient(25.0, 6.0) == 1.0
