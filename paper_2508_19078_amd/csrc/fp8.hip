@@ -27,14 +27,16 @@
 // * X and H in the workspace have rows of whole 128-blocks, zero behind the row's end, so
 //   weight chunks past K (clamped reads) meet zero codes.
 //
-// 262144 rows, d = 4096, I = 1024 (64 slots): gate and up 2.20 ms (2.0 PFLOP/s), down 1.30 ms
+// 262144 rows, d = 4096, I = 1024 (64 slots): gate and up 2.15 ms (2.0 PFLOP/s), down 1.30 ms
 // (1.7, with 2.1 GB of O).  The matrix unit alone, on registers with random codes, does
 // 3.9 PFLOP/s.  A slab of a 256 x 256 tile takes 1.9 us, of which the products alone are
 // 1.2 and the requests alone 1.4 to 1.55; a tile's lookup, first slab and epilogue 9 us.
-// 32x32x64 products gave 2.16 us a slab, three slabs of activations with two of weights 2.11,
-// padding activation rows to odd lines nothing, bands of 4 to 16 row tiles nothing or 4 %
-// more time.  The next tile's first slab requested before the epilogue: 3 % less there, 12 %
-// more at 333 tokens.
+// It is bound by power as much as by waiting: the clock falls to 1.9 GHz, and with all codes
+// zero the same call takes 11 % less; with all blocks on the same rows and weights (L2 only)
+// 5 % less.  32x32x64 products gave 2.16 us a slab, three slabs of activations with two of
+// weights 2.11, padding activation rows to odd lines nothing, bands of 4 to 16 row tiles
+// nothing or 4 % more time, wave priorities nothing.  The next tile's first slab requested
+// before the epilogue: 3 % less there, 12 % more at 333 tokens.
 #include <type_traits>
 #include <utility>
 
@@ -272,16 +274,22 @@ __global__ __launch_bounds__(256) void k_f8_prep(const bf16* __restrict__ X, Row
 
 // RA activation rows x RB weight rows by 2 x 4 waves, one block per compute unit.  LDS: rings
 // of RING slabs of activations (the place of BIG rows, the larger tile's that shares the
-// kernel) and of weights, then two groups of scales [BIG rows][16 bytes].
+// kernel) and of weights, then two groups of scales [BIG rows][16 bytes], then
+// the waves' weight scales.
 template <int RA_, int RING_, int BIG> struct F8Cfg {
   static constexpr int RA = RA_, RB = 256, NW = 8, BPC = 1, RING = RING_;
   static constexpr int TM = RA / 2, TN = RB / 4, MI = TM / 16, NJ = TN / 16;
   static constexpr int A_BYTES = RA * 128, B_BYTES = RB * 128, B_BASE = RING * BIG * 128;   // 128 k
   static constexpr int A_INS = RA / 8 / NW, B_INS = RB / 8 / NW;        // 8 rows each, per wave
+  // Requests of gate and up one by one between the first products, not all at a slab's start,
+  // where the first fragments wait for their turn: 2.26 ms to 2.15 of the layer above.  The
+  // down product took 1.35 ms so for 1.31 (its 8 slabs come from HBM), small tiles 2 to 4 % more.
+  static constexpr bool SPREAD = RA == 256;
+  static_assert(!SPREAD || 2 * (A_INS + B_INS) <= MI * NJ, "places between products");
   static constexpr int AHEAD = RING == 3 ? A_INS + B_INS : 0;           // requests of slab kt + 1 that may be under way at kt
   static constexpr int LAST = B_BASE + (RING - 1) * B_BYTES;            // the last weight slab's place, free until a tile's first barrier
   static constexpr int SCALES = B_BASE + RING * B_BYTES, GROUP = BIG * 16;
-  static constexpr int LDS = SCALES + 2 * GROUP;
+  static constexpr int WEIGHT_SCALES = SCALES + 2 * GROUP, LDS = WEIGHT_SCALES + NW * 512;   // per wave [2][64 slabs]
   static_assert(RA % 64 == 0 && RA <= BIG && RA <= 64 * NW && NJ == 4 && (RING == 2 || RING == 3), "tile");
   static_assert(LDS <= 160 * 1024 && NW * 2048 <= B_BYTES, "LDS");
 };
@@ -292,6 +300,41 @@ template <int RA_, int RING_, int BIG> struct F8Cfg {
 __device__ __forceinline__ int f8_swz_a(int r) { return (r >> 1) & 7; }
 template <bool PAIR> __device__ __forceinline__ int f8_swz_b(int r) {
   return ((r >> 1) & 1) | ((PAIR ? r >> 3 : r >> 4) & 3) << 1;
+}
+
+// 4 bytes per lane, as dma16s.
+__device__ __forceinline__ void dma4s(const void* base, uint32_t off, FM_LDS void* l) {
+  base = uniform_ptr(base);
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %3\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dword %1, %2\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(off), "s"(base), "s"((uint32_t)(uintptr_t)l)
+      : "memory");
+}
+
+// dma16s of the lanes in a mask (without a branch, which would end the schedule around it).
+__device__ __forceinline__ void dma16m(const void* base, uint32_t off, FM_LDS void* l, uint32_t lanes) {
+  base = uniform_ptr(base);
+  uint32_t saved;
+  uint64_t all;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b64 %1, exec\n\t"
+      "s_mov_b32 exec_lo, %5\n\t"
+      "s_mov_b32 exec_hi, %5\n\t"
+      "s_mov_b32 m0, %4\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %2, %3\n\t"
+      "s_mov_b32 m0, %0\n\t"
+      "s_mov_b64 exec, %1"
+      : "=&s"(saved), "=&s"(all)
+      : "v"(off), "s"(base), "s"((uint32_t)(uintptr_t)l), "s"(__builtin_amdgcn_readfirstlane(lanes))
+      : "memory");
 }
 
 // One operand pair of a tile, rows relative to it.  w2: the second of two matrices
@@ -339,22 +382,30 @@ __device__ __forceinline__ void f8_gemm(const F8Tile& t, FM_LDS char* lds, f32x4
     const int r = 8 * (wave * C::B_INS + u) + (lane >> 3);
     ob[u] = (uint32_t)min(PAIR ? 32 * (r >> 6) + (r & 31) : r, t.wrows - 1) * ldw + 16 * ((lane & 7) ^ f8_swz_b<PAIR>(r));
   }
-  // behind a row's end, weights repeat their row's last chunk (it meets zeros)
+  // request u of a slab's (rows of activations, then of weights), for slabs of whole rows
+  constexpr int PIECES = C::A_INS + C::B_INS;
+  auto request = [&](int u, int slab, int place, uint32_t lanes) __attribute__((always_inline)) {
+    if (u < C::A_INS) {
+      dma16m(t.x + (size_t)slab * 128, oa[u], lds + place * C::A_BYTES + (wave * C::A_INS + u) * 1024, lanes);
+    } else {
+      const int b = u - C::A_INS, ins = wave * C::B_INS + b;
+      dma16m((PAIR && ((ins >> 2) & 1) ? t.w2 : t.w) + (size_t)slab * 128, ob[b], lds + C::B_BASE + place * C::B_BYTES + ins * 1024, lanes);
+    }
+  };
+  // a slab at once; behind a row's end, weights repeat their row's last chunk (it meets zeros)
   auto issue = [&](int slab, int place) {
-    FM_LDS char* const la = lds + place * C::A_BYTES;
-    FM_LDS char* const lb = lds + C::B_BASE + place * C::B_BYTES;
 #pragma unroll
-    for (int u = 0; u < C::A_INS; ++u) dma16s(t.x + (size_t)slab * 128, oa[u], la + (wave * C::A_INS + u) * 1024);
+    for (int u = 0; u < C::A_INS; ++u)
+      dma16s(t.x + (size_t)slab * 128, oa[u], lds + place * C::A_BYTES + (wave * C::A_INS + u) * 1024);
 #pragma unroll
-    for (int u = 0; u < C::B_INS; ++u) {
-      const int ins = wave * C::B_INS + u;
-      const uint8_t* const w = (PAIR && ((ins >> 2) & 1) ? t.w2 : t.w) + (size_t)slab * 128;
-      uint32_t at = ob[u];
+    for (int b = 0; b < C::B_INS; ++b) {
+      const int ins = wave * C::B_INS + b;
+      uint32_t at = ob[b];
       if (8 * slab + 8 > t.kw) {
         const int k = (lane & 7) ^ f8_swz_b<PAIR>(8 * ins + (lane >> 3));
         at += 16 * (min(k, t.kw - 1 - 8 * slab) - k);
       }
-      dma16s(w, at, lb + ins * 1024);
+      dma16s((PAIR && ((ins >> 2) & 1) ? t.w2 : t.w) + (size_t)slab * 128, at, lds + C::B_BASE + place * C::B_BYTES + ins * 1024);
     }
   };
   const bool keeper = 64 * wave < C::RA;
@@ -374,23 +425,36 @@ __device__ __forceinline__ void f8_gemm(const F8Tile& t, FM_LDS char* lds, f32x4
 #pragma unroll
     for (int j = 0; j < C::NJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
+  // weight scales of 64 slabs, by way of LDS as well: scalar loads return out of order and
+  // share a counter with LDS reads, so they would make every wait for a fragment one for all
+  FM_LDS char* const lw = lds + C::WEIGHT_SCALES + wave * 512;
+  auto weight_scales = [&](int kt) {
+    const uint32_t at = 4 * min(kt + lane, nk - 1);
+    dma4s(t.s[0], at, lw);
+    if (PAIR) dma4s(t.s[1], at, lw + 256);
+  };
+  weight_scales(0);
   issue_scales(0);
   issue(0, 0);
   if (C::RING == 3 && nk > 1) issue(1, 1);
-  float w0 = ld_scalar(t.s[0]), w1 = PAIR ? ld_scalar(t.s[1]) : 0.f;
   const FM_LDS char* const sc = lds + C::SCALES + (row0 + o) * 16;
   int place = 0;   // of slab kt
 #pragma nounroll
   for (int kt = 0; kt < nk; ++kt) {
-    if (kt + 1 < nk) wait_vmcnt<C::AHEAD>();
-    else wait_vmcnt<0>();
+    if (kt > 0 && kt % 64 == 0) {
+      weight_scales(kt);
+      wait_vmcnt<0>();
+    } else if (kt + 1 < nk) {
+      wait_vmcnt<C::AHEAD>();
+    } else {
+      wait_vmcnt<0>();
+    }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if ((kt & 3) == 2 && kt + 2 < nk) issue_scales((kt >> 2) + 1);
-    if (kt + C::RING - 1 < nk) issue(kt + C::RING - 1, place == 0 ? C::RING - 1 : place - 1);   // where slab kt - 1 was
-    const float sw[2] = {w0, w1};
-    const int kn = min(kt + 1, nk - 1);
-    w0 = ld_scalar(t.s[0] + kn);
-    if (PAIR) w1 = ld_scalar(t.s[1] + kn);
+    const int next = kt + C::RING - 1, free = place == 0 ? C::RING - 1 : place - 1;   // where slab kt - 1 was
+    const bool later = C::SPREAD && PAIR && 8 * next + 8 <= t.kw;
+    const uint32_t more = __builtin_amdgcn_readfirstlane(next < nk && later ? ~0u : 0u);
+    if (next < nk && !later) issue(next, free);
     const uint32_t aa = fa + place * C::A_BYTES, ab = fb + C::B_BASE + place * C::B_BYTES;
     const FM_LDS char* const s = sc + ((kt >> 2) & 1) * C::GROUP + 4 * (kt & 3);
     auto frag = [](uint32_t at, int off) {
@@ -405,15 +469,21 @@ __device__ __forceinline__ void f8_gemm(const F8Tile& t, FM_LDS char* lds, f32x4
     xa[0] = frag(aa, 0);
     sched_fence();
 #pragma unroll
-    for (int j = 1; j < C::NJ; ++j) xb[j] = frag(ab, b_off(j));
+    for (int j = 1; j < C::NJ; ++j) {
+      xb[j] = frag(ab, b_off(j));
+      sched_fence();
+    }
 #pragma unroll
     for (int i = 0; i < C::MI; ++i) sx[i] = *(const FM_LDS float*)(s + 256 * i);
+    const FM_LDS float* const wk = (const FM_LDS float*)lw + (kt & 63);
+    const float sw[2] = {wk[0], PAIR ? wk[64] : 0.f};
     sched_fence();
     constexpr int N = C::MI * C::NJ, D = 2;   // D: products between one and its sums
     f32x4_t p[4];
     float f[2];
     auto step = [&](auto n_) {
       constexpr int n = decltype(n_)::value, i = n / C::NJ, j = n % C::NJ;
+      if constexpr (C::SPREAD && PAIR && n % 2 == 0 && n / 2 < PIECES) request(n / 2, next, free, more);
       if constexpr (n < N) {
         if constexpr (j == 0 && i + 1 < C::MI) xa[(i + 1) & 1] = frag(aa, 2048 * (i + 1));
         p[n & 3] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(xb[j], xa[i & 1], f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);

@@ -55,6 +55,8 @@ SMALL_CASES = {
     "four_slabs_and_a_part": (100, 528, 3, 1, 560, 0, 3),     # a second group of scales
     "columns_end_inside_tiles": (70, 656, 2, 1, 400, 2, 2),
     "tiles_of_two_rows": (260, 272, 2, 1, 272, 0, 2),
+    "gate_and_up_of_66_slabs": (20, 8336, 2, 1, 144, 0, 2),   # a second group of weight scales
+    "down_of_66_slabs": (20, 144, 2, 1, 8336, 0, 2),
 }
 LARGE_CASES = {
     "one_slab": (300, 128, 1, 1, 128, 0, 1),
@@ -63,6 +65,7 @@ LARGE_CASES = {
     "nine_slabs_ragged": (530, 1040, 2, 1, 1072, 1, 2),
     "a_row_more_than_the_half_tile": (385, 272, 1, 1, 272, 0, 1),
     "the_half_tile": (384, 272, 1, 1, 272, 0, 1),
+    "gate_and_up_of_66_slabs": (290, 8336, 1, 1, 144, 0, 1),
     "more_tiles_than_blocks": (4000, 144, 4, 2, 1168, 0, 4),
 }
 
