@@ -28,7 +28,7 @@ def runner(name, **over):
 
 
 def rel(a, b):
-    return float((a.double() - b).norm() / b.norm())
+    return float(((a.double() - b).norm() / b.norm()).detach())
 
 
 @pytest.mark.parametrize("name", list(GATINGS))
