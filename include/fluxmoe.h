@@ -803,7 +803,8 @@ int moe_permute_bwd(const moe_layer* L, const void* dX_perm, const int32_t* inv,
  * moe_grouped_swiglu_bwd, moe_router_bwd and moe_sublayer_norm_bwd left (fp32).
  * data[i] points to start[i+1] - start[i] dense elements, aligned to their size (read
  * on the device only, not checked), or is NULL: a frozen tensor, which takes no part.
- * start[0] = 0, start does not decrease, start[n] = total.
+ * start[0] = 0, start does not decrease, start[n] = total.  Tensors of a set do not
+ * share memory.
  */
 typedef struct moe_tensor_set {
   int n;                    /* tensors, 1 to 2^20 */

@@ -721,7 +721,7 @@ def moe_grad_clip(grads, sumsq, max_norm, out=None, eps=1e-6, stream=None):
 
 class TensorSet:
     """Device tables of a list of tensors (None: frozen, left out) and the moe_tensor_set
-    struct.  The tensors are dense, of one dtype, on one GPU; they are kept, as the
+    struct.  The tensors are dense, of one dtype, on one GPU, apart in memory; they are kept, as the
     library reads their addresses on the device.  dtype: needed where all are None."""
 
     def __init__(self, tensors: Sequence[Optional[torch.Tensor]], dtype: Optional[torch.dtype] = None, device=None):
@@ -738,6 +738,11 @@ class TensorSet:
             ptr(t, dtype)
             if t.device != dev:
                 raise ValueError(f"tensors[{i}] is on {t.device}, the set is on {dev}")
+        # a tensor named twice, or a view of another, would be counted and clipped twice
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.nbytes, i) for i, t in enumerate(self.tensors) if t is not None and t.numel())
+        for (_, end, i), (begin, _, j) in zip(spans, spans[1:]):
+            if begin < end:
+                raise ValueError(f"tensors[{i}] and tensors[{j}] share memory")
         self.sizes = [0 if t is None else t.numel() for t in self.tensors]
         start = [0]
         for n in self.sizes:

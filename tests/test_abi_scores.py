@@ -276,6 +276,11 @@ def test_binding_refuses_tensors_it_would_misread():
     with pytest.raises(ValueError, match="aligned"):
         q, s = [t(32, 64, dt=U8).view(-1)[4:][:1024].view(16, 64)], [t(1, 1)]
         api.LayerTablesFP8(64, 16, 1, 0, q, q, [t(64, 16, dt=U8)], s, s, s)
+    x = t(12)
+    for shared in ([x, t(4), x], [x[8:], None, x[:9]], [x, x[4:5]]):
+        with pytest.raises(ValueError, match="share memory"):
+            api.TensorSet(shared)
+    assert api.TensorSet([x[8:], x[:0], x[:8], x[12:]]).sizes == [4, 0, 8, 0]
     a = api.TensorSet([t(4), None, t(3, 5)])
     with pytest.raises(TypeError, match="bfloat16"):
         api.TensorSet([t(4), t(4, dt=torch.bfloat16)])
