@@ -36,7 +36,7 @@
 // 5 % less.  32x32x64 products gave 2.16 us a slab, three slabs of activations with two of
 // weights 2.11, padding activation rows to odd lines nothing, bands of 4 to 16 row tiles
 // nothing or 4 % more time, wave priorities nothing.  The next tile's first slab requested
-// before the epilogue: 3 % less there, 12 % more at 333 tokens.
+// before the epilogue, with the slots' tables in LDS: 1 to 6 % more.
 #include <type_traits>
 #include <utility>
 
@@ -361,7 +361,7 @@ template <typename F, int... N> __device__ __forceinline__ void f8_steps(F f, st
 // slab kt - 1, whose places then take slab kt + RING - 1.  Scales of group g (slabs 4 g to
 // 4 g + 3), 16 bytes of a row, are requested at slab 4 g - 2 by the waves that 64 rows each
 // give work.  Sums of a 16 x 16 tile are taken two products after it was issued, so that
-// neither waits for the other.
+// neither waits for the other (one product: 4 % more time; three: the same).
 template <class C, bool PAIR>
 __device__ __forceinline__ void f8_gemm(const F8Tile& t, FM_LDS char* lds, f32x4_t (&acc)[C::MI][C::NJ]) {
   const int lane = lane_id(), wave = wave_id();
