@@ -875,9 +875,10 @@ long f8_active(const moe_layer_fp8* L, int T, int k) {
 int fp8_tile(const moe_layer_fp8* L, int T, int k) {
   const long active = f8_active(L, T, k);
   if (f8_few_tokens(L, T, active)) return 0;
-  // us on 256- and 128-row tiles by rows per slot: d = 2048, I = 1408, 64 slots: 28 rows 144,
-  // 110; 140 219, 196; 187 246, 219; 281 307, 310; 384 361, 373; 768 615, 664.  d = 4096, I =
-  // 688, 16 slots: 128 rows 91, 63; 256 94, 75; 512 119, 133.
+  // us on 256- and 128-row tiles by rows per slot: d = 2048, I = 1408, 64 slots: 140 rows 213,
+  // 191; 187 232, 225; 234 262, 249; 272 276, 279; 300 291, 299; 384 342, 357; 512 417, 444.
+  // d = 4096, I = 688, 16 slots: 128 rows 87, 65; 256 93, 78; 272 93, 80; 320 96, 113.  d = 4096,
+  // I = 1024, 64 slots: 128 rows 284, 258; 192 312, 307; 256 369, 375; 300 399, 406; 512 580, 623.
   const double r = (double)T * (k + L->S_shared) / active;
   return r >= 272 ? 256 : 128;
 }
