@@ -9,7 +9,7 @@
 // bits: a key's distance from the bottom of a window below the largest, in 24 bits, then
 // 255 - expert, so that one unsigned maximum finds a round's winner and its index, and the
 // next round's is the largest of the differences to it that wrap.  The map to 24 bits does
-// not decrease, so where neighbours in rank order (the first one left out among them)
+// not decrease (it is held to them at both ends), so where neighbours in rank order (the first one left out among them)
 // differ by more than the fp32 keys' error, and the worst group kept and the best one not
 // do, the selection is the exact one.  Elsewhere fp64 decides, on as few keys as it takes (a
 // kernel of 32768 tokens always meets some such, and waits for its slowest wave): the
@@ -462,14 +462,16 @@ __global__ __launch_bounds__(64 * WAVES) void k_route_scored(Gating g, const flo
       if (__any(near != 0)) left = near_groups<BIAS, N>(g, s, zr, sel_bias, near, rows[tok]);
     }
     if (!(fabsf(top) < __builtin_inff())) sure = false;
-    // packed keys: 1 + the distance from the window's bottom, then 255 - expert; 0: cannot be chosen
+    // packed keys: 1 + the distance from the window's bottom, then 255 - expert; 0: cannot be
+    // chosen.  (The bottom may be rounded down, by more than the window far from zero: the
+    // distance is held to 24 bits, and keys that meet at the end of them are not apart.)
     constexpr float UNITS = 0xFFFFFE.0p0f / WINDOW;
     const float bottom = top - WINDOW;
     uint32_t pk[N];
     const uint32_t base = 256 + 255 - 4 * q;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float d = __builtin_fmaxf(((BIAS ? s[i] : z[i]) - bottom) * UNITS, 0.f);
+      const float d = __builtin_amdgcn_fmed3f(((BIAS ? s[i] : z[i]) - bottom) * UNITS, 0.f, 0xFFFFFE.0p0f);
       const uint32_t v = ((uint32_t)d << 8) + (base - expert_at(i, 0));
       pk[i] = expert_at(i, q) < g.E && (left >> i & 1) ? v : 0u;
     }

@@ -320,3 +320,52 @@ def test_two_graphs_and_another_stream():
                 torch.cuda.synchronize()
                 for n, v in zip(names, w):
                     assert torch.equal(s[n], v), n
+
+
+SHIFTS = [-1e9, -3e7, -1000, -230, -120, -100, -60, -40, -33, -20, 20, 33, 40, 60, 100, 230, 1000, 3e7]
+SHIFTED = {
+    # name: (T, E, k, gating)
+    "64_experts": (300, 64, 6, dict()),
+    "odd_experts_plain": (90, 37, 3, dict(renorm=False)),
+    "groups_of_two_best": (130, 160, 6, dict(n_group=8, topk_group=3, group_top=2)),
+    "sigmoid_groups": (130, 128, 6, dict(score="sigmoid", n_group=8, topk_group=3)),
+    "sigmoid_256_experts": (130, 256, 8, dict(score="sigmoid")),
+    "many_tokens": (3000, 64, 6, dict()),
+}
+
+
+@pytest.mark.parametrize("name", list(SHIFTED))
+@pytest.mark.parametrize("shift", SHIFTS)
+def test_logits_far_from_zero(shift, name):
+    """A softmax does not see a shift of its logits, and a window below the largest of them
+    ends at a number that fp32 may have to round, to either side."""
+    T, E, k, how = SHIFTED[name]
+    z, _ = draw(T, E, False, 3)
+    z = (z + np.float32(shift)).astype(np.float32)
+    g, idx = check(z, None, k, how)
+    check_backward(g, z, idx, how)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_logits_around_every_power_of_two(score):
+    """Rows whose largest logit lies a few steps of fp32 to either side of a power of two, of
+    either sign, or 32 above it; the others lie steps, ones and more than 32 below."""
+    rng = np.random.default_rng(4)
+    z = []
+    for e in range(-20, 127):
+        for base in (2.0 ** e, -2.0 ** e, 32 + 2.0 ** e, 32 - 2.0 ** e):
+            for n in (-9, -1, 0, 1, 2, 40):
+                top = np.float32(base)
+                top = np.float32(top + n * np.spacing(np.abs(top)))
+                below = np.concatenate((np.spacing(np.abs(top)) * np.arange(6), 2.0 ** rng.uniform(-18, 0, 6), np.arange(1, 13),
+                                        32 + 2.0 ** rng.uniform(-20, 3, 8)))
+                z.append(top - rng.permutation(below).astype(np.float32))
+    check(np.stack(z).astype(np.float32), None, 4, dict(score=score, renorm=score == "softmax"))
+
+
+@pytest.mark.parametrize("shift", [-1e6, -100, -15, -7.5, -5, -3.8, -3, -2, 2, 3, 3.8, 7.5, 100, 1e6])
+@pytest.mark.parametrize("T,E,k,how", [(300, 64, 6, dict(score="sigmoid")), (130, 256, 8, dict(score="sigmoid", n_group=8, topk_group=4, group_top=2)),
+                                       (130, 60, 5, dict(n_group=5, topk_group=2)), (130, 128, 4, dict(renorm=False))])
+def test_biases_far_from_zero(T, E, k, how, shift):
+    z, b = draw(T, E, True, 5)
+    check(z, (b + np.float32(shift)).astype(np.float32), k, how)
