@@ -140,21 +140,34 @@ template <int CTRL> __device__ __forceinline__ void merge_two(float& h, float& l
   h = larger(h, h2);
 }
 
+// Between what a group's rank r in fp32, of its largest key h and its second l (if two
+// count), lies in fp64.  A key is off by its score's error err and half a step of its own, which a
+// bias can make far larger than the largest key's; the sum by half a step.  Steps count
+// twice here, which covers the roundings of the bounds.  A rank that fp32 cannot hold is
+// beyond all that it can; infinite keys are exact.
+__device__ __forceinline__ void rank_bounds(float h, float l, float r, bool two, float err, float& lo, float& hi) {
+  const float inf = __builtin_inff();
+  const float e = two ? 2 * err + 0x1p-23f * (fabsf(h) + fabsf(l) + fabsf(r)) : err + 0x1p-23f * fabsf(h);
+  const bool fits = fabsf(r) < inf, over = two && l > -inf;
+  lo = fits ? r - e : over && r > 0 ? 0x1.fp127f : r;
+  hi = fits ? r + e : over && r < 0 ? -0x1.fp127f : r;
+}
+
 // Which of this lane's chunks lie in a group that stays (bits), from the groups' keys.
 // Groups of 4, 8, .. 64 experts are lanes of one chunk; of others the ranks are read from
-// LDS key by key and bits has one per expert.  near: where the worst group kept and the
-// best one not are not further apart than gap (0: keys are exact, ties as defined), the
-// experts that decide between them, which are those not key_gap below what their group
-// ranks by.
+// LDS key by key and bits has one per expert.  near: where a group kept and one not may
+// have changed places by the error err of their keys' scores (0: keys are exact, ties as
+// defined), the experts that decide between such groups, which are those not clearly below
+// what their group ranks by.
 template <int N>
-__device__ __forceinline__ uint32_t groups_kept(const Gating& g, const float (&of)[N], float gap, float key_gap, float* row,
-                                                uint32_t& near) {
+__device__ __forceinline__ uint32_t groups_kept(const Gating& g, const float (&of)[N], float err, float* row, uint32_t& near) {
   const int q = lane_id() & 15;
   const float none = minus_inf<float>();
-  float worst = -none, best = none;   // of the groups kept, of the others
+  const bool two = g.group_top == 2;
+  float worst = -none, best = none;   // the least that a kept group's rank may be, the most that another's may
   uint32_t left = 0;
   if (g.lanes > 0) {
-    float r[N / 4], last[N / 4];   // ranks, and the least key in them
+    float r[N / 4], last[N / 4], lo[N / 4], hi[N / 4];   // ranks, the least key in them, their bounds
     const int mine = q / g.lanes, per = 16 / g.lanes;
 #pragma unroll
     for (int c = 0; c < N / 4; ++c) {
@@ -165,8 +178,9 @@ __device__ __forceinline__ uint32_t groups_kept(const Gating& g, const float (&o
       if (g.lanes > 2) merge_two<0x4E>(h, l);     // quad_perm [2, 3, 0, 1]
       if (g.lanes > 4) merge_two<0x141>(h, l);    // row_half_mirror
       if (g.lanes > 8) merge_two<0x140>(h, l);    // row_mirror
-      r[c] = g.group_top == 2 ? __builtin_fmaxf(h + l, none) : h;
-      last[c] = g.group_top == 2 ? l : h;
+      r[c] = two ? __builtin_fmaxf(h + l, none) : h;
+      last[c] = two ? l : h;
+      rank_bounds(h, l, r[c], two, err, lo[c], hi[c]);
       const int grp = c * per + mine;
       if (q % g.lanes == 0 && grp < g.n_group) row[grp] = r[c];
     }
@@ -184,24 +198,27 @@ __device__ __forceinline__ uint32_t groups_kept(const Gating& g, const float (&o
       if (c * per + mine >= g.n_group) continue;
       if (ahead[c] < g.topk_group) {
         left |= 15u << (4 * c);
-        worst = fminf(worst, r[c]);
+        worst = fminf(worst, lo[c]);
       } else {
-        best = larger(best, r[c]);
+        best = larger(best, hi[c]);
       }
     }
     worst = -row_max(-worst);
     best = row_max(best);
-    if (gap > 0.f && !(worst - best > gap))
+    if (err > 0.f && !(worst > best))
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (r[i / 4] >= worst - gap && r[i / 4] <= best + gap && !(of[i] < last[i / 4] - key_gap)) near |= 1u << i;
+      for (int i = 0; i < N; ++i) {
+        const int c = i / 4;
+        const bool open = left >> i & 1 ? lo[c] <= best : hi[c] >= worst;
+        if (open && !(of[i] < last[c] - (2 * err + 0x1p-22f * fabsf(last[c])))) near |= 1u << i;
+      }
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i)
       if (expert_at(i, q) < g.E) row[expert_at(i, q)] = of[i];
     wave_lds_fence();
     // lane q ranks groups q and q + 16
-    float r[2];
+    float r[2], lo[2], hi[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       float a = none, b = none;
@@ -211,7 +228,8 @@ __device__ __forceinline__ uint32_t groups_kept(const Gating& g, const float (&o
           b = larger(b, fminf(v, a));
           a = larger(a, v);
         }
-      r[h] = g.group_top == 2 ? __builtin_fmaxf(a + b, none) : a;
+      r[h] = two ? __builtin_fmaxf(a + b, none) : a;
+      rank_bounds(a, b, r[h], two, err, lo[h], hi[h]);
     }
     wave_lds_fence();
 #pragma unroll
@@ -227,9 +245,9 @@ __device__ __forceinline__ uint32_t groups_kept(const Gating& g, const float (&o
       if (grp >= g.n_group) continue;
       if (ahead < g.topk_group) {
         in |= 1u << grp;
-        worst = fminf(worst, r[h]);
+        worst = fminf(worst, lo[h]);
       } else {
-        best = larger(best, r[h]);
+        best = larger(best, hi[h]);
       }
     }
     in = (uint32_t)row_fold((int)in, [](int a, int b) { return a | b; });
@@ -237,7 +255,7 @@ __device__ __forceinline__ uint32_t groups_kept(const Gating& g, const float (&o
     for (int i = 0; i < N; ++i) left |= (in >> (min(expert_at(i, q), g.E - 1) / g.size) & 1u) << i;
     worst = -row_max(-worst);
     best = row_max(best);
-    if (gap > 0.f && !(worst - best > gap)) near = ~0u;
+    if (err > 0.f && !(worst > best)) near = ~0u;
   }
   wave_lds_fence();
   return left;
@@ -434,8 +452,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_route_scored(Gating g, const flo
     bool sure = true;
     const bool two = g.n_group > 1 && g.group_top == 2;
     if (BIAS || two || (!g.sigmoid && !g.renorm)) fast_scores<N>(g, z, s, m, total);
-    // a key's error in fp32, twice, and half a step of each of two keys
-    float gap = g.sigmoid ? 0x1p-21f : 0x1p-18f;
+    // a score's error, and that of the difference of two keys: half a step of each besides
+    const float err = g.sigmoid ? 0x1p-22f : 0x1p-19f;
+    float gap = 2 * err;
     float top = minus_inf<float>();
     uint32_t left = ~0u;
     // keys, into s with a bias
@@ -454,11 +473,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_route_scored(Gating g, const flo
     constexpr float WINDOW = BIAS ? 2.f : 32.f;
     if (BIAS) gap += 0x1p-23f * (fabsf(top) + WINDOW);
     if (g.n_group > 1) {
-      // (a rank of two keys: twice the error, and the sum's rounding)
-      const float rank_gap = two ? 2 * gap + 0x1p-22f * (BIAS ? fabsf(top) + WINDOW : 2.f) : BIAS ? gap : 0.f;
       uint32_t near = 0;
-      if (BIAS || two) left = groups_kept<N>(g, s, rank_gap, gap, (float*)rows[tok], near);
-      else left = groups_kept<N>(g, z, 0.f, 0.f, (float*)rows[tok], near);
+      if (BIAS || two) left = groups_kept<N>(g, s, 1.0625f * err, (float*)rows[tok], near);
+      else left = groups_kept<N>(g, z, 0.f, (float*)rows[tok], near);
       if (__any(near != 0)) left = near_groups<BIAS, N>(g, s, zr, sel_bias, near, rows[tok]);
     }
     if (!(fabsf(top) < __builtin_inff())) sure = false;

@@ -369,3 +369,55 @@ def test_logits_around_every_power_of_two(score):
 def test_biases_far_from_zero(T, E, k, how, shift):
     z, b = draw(T, E, True, 5)
     check(z, (b + np.float32(shift)).astype(np.float32), k, how)
+
+
+@pytest.mark.parametrize("off", [-50, -1e3, -1e4, -1e5, -1e6, -1e7, -1e9])
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("E,ks,how", [(64, (3, 6), dict(n_group=8, topk_group=3, group_top=2)), (256, (4, 8), dict(n_group=8, topk_group=4, group_top=2)),
+                                      (128, (1, 4), dict(n_group=2, topk_group=1, group_top=2)), (64, (6, 14), dict(n_group=16, topk_group=4)),
+                                      (60, (2, 5), dict(n_group=5, topk_group=2, group_top=2)), (48, (4, 5), dict(n_group=16, topk_group=5, group_top=2)),
+                                      (256, (1, 8), dict(n_group=2, topk_group=1, group_top=2)), (48, (5, 11), dict(n_group=16, topk_group=4))])
+def test_groups_with_experts_switched_off(E, ks, how, score, off):
+    """One expert per group, or every expert of three groups, carries no bias and the others a
+    large negative one: ranks hold keys whose steps are far larger than the largest key's.
+    The choices end among the experts that are on, and reach those that are off.
+    Scores lie about as close as those steps, so that fp32 ranks of different groups tie or
+    change places."""
+    how, n = dict(how, score=score), how["n_group"]
+    rng = np.random.default_rng([E, n])
+    b = np.full((n, E // n), off, dtype=np.float32)
+    if how.get("group_top") == 2:
+        b[np.arange(n), rng.integers(0, E // n, n)] = 0
+    else:
+        b[:3] = 0
+    for steps in (0.5, 4, 64):
+        spread = min(1.0, steps * abs(off) * 2.0 ** -23 * (4 if score == "sigmoid" else E))
+        for k in ks:
+            check((0.3 + spread * rng.standard_normal((1500, E))).astype(np.float32), b.ravel(), k, how)
+
+
+@pytest.mark.parametrize("how", [dict(n_group=8, topk_group=3, group_top=2), dict(n_group=8, topk_group=3), dict(n_group=16, topk_group=9, group_top=2)])
+def test_groups_with_biases_of_every_size(how):
+    """Biases of both signs from 1e-3 to the largest of fp32, the type's lowest value and
+    -inf among them; ranks that fp32 cannot hold."""
+    rng = np.random.default_rng(6)
+    low = np.finfo(np.float32).min
+    for E in (64, 96, 256):
+        for trial in range(12):
+            b = np.exp(rng.uniform(-7, 86 if trial % 2 else 30, E)) * rng.choice((-1, -1, -1, 1), E)
+            b[rng.random(E) < 0.3] = (low, -np.inf, 0, -3e38)[trial % 4]
+            b[rng.random(E) < 0.2] = (0, low, low, -2.9e38)[trial % 4]
+            z, _ = draw(150, E, False, trial, (1.0, 1e-6)[trial % 2])
+            with np.errstate(over="ignore"):
+                check(z, b.astype(np.float32), 6, dict(how, score=("sigmoid", "softmax")[trial // 2 % 2]))
+
+
+def test_groups_masked_by_the_lowest_value():
+    """Whole groups off by the type's lowest value: one rank that fp32 cannot hold, or that
+    ties with others."""
+    z, _ = draw(400, 64, False, 7)
+    b = np.zeros((8, 8), dtype=np.float32)
+    b[[1, 2, 4, 5, 6]] = np.finfo(np.float32).min
+    for kept in (2, 3, 4):
+        for top in (1, 2):
+            check(z, b.ravel(), 6, dict(score="sigmoid", n_group=8, topk_group=kept, group_top=top))
