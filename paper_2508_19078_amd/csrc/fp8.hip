@@ -98,7 +98,7 @@ __device__ __forceinline__ F8Block f8_block_h(uint32_t bits) {
   F8Block b;
   const float top = fmaxf(__uint_as_float(bits), F8_FLOOR);
   b.scale = bits ? top * (1.f / F8_TOP) : 0.f;
-  b.inv = F8_TOP * __builtin_amdgcn_rcpf(top);
+  b.inv = F8_TOP * 0x1p-8f * __builtin_amdgcn_rcpf(top * 0x1p-8f);   // (1 / top itself may be below the normal range, where it is 0)
   if (bits >= 0x7F800000u) {
     b.scale = __uint_as_float(0x7FC00000u);
     b.inv = 0.f;

@@ -130,3 +130,23 @@ def test_small_tiles(name):
 @pytest.mark.parametrize("name", list(LARGE_CASES))
 def test_large_tiles(name):
     forward(LARGE_CASES[name])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,want", [(3, FEW), (100, SMALL), (600, LARGE)])
+def test_h_at_the_top_of_fp32(T, want):
+    """Finite blocks of H whose largest value lies between 2^126 and the top of fp32: 448 over
+    it is a normal number, its plain reciprocal is not."""
+    d, E, I = 256, 2, 272
+    assert path(T, d, E, 1, I, 0) == want
+    X, w, offsets, tok = M.draw(T, d, E, 1, I, 0, E)
+    X = X.abs()
+    w["g"] = w["g"].abs() * 0.75                              # the gate's sums are some 3 to 20
+    a, u = (np.concatenate([X.double().numpy() @ x.double().numpy().T for x in w[m]]) for m in "gu")
+    H = np.abs(a * O.sigmoid(a) * u)
+    e = np.floor(127.9 - np.log2(H.max()))                    # 7 % are left for what quantisation adds
+    tops = np.maximum.reduceat(H * 2.0 ** e, np.arange(0, I, 128), axis=1)
+    assert (tops > 2.0 ** 126).mean() > 0.05 and a.min() > 2
+    w["u"], w["d"] = w["u"] * 2.0 ** e, w["d"] * 2.0 ** -100
+    got = M.run(M.tables(w, d, E, 1, I, 0), X, offsets, tok, T, 1, 0, d)
+    M.check(got, X, w, offsets, tok, T, d, E, 1, I, 0)
