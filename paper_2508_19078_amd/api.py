@@ -7,8 +7,10 @@ happens here.  If the library is not built, the first call raises.
 """
 from __future__ import annotations
 
+import bisect
 import ctypes
 import os
+import weakref
 from typing import List, Optional, Sequence
 
 import torch
@@ -711,12 +713,32 @@ def moe_grad_norm(grads, sumsq, norm, ws, accumulate=False, stream=None):
 
 def moe_grad_clip(grads, sumsq, max_norm, out=None, eps=1e-6, stream=None):
     """Scales grads (a TensorSet) by min(1, max_norm / (sqrt(sumsq) + eps)), in place or into
-    the TensorSet out, whose tensors have the same sizes."""
+    the TensorSet out, whose tensors have the same sizes and are each grads' own or apart
+    from all of grads'."""
     v = _device()
-    if out is not None and out.sizes != grads.sizes:
-        raise ValueError("out has other sizes than grads")
+    if out is not None:
+        if out.sizes != grads.sizes:
+            raise ValueError("out has other sizes than grads")
+        out.results_of(grads)
     return _call("moe_grad_clip", _set_on(v, "grads", grads), _arg(v, "sumsq", sumsq, torch.float64, (1,)), float(max_norm),
                  float(eps), None if out is None else _set_on(v, "out", out), stream_ptr(stream))
+
+
+def _spans(tensors):
+    """(first address, address behind the end, index) of the tensors with elements, by address."""
+    return sorted((t.data_ptr(), t.data_ptr() + t.nbytes, i) for i, t in enumerate(tensors) if t is not None and t.numel())
+
+
+def _check_results(spans, of):
+    """Refuses results (spans) that share memory with another of the tensors they are made
+    of than their own, or with a part of it: one would be written while it is read."""
+    begins = [s[0] for s in of]
+    for begin, end, i in spans:
+        j = max(bisect.bisect_right(begins, begin) - 1, 0)
+        while j < len(of) and of[j][0] < end:
+            if of[j][1] > begin and of[j] != (begin, end, i):
+                raise ValueError(f"out[{i}] and grads[{of[j][2]}] share memory")
+            j += 1
 
 
 class TensorSet:
@@ -739,8 +761,8 @@ class TensorSet:
             if t.device != dev:
                 raise ValueError(f"tensors[{i}] is on {t.device}, the set is on {dev}")
         # a tensor named twice, or a view of another, would be counted and clipped twice
-        spans = sorted((t.data_ptr(), t.data_ptr() + t.nbytes, i) for i, t in enumerate(self.tensors) if t is not None and t.numel())
-        for (_, end, i), (begin, _, j) in zip(spans, spans[1:]):
+        self.spans = _spans(self.tensors)
+        for (_, end, i), (begin, _, j) in zip(self.spans, self.spans[1:]):
             if begin < end:
                 raise ValueError(f"tensors[{i}] and tensors[{j}] share memory")
         self.sizes = [0 if t is None else t.numel() for t in self.tensors]
@@ -754,6 +776,15 @@ class TensorSet:
                                                                  for t in self.tensors], dtype=I64, device=dev)
         base = self.tables.data_ptr()
         self.struct = moe_tensor_set(n, code, base + 8 * at, base, start[-1])
+        self._checked = None   # the set whose results these were last (weakly)
+
+    def results_of(self, grads: "TensorSet"):
+        """Refuses to be what grads' scaled copies go to, where that would race.  (Sets do
+        not change, so that a step's two are compared once.)"""
+        if self is grads or (self._checked is not None and self._checked() is grads):
+            return
+        _check_results(self.spans, grads.spans)
+        self._checked = weakref.ref(grads)
 
 
 # ----------------------------------------------------- layer descriptor ----

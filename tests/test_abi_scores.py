@@ -290,3 +290,43 @@ def test_binding_refuses_tensors_it_would_misread():
         api.moe_grad_clip(a, t(1, dt=D), 1.0, out=api.TensorSet([t(4), t(3, 5)]))
     with pytest.raises(api.MoeError, match="workspace"):
         api.moe_grad_norm(a, t(1, dt=D), t(1), t(8))
+
+
+def results(grads, outs):
+    api._check_results(api._spans(outs), api._spans(grads))
+
+
+def test_results_that_would_be_written_while_they_are_read():
+    """Addresses alone decide, so host tensors stand for device ones."""
+    x, y, z = torch.zeros(64), torch.zeros(32), torch.zeros(64)
+    a, b = x[8:24], x[24:40]
+    grads = [a, None, b, y]
+    for outs in (grads, [z[:16], None, z[16:32], y], [a, None, z[:16], z[16:48]], [x[:8], None, x[40:56], z[:32]], [x[:0], None, z[:0], x[8:8]]):
+        results(grads, outs)
+    for outs, word in (([x[9:25], None, z[:16], y], r"out\[0\] and grads\[0\]"), ([x[7:23], None, z[:16], y], r"out\[0\] and grads\[0\]"),
+                       ([z[:16], None, a, y], r"out\[2\] and grads\[0\]"), ([b, None, a, y], "share memory"),
+                       ([z[:16], None, z[16:32], x[:32]], r"out\[3\] and grads\[0\]"), ([z[:16], None, z[16:32], x[39:]], r"out\[3\] and grads\[2\]"),
+                       ([z[:16], y[:16], z[16:32], z[32:]], r"out\[1\] and grads\[3\]"), ([x, None, z[:16], y], r"out\[0\] and grads"),
+                       ([a[:15], None, z[:16], y], r"out\[0\] and grads\[0\]")):
+        with pytest.raises(ValueError, match=word):
+            results(grads, outs)
+    many = [t[1:] for t in torch.zeros(4096).split(4)]
+    results(many, many)
+    results(many, [torch.zeros(3) for _ in many])
+    with pytest.raises(ValueError, match=r"out\[700\] and grads\[701\]"):
+        results(many, many[:700] + [many[701]])
+
+
+@pytest.mark.gpu
+def test_binding_refuses_results_that_share_memory():
+    t = lambda *s, dt=F: torch.zeros(*s, dtype=dt, device="cuda")  # noqa: E731
+    x, sumsq = t(300), t(1, dt=D)
+    grads = api.TensorSet([x[:100], None, x[100:200]])
+    for outs in ([x[1:101], None, x[150:250]], [x[100:200], None, x[:100]], [x[:100], None, x[101:201]]):
+        with pytest.raises(ValueError, match="share memory"):
+            api.moe_grad_clip(grads, sumsq, 1.0, out=api.TensorSet(outs))
+    apart, mixed = api.TensorSet([t(100), None, x[200:]]), api.TensorSet([x[:100], None, x[200:]])
+    for _ in range(2):                                     # compared once, and again with another set between
+        for out in (apart, mixed, grads):
+            api.moe_grad_clip(grads, sumsq, 1.0, out=out)
+    assert not x.any()
