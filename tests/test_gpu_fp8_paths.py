@@ -150,3 +150,52 @@ def test_h_at_the_top_of_fp32(T, want):
     w["u"], w["d"] = w["u"] * 2.0 ** e, w["d"] * 2.0 ** -100
     got = M.run(M.tables(w, d, E, 1, I, 0), X, offsets, tok, T, 1, 0, d)
     M.check(got, X, w, offsets, tok, T, d, E, 1, I, 0)
+
+
+def dropped(xc, xs, wc, ws):
+    """Variance of what the matrix unit drops of each sum of x W^T: of the products of 8
+    consecutive k, each the part below 2^(e - 13), of its product's sign, with e the largest
+    sum of exponents among them (whole scale blocks only).  A product has 6 bits behind its
+    leading one, so that those within 7 binades of the largest lose nothing."""
+    ex, ew = (np.maximum(np.frexp(v)[1] - 1, -6) for v in (xc, wc))
+    out = np.zeros((len(xc), len(wc)))
+    for b in range(xc.shape[1] // 128):
+        f = xs[:, b][:, None] * np.repeat(ws[:, b], 128)[None, :len(wc)]
+        for g in range(128 * b, 128 * b + 128, 8):
+            c = slice(g, g + 8)
+            p = np.abs(xc[:, None, c] * wc[None, :, c])
+            unit = np.exp2(np.where(p != 0, ex[:, None, c] + ew[None, :, c], -99).max(-1, keepdims=True) - 13.0)
+            out += f ** 2 * (np.mod(p, unit) ** 2).sum(-1)
+    return out
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,want", [(3, FEW), (100, SMALL), (600, LARGE)])
+def test_how_many_codes_of_h_the_matrix_unit_moves(T, want):
+    """W_down as the unit matrix, so that O holds what H's codes stand for, counted against the
+    formula's.  A code moves where the error of its H over the block's scale crosses a border:
+    with probability E|error| / step, at most the standard deviation in steps.  That is
+    the sums' (`dropped`; a few tokens drop nothing of them), carried through the formula, and
+    that of the block's largest H, which is its scale's.  A quarter and four standard deviations of the
+    count on top; with one bit less in the unit more than twice as many move."""
+    d, I = 256, 128
+    assert path(T, d, 1, 1, I, 0) == want
+    X, w, offsets, tok = M.draw(T, d, 1, 1, I, 0, 1)
+    w["d"] = torch.eye(d, I).to(M.BF)[None]
+    got = M.run(M.tables(w, d, 1, 1, I, 0), X, offsets, tok, T, 1, 0, d).double().cpu().numpy()
+    x = X.double().numpy()[tok]
+    (xc, xs), wg, wu = O.fp8_rows(x), *(O.fp8_rows(w[m][0].double().numpy(), 128) for m in "gu")
+    a, u = ((xc * O.fp8_spread(xs, T, d, 1)) @ (c * O.fp8_spread(s, I, d, 128)).T for c, s in (wg, wu))
+    sig = O.sigmoid(a)
+    H = a * sig * u
+    var = 0.0 if want == FEW else (u * sig * (1 + a * (1 - sig))) ** 2 * dropped(xc, xs, *wg) + (a * sig) ** 2 * dropped(xc, xs, *wu)
+    var = var + (H * 16 * 2.0 ** -23) ** 2                     # fp32 sums and the logistic function, amply
+    val, s = O.fp8_rows(H)
+    q, top = np.abs(H) / s, np.abs(H).argmax(1)[:, None]
+    off = np.take_along_axis(var, top, 1) / np.take_along_axis(H, top, 1) ** 2
+    step = np.exp2(np.maximum(np.frexp(q)[1] - 1, -6) - 3)
+    p = np.minimum(np.sqrt(var / s ** 2 + q ** 2 * off) / step, 1).sum()
+    moved = int((np.abs(got[:, :I] - val * s) > 0.25 * step * s).sum())
+    M.log(f"  {moved} of {H.size} codes moved, {p:.1f} expected at most")
+    assert not got[:, I:].any()
+    assert moved <= 1.25 * p + 4 * np.sqrt(p) + 1
