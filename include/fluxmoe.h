@@ -683,7 +683,8 @@ size_t moe_grouped_swiglu_fwd_mx4_workspace_size(const moe_layer_mx4* L, int T, 
  * what of the others lies below 2^-13 of it (the rounding of that largest product's own
  * operands to 8 bits weighs 2^-4), but for gate and up in calls of a few tokens, where no
  * average over rows hides an element of H that takes the other code for it.  H is
- * quantised from its fp32 values and not written out.  X [T,d] bf16 is quantised once
+ * quantised from its fp32 values (in larger calls with scale and quotient to an ulp) and
+ * not written out.  X [T,d] bf16 is quantised once
  * per token; routed row p reads token perm_token[p] (moe_permute's; values clamped to
  * [0, T)), so X_perm is not needed.  offsets, the row space and O [R_tot, d] bf16 as
  * in moe_grouped_swiglu_fwd; O's rows behind the last routed one are left as they

@@ -714,7 +714,7 @@ def moe_grad_norm(grads, sumsq, norm, ws, accumulate=False, stream=None):
 def moe_grad_clip(grads, sumsq, max_norm, out=None, eps=1e-6, stream=None):
     """Scales grads (a TensorSet) by min(1, max_norm / (sqrt(sumsq) + eps)), in place or into
     the TensorSet out, whose tensors have the same sizes and are each grads' own or apart
-    from all of grads'."""
+    from all of grads'.  max_norm and eps are passed on in fp32."""
     v = _device()
     if out is not None:
         if out.sizes != grads.sizes:

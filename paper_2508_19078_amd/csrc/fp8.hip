@@ -14,7 +14,9 @@
 // (128-row tiles of at most 64 rows so: 333 tokens 130 us to 133, 32 tokens 41 to 55).
 // Only calls of a few tokens, which wait for bytes and not for the matrix unit, take gate
 // and up in bf16 (1 token 13.9 us to 14.7): a large element's step is 0.6 % of one token's
-// output there, and 2e-3 is what many rows leave of it.
+// output there, and 2e-3 is what many rows leave of it.  Their down product stays at 8 bits:
+// no code hangs on it, the error of O is 1.7e-3 with either (its rounding to bf16), and
+// bf16 products there took 2 to 8 % more time (1 token 14.4 us to 14.8, 4 tokens 23.7 to 25.5).
 //
 // * A slab row is one 128-byte line; slabs go global -> LDS with global_load_lds_dwordx4, 8
 //   rows per instruction, into a ring of RING slabs, the scales of 4 slabs of a row (16
@@ -33,10 +35,11 @@
 // 1.2 and the requests alone 1.4 to 1.55; a tile's lookup, first slab and epilogue 9 us.
 // It is bound by power as much as by waiting: the clock falls to 1.9 GHz, and with all codes
 // zero the same call takes 11 % less; with all blocks on the same rows and weights (L2 only)
-// 5 % less.  32x32x64 products gave 2.16 us a slab, three slabs of activations with two of
-// weights 2.11, padding activation rows to odd lines nothing, bands of 4 to 16 row tiles
+// 5 % less.  Padding activation rows to odd lines gave nothing, bands of 4 to 16 row tiles
 // nothing or 4 % more time, wave priorities nothing.  The next tile's first slab requested
-// before the epilogue, with the slots' tables in LDS: 1 to 6 % more.
+// before the epilogue, with the slots' tables in LDS: 1 to 6 % more.  Of builds whose gate
+// and up took 2.2 ms and more, before its requests were spread: 32x32x64 products 2.16 us a
+// slab, three slabs of activations with two of weights 2.11.
 #include <type_traits>
 #include <utility>
 
@@ -643,16 +646,18 @@ typedef F8Cfg<64, 3, 128> E128h;
 
 // --------------------------------------------------------- a few tokens ----
 // Calls of a few tokens are bound by latency and by the weights' bytes, which have to be
-// spread over all compute units: a block takes 8 columns of H (8 gate and 8 up rows, one
-// fragment of v_mfma_f32_16x16x128_f8f6f4: lane l row l % 16, 32 k from l / 16 on), or 32 of
-// O, of one slot, and its NW waves split the slabs of 128 k into consecutive parts whose
-// sums meet in LDS.  A wave requests BS slabs of weights straight into registers, and the
-// block quantises its activation rows into LDS while they are on their way.  H goes
-// through the workspace in fp32 and is quantised the same way.  Rows come 16 at a time.
-// Blocks exist for the slots that may hold rows only.  d = 4096, I = 688, one token on 4
-// slots: 11.8 us gate and up (22.5 MB), 4.6 down (11.3 MB), each a chain of slot, pointers,
-// rows and their sums; 8 waves per block in place of 4: 13 us a call here for 14, 27 for 24 with
-// two tokens of d = 2048, I = 1408.
+// spread over all compute units: a block takes 8 columns of H (8 gate and 8 up rows: 16
+// rows of one operand), or 32 of O (two operands), of one slot, and its NW waves split the
+// slabs of 128 k into consecutive parts whose sums meet in LDS.  Lane l has row l % 16 and 32 k
+// from l / 16 on; gate and up widen them for four v_mfma_f32_16x16x32_bf16 per slab, the
+// down product is one v_mfma_f32_16x16x128_f8f6f4.  A wave requests BS slabs of weights
+// straight into registers, and the block quantises its activation rows, all of the slot's
+// up to one per token (at most 16), into LDS while they are on their way.  H goes through the
+// workspace in fp32 and is quantised the same way.  Blocks exist for the slots that may
+// hold rows only.  d = 4096, I = 688, one token on 4 slots: 11.1 us gate and up (22.5 MB),
+// 4.4 down (11.3 MB), 14.4 a call among others, each a chain of slot, pointers, rows and
+// their sums.  8 waves per block in place of 4, when gate and up were 8-bit products: 13 us a
+// call here for 13.9, 27 for 24 with two tokens of d = 2048, I = 1408.
 
 // Rows of nb 128-blocks in LDS: codes, then scales; padded so that 16 rows' chunks at one
 // place lie on different banks.
@@ -879,6 +884,8 @@ int fp8_tile(const moe_layer_fp8* L, int T, int k) {
   // 191; 187 232, 225; 234 262, 249; 272 276, 279; 300 291, 299; 384 342, 357; 512 417, 444.
   // d = 4096, I = 688, 16 slots: 128 rows 87, 65; 256 93, 78; 272 93, 80; 320 96, 113.  d = 4096,
   // I = 1024, 64 slots: 128 rows 284, 258; 192 312, 307; 256 369, 375; 300 399, 406; 512 580, 623.
+  // Rows alone decide.  Where few slots and columns leave compute units without a tile, the
+  // border lies higher: 272 rows of the second layer lose 16 % by this rule.
   const double r = (double)T * (k + L->S_shared) / active;
   return r >= 272 ? 256 : 128;
 }

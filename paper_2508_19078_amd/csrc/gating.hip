@@ -422,9 +422,9 @@ __device__ __forceinline__ int order_exact(const Gating& g, const float* zr, con
 // a histogram of its own, as many as the registers allow (additions to one address come
 // some 17 ns apart, whatever block they are of: 512 blocks cost 8.6 us).
 //
-// Bound by the rounds' vector instructions, and by latency at few tokens: 1 token 3.6 us; 1000
-// of 60 experts, top-5, 5.3; 8192 of 64, top-6 in groups, 5.8 without counts and 9.9 with; 32768
-// of 256, top-8 from 4 of 8 groups, 35 and 38.8 (34 MB: 6.6 us of bytes).  Selecting on fp64 keys
+// Bound by the rounds' vector instructions, and by latency at few tokens: 1 token 3.3 us; 1000
+// of 60 experts, top-5, 5.6; 8192 of 64, top-6 in groups, 5.8 without counts and 10.1 with; 32768
+// of 256, top-8 from 4 of 8 groups, 35 and 38.6 (34 MB: 6.6 us of bytes).  Selecting on fp64 keys
 // throughout, that last pass and its gradient took 136 us in place of 50.
 template <int N, bool BIAS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_route_scored(Gating g, const float* __restrict__ logits,
@@ -556,8 +556,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_route_scored(Gating g, const flo
 }
 
 // The logits' gradient: lane j forms the share of choice j, the shares meet in an LDS row,
-// which goes out 16 bytes per lane.  Bound by the bytes of dlogits: 32768 x 256 in 11.0
-// us (36 MB, 3.3 TB/s), 8192 x 64 in 3.8.
+// which goes out 16 bytes per lane.  Bound by the bytes of dlogits: 32768 x 256 in 11.2
+// us (36 MB, 3.2 TB/s), 8192 x 64 in 4.0.
 template <int N>
 __global__ __launch_bounds__(256) void k_route_scored_bwd(Gating g, const float* logits, const int32_t* __restrict__ idx,
                                                           const float* __restrict__ dgate, int T, float* dlogits,
